@@ -256,6 +256,118 @@ incvit_status incvit_flow_two_anchor(int32_t S, int64_t n, const float* x0, cons
                                      const float* v7, const float* alpha, const float* beta,
                                      const float* b, float* xT, void* stream);
 
+/* ------------------------------------------------------ rotary positions -- */
+
+/* Rotary positions with one to three axes (time, height, width), for images
+ * and videos.  The rotated dims of a head are `pairs[0] + .. + pairs[axes - 1]`
+ * pairs; pair i belongs to one axis a as its j-th pair and turns by
+ *   angle = position_a * f,   f = scale[a] * theta^(-j / pairs[a])  (ladder AXIS)
+ *                             f = scale[a] * theta^(-i / sum pairs) (ladder HEAD).
+ * layout BLOCKS: the first axis has the first pairs[0] pairs, and so on; CYCLE:
+ * the pairs are dealt to the axes in turn, an axis that has all of its own
+ * being passed over.  1 <= axes <= 3, pairs[a] >= 1 for a < axes, at most 128
+ * pairs, theta in [1, 1e12], 0 < |scale| <= 2^20 (1 unless positions are
+ * stretched or count something else than the model's unit). */
+typedef enum { INCVIT_LADDER_AXIS = 0, INCVIT_LADDER_HEAD = 1 } incvit_ladder;
+typedef enum { INCVIT_LAYOUT_BLOCKS = 0, INCVIT_LAYOUT_CYCLE = 1 } incvit_layout;
+
+typedef struct {
+  int32_t axes;
+  int32_t pairs[3];
+  int32_t ladder; /* incvit_ladder */
+  int32_t layout; /* incvit_layout */
+  double theta;
+  double scale[3];
+} incvit_rope;
+
+/* An image (t = 1), a video, or a tile of either: t frames of h x w tokens whose
+ * first one is at (t0, y0, x0). */
+typedef struct {
+  int32_t t, h, w;
+  int32_t t0, y0, x0;
+} incvit_grid;
+
+/* Cosines and sines of the tokens' angles: table[token][pair] = (cos, sin),
+ * device fp32 [tokens][pairs][2], 8-byte aligned.  pos: device int32, token k's
+ * position on axis a at pos[a * axis_stride + k * token_stride] (any value,
+ * negative too; strides in elements, in [0, 2^40]).  tokens >= 0 (none: nothing
+ * is enqueued), tokens * pairs < 2^31.  Angles are formed and reduced in 64 bits: their error
+ * in radians is about 2^-52 of the angle.  Errors: INCVIT_ERR_ARG (text:
+ * incvit_last_error(NULL)).  Asynchronous on `stream`. */
+incvit_status incvit_rope_table(const incvit_rope* r, int64_t tokens, const int32_t* pos,
+                                int64_t axis_stride, int64_t token_stride, float* table,
+                                void* stream);
+
+/* The same for the tokens of n grids, packed one after another: frame by frame,
+ * and a frame in windows of merge x merge tokens (window rows, then windows,
+ * then the rows and columns inside one; merge = 1: row by row).  With three
+ * axes a token is at (t0 + frame, y0 + row, x0 + column), with two at (y0 + row,
+ * x0 + column), with one at t0 + its number within the grid counted frame by
+ * frame and row by row (whatever merge is).  grids: HOST [n], read before the
+ * call returns; sizes >= 1, h and w multiples of merge >= 1; n >= 0; tokens and
+ * table as above. */
+incvit_status incvit_rope_table_grids(const incvit_rope* r, int32_t n, const incvit_grid* grids,
+                                      int32_t merge, float* table, void* stream);
+
+/* ------------------------------------------- head norms and the rotation -- */
+
+/* What is done to every head x of a row (d = head_dim values, fp32 inside, one
+ * rounding to the storage type at the end):
+ *   norm RMS:   x * 1/sqrt(mean(x^2) + eps) * gamma
+ *   norm LAYER: (x - mean) * 1/sqrt(var + eps) * gamma + beta  (biased variance)
+ *   norm NONE:  x
+ * and then pair i of the first rot_dim values, (x_i, x_{i + rot_dim/2}) with
+ * HALVES or (x_{2i}, x_{2i+1}) with ADJACENT, becomes
+ *   (x_a cos - x_b sin, x_b cos + x_a sin)
+ * with (cos, sin) of pair i in the row's table row; the values past rot_dim stay
+ * as the norm left them.  2 <= head_dim <= 256, even; 0 <= rot_dim <= head_dim,
+ * even (0: no rotation, no table); eps >= 0 and finite. */
+typedef enum { INCVIT_NORM_NONE = 0, INCVIT_NORM_RMS = 1, INCVIT_NORM_LAYER = 2 } incvit_norm;
+typedef enum { INCVIT_PAIR_HALVES = 0, INCVIT_PAIR_ADJACENT = 1 } incvit_pairing;
+
+typedef struct {
+  int32_t dtype; /* incvit_dtype of all rows, gammas and betas */
+  int32_t head_dim, rot_dim;
+  int32_t pairing; /* incvit_pairing */
+  int32_t norm;    /* incvit_norm */
+  float eps;
+} incvit_qk;
+
+/* The heads of the queries or keys: head h of row r starts at element
+ * r * row + h * head of `in` (strides in elements, >= 0) and its values lie one
+ * after another, so q and k may be views of one projection output and grouped
+ * keys have fewer heads; likewise `out`, whose heads must not overlap.  `out`
+ * may be `in` with the same strides (not together with k_rows); any other
+ * overlap with the inputs is the caller's mistake.  gamma, beta: [head_dim], or
+ * NULL (ones, zeros); beta only with LAYER.  0 <= heads <= 65536. */
+typedef struct {
+  const void* in;
+  void* out;
+  const void* gamma;
+  const void* beta;
+  int64_t in_row, in_head, out_row, out_head;
+  int32_t heads;
+} incvit_heads;
+
+/* Norm and rotation of `rows` rows of queries and keys in one pass.  q or k may
+ * be NULL (the other alone).
+ *   table: fp32 [table_rows][rot_dim / 2][2] as incvit_rope_table writes it,
+ *     8-byte aligned; row r is rotated by table row index[r] (device int32
+ *     [rows]), or r % table_rows if index is NULL (frames that share a grid);
+ *   k_rows: device int32 [rows]: the row of k->out that row r's keys go to, of
+ *     k_out_rows rows (a cache); NULL: row r.  The rows must differ from each
+ *     other; rows of k->out that are not named keep what they hold.
+ * A row whose index is outside the table (padding: negative) gets no output,
+ * and one whose k_rows is outside [0, k_out_rows) no key.  rows >= 0 (none:
+ * nothing is enqueued), rows * heads < 2^31.  Any alignment of whole elements
+ * is served; 16-byte aligned heads take the fast path.  Errors: INCVIT_ERR_ARG,
+ * INCVIT_ERR_SHAPE or INCVIT_ERR_UNSUPPORTED (text: incvit_last_error(NULL)).
+ * Asynchronous on `stream`. */
+incvit_status incvit_qk_norm_rope(const incvit_qk* c, int64_t rows, const incvit_heads* q,
+                                  const incvit_heads* k, const float* table, int64_t table_rows,
+                                  const int32_t* index, const int32_t* k_rows, int64_t k_out_rows,
+                                  void* stream);
+
 /* ------------------------------------------------------------ HIP graphs -- */
 
 typedef struct incvit_graph incvit_graph;

@@ -11,6 +11,7 @@
 
 #include "common.hpp"
 #include "incvit.h"
+#include "ops.hpp"
 
 using namespace incvit;
 
@@ -366,6 +367,11 @@ struct incvit_graph {
   hipGraph_t graph = nullptr;
   hipGraphExec_t exec = nullptr;
 };
+
+incvit_status incvit::op_fail(incvit_status st, const char* msg) {
+  g_error = msg;
+  return st;
+}
 
 LaunchEvents& incvit::launch_events() {
   static thread_local LaunchEvents ev;

@@ -1,0 +1,153 @@
+// C ABI of the stand-alone operators: argument checks and launches.
+#include <cmath>
+
+#include "ops.hpp"
+
+using namespace incvit;
+
+namespace {
+
+bool is_dtype(int32_t t) { return t == INCVIT_F32 || t == INCVIT_BF16; }
+
+incvit_status launched(hipError_t e, const char* what) {
+  if (e == hipSuccess) return INCVIT_OK;
+  char buf[160];
+  snprintf(buf, sizeof buf, "%s: %s", what, hipGetErrorString(e));
+  return op_fail(INCVIT_ERR_HIP, buf);
+}
+
+// Whether rows x heads runs of d elements at r * row + h * head never overlap.
+bool disjoint(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t d) {
+  if (rows <= 1) return heads <= 1 || head >= d;
+  if (heads <= 1) return row >= d;
+  const int64_t lo = row < head ? row : head, hi = row < head ? head : row, n = row < head ? rows : heads;
+  return lo >= d && (n - 1 <= (hi - d) / lo) && hi >= d;
+}
+
+incvit_status check_heads(const incvit_qk& c, int64_t rows, int64_t out_rows, const incvit_heads* h, QkSide& s) {
+  s = QkSide{};
+  if (!h || h->heads == 0) return INCVIT_OK;
+  const uintptr_t eb = c.dtype == INCVIT_BF16 ? 2 : 4;
+  if (h->heads < 0 || h->heads > 65536) return op_fail(INCVIT_ERR_ARG, "heads must be in [0, 65536]");
+  if (!h->in || !h->out) return op_fail(INCVIT_ERR_ARG, "null rows of queries or keys");
+  if (((uintptr_t)h->in | (uintptr_t)h->out | (uintptr_t)h->gamma | (uintptr_t)h->beta) % eb)
+    return op_fail(INCVIT_ERR_ARG, "rows, gammas and betas must be aligned to their elements");
+  if (h->beta && c.norm != INCVIT_NORM_LAYER) return op_fail(INCVIT_ERR_ARG, "beta is given without a LayerNorm");
+  const int64_t most = (int64_t)1 << 40;
+  for (int64_t st : {h->in_row, h->in_head, h->out_row, h->out_head})
+    if (st < 0 || st > most) return op_fail(INCVIT_ERR_ARG, "strides must be in [0, 2^40] elements");
+  if (!disjoint(out_rows, h->out_row, h->heads, h->out_head, c.head_dim))
+    return op_fail(INCVIT_ERR_SHAPE, "heads of the output overlap");
+  if (h->in == h->out && ((rows > 1 && h->in_row != h->out_row) || (h->heads > 1 && h->in_head != h->out_head)))
+    return op_fail(INCVIT_ERR_SHAPE, "in place, the output's strides must be the input's");
+  s = QkSide{h->in, h->out, h->gamma, h->beta, (long)h->in_row, (long)h->in_head, (long)h->out_row, (long)h->out_head, h->heads};
+  return INCVIT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+incvit_status incvit_rope_table(const incvit_rope* r, int64_t tokens, const int32_t* pos, int64_t axis_stride, int64_t token_stride,
+                                float* table, void* stream) {
+  RopeArgs a = {};
+  if (!r) return op_fail(INCVIT_ERR_ARG, "null rope");
+  if (!rope_pairs(*r, a)) return op_fail(INCVIT_ERR_ARG, "rope out of range (axes, pairs, ladder, layout, theta or scale)");
+  if (tokens < 0 || tokens > INT32_MAX / a.pairs) return op_fail(INCVIT_ERR_ARG, "tokens must be >= 0 and tokens * pairs < 2^31");
+  if (tokens == 0) return INCVIT_OK;
+  if (!pos || !table) return op_fail(INCVIT_ERR_ARG, "null positions or table");
+  if ((uintptr_t)pos % 4 || (uintptr_t)table % 8) return op_fail(INCVIT_ERR_ARG, "positions must be 4-byte and the table 8-byte aligned");
+  const int64_t most = (int64_t)1 << 40;
+  if (axis_stride < 0 || axis_stride > most || token_stride < 0 || token_stride > most)
+    return op_fail(INCVIT_ERR_ARG, "strides must be in [0, 2^40] elements");
+  a.tokens = (int)tokens;
+  a.pos = pos;
+  a.axis_stride = (long)axis_stride;
+  a.token_stride = (long)token_stride;
+  a.table = table;
+  return launched(launch_rope(a, static_cast<hipStream_t>(stream)), "rope_table");
+}
+
+incvit_status incvit_rope_table_grids(const incvit_rope* r, int32_t n, const incvit_grid* grids, int32_t merge, float* table,
+                                      void* stream) {
+  RopeArgs a = {};
+  if (!r) return op_fail(INCVIT_ERR_ARG, "null rope");
+  if (!rope_pairs(*r, a)) return op_fail(INCVIT_ERR_ARG, "rope out of range (axes, pairs, ladder, layout, theta or scale)");
+  if (n < 0) return op_fail(INCVIT_ERR_ARG, "n must be >= 0");
+  if (n == 0) return INCVIT_OK;
+  if (!grids || !table) return op_fail(INCVIT_ERR_ARG, "null grids or table");
+  if ((uintptr_t)table % 8) return op_fail(INCVIT_ERR_ARG, "the table must be 8-byte aligned");
+  if (merge < 1) return op_fail(INCVIT_ERR_ARG, "merge must be >= 1");
+  int64_t tokens = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const incvit_grid& g = grids[i];
+    if (g.t < 1 || g.h < 1 || g.w < 1) return op_fail(INCVIT_ERR_ARG, "grid sizes must be >= 1");
+    if (g.h % merge || g.w % merge) return op_fail(INCVIT_ERR_SHAPE, "grid height and width must be multiples of merge");
+    const int64_t frame = (int64_t)g.h * g.w;
+    if (frame > INT32_MAX || g.t > INT32_MAX / frame) tokens = INT64_MAX / 2;
+    else tokens += frame * g.t;
+    if (tokens > INT32_MAX / a.pairs) return op_fail(INCVIT_ERR_ARG, "tokens * pairs must be < 2^31");
+  }
+  a.merge = merge;
+  for (int32_t i = 0; i < n; i += kGridsPerLaunch) {
+    a.n_grids = n - i < kGridsPerLaunch ? n - i : kGridsPerLaunch;
+    a.tokens = 0;
+    for (int j = 0; j < a.n_grids; ++j) {
+      const incvit_grid& g = grids[i + j];
+      a.grid[j] = RopeGrid{g.t, g.h, g.w, g.t0, g.y0, g.x0, a.tokens};
+      a.tokens += g.t * g.h * g.w;
+    }
+    a.table = table;
+    table += (size_t)a.tokens * a.pairs * 2;
+    const incvit_status st = launched(launch_rope(a, static_cast<hipStream_t>(stream)), "rope_table_grids");
+    if (st != INCVIT_OK) return st;
+  }
+  return INCVIT_OK;
+}
+
+incvit_status incvit_qk_norm_rope(const incvit_qk* c, int64_t rows, const incvit_heads* q, const incvit_heads* k,
+                                  const float* table, int64_t table_rows, const int32_t* index, const int32_t* k_rows,
+                                  int64_t k_out_rows, void* stream) {
+  if (!c) return op_fail(INCVIT_ERR_ARG, "null configuration");
+  if (!is_dtype(c->dtype)) return op_fail(INCVIT_ERR_UNSUPPORTED, "dtype must be INCVIT_F32 or INCVIT_BF16");
+  if (c->head_dim < 2 || c->head_dim > 2 * kMaxPairs || c->head_dim % 2)
+    return op_fail(INCVIT_ERR_UNSUPPORTED, "head_dim must be even and in [2, 256]");
+  if (c->rot_dim < 0 || c->rot_dim > c->head_dim || c->rot_dim % 2)
+    return op_fail(INCVIT_ERR_SHAPE, "rot_dim must be even and in [0, head_dim]");
+  if (c->pairing != INCVIT_PAIR_HALVES && c->pairing != INCVIT_PAIR_ADJACENT)
+    return op_fail(INCVIT_ERR_ARG, "pairing must be INCVIT_PAIR_HALVES or INCVIT_PAIR_ADJACENT");
+  if (c->norm != INCVIT_NORM_NONE && c->norm != INCVIT_NORM_RMS && c->norm != INCVIT_NORM_LAYER)
+    return op_fail(INCVIT_ERR_ARG, "norm must be INCVIT_NORM_NONE, _RMS or _LAYER");
+  if (!(c->eps >= 0.0f) || !std::isfinite(c->eps)) return op_fail(INCVIT_ERR_ARG, "eps must be >= 0 and finite");
+  if (rows < 0) return op_fail(INCVIT_ERR_ARG, "rows must be >= 0");
+  if (rows == 0) return INCVIT_OK;
+  if (c->rot_dim > 0) {
+    if (!table || (uintptr_t)table % 8) return op_fail(INCVIT_ERR_ARG, "the table must be non-null and 8-byte aligned");
+    if (table_rows < 1 || table_rows > INT32_MAX) return op_fail(INCVIT_ERR_ARG, "table_rows must be in [1, 2^31)");
+  }
+  if (((uintptr_t)index | (uintptr_t)k_rows) % 4) return op_fail(INCVIT_ERR_ARG, "index and k_rows must be 4-byte aligned");
+  if (k_rows && (k_out_rows < 1 || k_out_rows > INT32_MAX)) return op_fail(INCVIT_ERR_ARG, "k_out_rows must be in [1, 2^31)");
+  QkArgs a = {};
+  incvit_status st = check_heads(*c, rows, rows, q, a.q);
+  if (st != INCVIT_OK) return st;
+  if ((st = check_heads(*c, rows, k_rows ? k_out_rows : rows, k, a.k)) != INCVIT_OK) return st;
+  if (k_rows && a.k.heads && a.k.in == a.k.out) return op_fail(INCVIT_ERR_SHAPE, "k_rows cannot move keys in place");
+  const int64_t heads = (int64_t)a.q.heads + a.k.heads;
+  if (heads == 0) return INCVIT_OK;
+  if (rows > INT32_MAX / heads) return op_fail(INCVIT_ERR_ARG, "rows * heads must be < 2^31");
+  a.dtype = c->dtype;
+  a.head_dim = c->head_dim;
+  a.rot_pairs = c->rot_dim / 2;
+  a.adjacent = c->pairing;
+  a.norm = c->norm;
+  a.eps = c->eps;
+  a.rows = (long)rows;
+  a.table = table;
+  a.table_rows = (long)table_rows;
+  a.index = index;
+  a.k_rows = k_rows;
+  a.k_out_rows = (long)k_out_rows;
+  return launched(launch_qk(a, static_cast<hipStream_t>(stream)), "qk_norm_rope");
+}
+
+}  // extern "C"

@@ -27,6 +27,10 @@ SCORES = {"embed": INCVIT_SCORE_EMBED, "key": INCVIT_SCORE_KEY}
 KERNEL_KINDS = ("embed", "sim", "select", "commit", "qkv", "attn", "oproj", "fc1", "fc2", "res_ln1",
                 "key_ln", "key_proj", "hsum")
 MLPS = {"reuse": 0, "all": 1}
+LADDERS = {"axis": 0, "head": 1}
+LAYOUTS = {"blocks": 0, "cycle": 1}
+NORMS = {None: 0, "rms": 1, "layer": 2}
+PAIRINGS = {"halves": 0, "adjacent": 1}
 
 # Exported symbols, as declared in include/incvit.h.
 EXPORTS = ("incvit_canonical_weights_bytes", "incvit_packed_weights_bytes", "incvit_pack_weights",
@@ -35,7 +39,8 @@ EXPORTS = ("incvit_canonical_weights_bytes", "incvit_packed_weights_bytes", "inc
            "incvit_cache_import", "incvit_cache_status", "incvit_last_error", "incvit_profile_enable",
            "incvit_profile_read", "incvit_step_graph_create", "incvit_full_graph_create",
            "incvit_graph_launch", "incvit_graph_destroy", "incvit_set_tuning", "incvit_encode_frame",
-           "incvit_flow_two_anchor", "incvit_step_noalloc")
+           "incvit_flow_two_anchor", "incvit_step_noalloc", "incvit_rope_table", "incvit_rope_table_grids",
+           "incvit_qk_norm_rope")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 
 
@@ -50,6 +55,27 @@ class incvit_config(ctypes.Structure):
 class incvit_tuning(ctypes.Structure):
     _fields_ = [("cols", ctypes.c_int32 * 4), ("attn_qtiles", ctypes.c_int32), ("row_groups", ctypes.c_int32),
                 ("attn_waves", ctypes.c_int32), ("fc2_mode", ctypes.c_int32), ("tiled", ctypes.c_int32)]
+
+
+class incvit_rope(ctypes.Structure):
+    _fields_ = [("axes", ctypes.c_int32), ("pairs", ctypes.c_int32 * 3), ("ladder", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("theta", ctypes.c_double), ("scale", ctypes.c_double * 3)]
+
+
+class incvit_grid(ctypes.Structure):
+    _fields_ = [("t", ctypes.c_int32), ("h", ctypes.c_int32), ("w", ctypes.c_int32), ("t0", ctypes.c_int32),
+                ("y0", ctypes.c_int32), ("x0", ctypes.c_int32)]
+
+
+class incvit_qk(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("pairing", ctypes.c_int32), ("norm", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class incvit_heads(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("gamma", ctypes.c_void_p),
+                ("beta", ctypes.c_void_p), ("in_row", ctypes.c_int64), ("in_head", ctypes.c_int64),
+                ("out_row", ctypes.c_int64), ("out_head", ctypes.c_int64), ("heads", ctypes.c_int32)]
 
 
 class IncvitError(RuntimeError):
@@ -69,6 +95,7 @@ def lib() -> ctypes.CDLL:
             raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2607_12287_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
         P, C, S, I32, F32 = ctypes.c_void_p, ctypes.POINTER(incvit_config), ctypes.c_size_t, ctypes.c_int32, ctypes.c_float
+        I64 = ctypes.c_int64
         sig = {
             "incvit_canonical_weights_bytes": (S, [C]),
             "incvit_packed_weights_bytes": (S, [C]),
@@ -94,6 +121,9 @@ def lib() -> ctypes.CDLL:
             "incvit_encode_frame": (I32, [P, I32, P, P, ctypes.c_int64, I32, F32, P, P, P, P, P, P]),
             "incvit_flow_two_anchor": (I32, [I32, ctypes.c_int64, P, P, P, P, P, P, P, P]),
             "incvit_step_noalloc": (I32, [P, I32, P, P, F32, P, P, P, P, P]),
+            "incvit_rope_table": (I32, [P, I64, P, I64, I64, P, P]),
+            "incvit_rope_table_grids": (I32, [P, I32, P, I32, P, P]),
+            "incvit_qk_norm_rope": (I32, [P, I64, P, P, P, I64, P, P, I64, P]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -195,6 +225,133 @@ def flow_two_anchor(x0, v0, v7, alpha, beta, b, out=None):
                                   beta.data_ptr(), b.data_ptr(), out.data_ptr(),
                                   torch.cuda.current_stream(x0.device).cuda_stream))
     return out
+
+
+def incvit_rope_table(rope: incvit_rope, tokens: int, pos: int, axis_stride: int, token_stride: int, table: int,
+                      stream: int = 0) -> int:
+    return lib().incvit_rope_table(ctypes.addressof(rope), tokens, pos, axis_stride, token_stride, table, stream)
+
+
+def incvit_rope_table_grids(rope: incvit_rope, grids, merge: int, table: int, stream: int = 0) -> int:
+    """grids: a ctypes array of incvit_grid, or a sequence of (t, h, w[, t0[, y0[, x0]]])."""
+    if not isinstance(grids, ctypes.Array):
+        grids = (incvit_grid * len(grids))(*[tuple(g) for g in grids])
+    return lib().incvit_rope_table_grids(ctypes.addressof(rope), len(grids), grids, merge, table, stream)
+
+
+def incvit_qk_norm_rope(c: incvit_qk, rows: int, q: Optional[incvit_heads], k: Optional[incvit_heads], table: int,
+                        table_rows: int, index: int, k_rows: int, k_out_rows: int, stream: int = 0) -> int:
+    return lib().incvit_qk_norm_rope(ctypes.addressof(c), rows, ctypes.addressof(q) if q is not None else None,
+                                     ctypes.addressof(k) if k is not None else None, table, table_rows, index, k_rows,
+                                     k_out_rows, stream)
+
+
+def make_rope(head_dim: int, pairs: Sequence[int], theta: float = 10000.0, ladder: str = "axis", layout: str = "blocks",
+              scale: Optional[Sequence[float]] = None) -> incvit_rope:
+    """Rotary positions with len(pairs) axes (time, height, width; height, width;
+    or one): pairs[a] pairs of a head's dims turn with axis a.  2 * sum(pairs) <=
+    head_dim dims are rotated."""
+    n = len(pairs)
+    if not 1 <= n <= 3 or 2 * sum(pairs) > head_dim or (scale is not None and len(scale) != n):
+        raise ValueError("pairs names one to three axes with at most head_dim / 2 pairs together, scale a factor for each")
+    return incvit_rope(n, (ctypes.c_int32 * 3)(*pairs), LADDERS[ladder], LAYOUTS[layout], float(theta),
+                       (ctypes.c_double * 3)(*(scale or (1.0,) * n)))
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _on(t, f, *args):
+    """f(*args, stream) with t's device current and on its current stream."""
+    import torch
+    if t.device.index == torch.cuda.current_device():
+        return f(*args, torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(t.device):
+        return f(*args, torch.cuda.current_stream().cuda_stream)
+
+
+def rope_table(rope: incvit_rope, positions=None, grids=None, merge: int = 1, out=None, device=None):
+    """[tokens][pairs][2] fp32 cosines and sines.  positions: device int32
+    [axes][tokens], any strides; or grids: (t, h, w[, t0[, y0[, x0]]]) on the host, whose tokens
+    follow one another (frame by frame, in merge x merge windows)."""
+    import torch
+    _need((positions is None) != (grids is None), "either positions or grids")
+    n = sum(rope.pairs[a] for a in range(rope.axes))
+    if positions is not None:
+        _need(positions.is_cuda and positions.dtype == torch.int32 and positions.dim() == 2 and
+              positions.shape[0] == rope.axes, "positions: device int32 [axes][tokens]")
+        tokens, device = positions.shape[1], positions.device
+    else:
+        arr = (incvit_grid * len(grids))(*grids)
+        tokens = sum(g.t * g.h * g.w for g in arr)
+        device = out.device if out is not None else device or torch.device("cuda", torch.cuda.current_device())
+    if out is None:
+        out = torch.empty((max(tokens, 0), n, 2), dtype=torch.float32, device=device)
+    _need(out.is_cuda and out.device == torch.device(device) and out.dtype == torch.float32 and out.is_contiguous() and
+          out.numel() == tokens * n * 2, "out: device fp32 [tokens][pairs][2]")
+    if positions is not None:
+        _check(_on(out, incvit_rope_table, rope, tokens, positions.data_ptr(), positions.stride(0),
+                   positions.stride(1), out.data_ptr()))
+    else:
+        _check(_on(out, incvit_rope_table_grids, rope, arr, merge, out.data_ptr()))
+    return out
+
+
+def _heads(x, out, gamma, beta, head_dim: int, who: str) -> incvit_heads:
+    for t, n in ((gamma, "gamma"), (beta, "beta")):
+        _need(t is None or (t.device == x.device and t.dtype == x.dtype and t.is_contiguous() and t.numel() == head_dim),
+              f"{who}_{n}: [head_dim] of the rows' type and device")
+    _need(out.dtype == x.dtype and out.device == x.device and out.dim() == 3 and out.shape[1:] == x.shape[1:],
+          f"{who}_out: rows of the same heads, type and device")
+    s, o = x.stride(), out.stride()
+    _need(s[2] == 1 and o[2] == 1, f"{who}: the values of a head lie one after another")
+    return incvit_heads(x.data_ptr(), out.data_ptr(), gamma.data_ptr() if gamma is not None else None,
+                        beta.data_ptr() if beta is not None else None, s[0], s[1], o[0], o[1], x.shape[1])
+
+
+def qk_norm_rope(q=None, k=None, table=None, pairing: str = "halves", norm: Optional[str] = "rms", q_gamma=None, k_gamma=None,
+                 q_beta=None, k_beta=None, eps: float = 1e-6, index=None, k_rows=None, q_out=None, k_out=None):
+    """Norm of every head of q [rows][q heads][d] and k [rows][k heads][d] (views
+    with any row and head strides; either may be None), then the rotation by the
+    table rows `index` (device int32 [rows]; without it row r % table rows) of
+    `table` (rope_table's; None: no rotation).  k_rows (device int32 [rows]): the
+    rows of k_out (a cache [..][k heads][d], then required) that the new keys go
+    to.  q_out, k_out may be q and k (in place).  Returns (q_out, k_out)."""
+    import torch
+    x = q if q is not None else k
+    _need(x is not None, "q or k")
+    rows, d = x.shape[0], x.shape[-1]
+    _need(x.is_cuda and x.dtype in (torch.float32, torch.bfloat16), "rows: device tensors, fp32 or bf16")
+    for t in (q, k):
+        _need(t is None or (t.dim() == 3 and t.shape[0] == rows and t.shape[2] == d and t.dtype == x.dtype and
+                            t.device == x.device), "q and k: [rows][heads][d] of one type on one device")
+    rot = 0
+    if table is not None:
+        _need(table.device == x.device and table.dtype == torch.float32 and table.is_contiguous() and table.dim() == 3 and
+              table.shape[2] == 2, "table: device fp32 [rows][pairs][2]")
+        rot = 2 * table.shape[1]
+    for t, n in ((index, "index"), (k_rows, "k_rows")):
+        _need(t is None or (t.device == x.device and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == rows),
+              f"{n}: device int32 [rows]")
+    _need(k_rows is None or (k is not None and k_out is not None), "k_rows: rows of k_out, which has to be given")
+    hq = hk = None
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        _need(q_out.shape[0] == rows, "q_out: as many rows as q")
+        hq = _heads(q, q_out, q_gamma if norm else None, q_beta, d, "q")
+    if k is not None:
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        _need(k_rows is not None or k_out.shape[0] == rows, "k_out: as many rows as k")
+        hk = _heads(k, k_out, k_gamma if norm else None, k_beta, d, "k")
+    c = incvit_qk(INCVIT_BF16 if x.dtype == torch.bfloat16 else INCVIT_F32, d, rot, PAIRINGS[pairing], NORMS[norm], eps)
+    _check(_on(x, incvit_qk_norm_rope, c, rows, hq, hk, table.data_ptr() if rot else None, table.shape[0] if rot else 0,
+               index.data_ptr() if index is not None else None, k_rows.data_ptr() if k_rows is not None else None,
+               k_out.shape[0] if k_rows is not None else 0))
+    return q_out, k_out
 
 
 def incvit_cache_export(h, cache: int, dst: int, stream: int = 0) -> int:
