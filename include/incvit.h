@@ -368,6 +368,72 @@ incvit_status incvit_qk_norm_rope(const incvit_qk* c, int64_t rows, const incvit
                                   const int32_t* index, const int32_t* k_rows, int64_t k_out_rows,
                                   void* stream);
 
+/* --------------------------------------------------------- 8-bit products -- */
+
+/* y = act(x W + b) + residual in 8-bit integers with a scale for each token (row
+ * of x) and each channel (column of W):
+ *   s_m = max_k |x_mk| / 127 rounded to fp32, q_mk = x_mk / s_m rounded to fp32
+ *   and then to the nearest integer (ties to even), likewise s_n and w_kn over
+ *   the K values of column n;
+ *   y_mn = act((sum_k q_mk w_kn) * (s_m * s_n) + b_n) + residual_mn, the sum
+ *   exact in int32, the rest in fp32 with one rounding at the end; act is the
+ *   identity or the tanh GELU.
+ * A row or column of zeros has scale 0 (and integers 0), one that holds an
+ * infinity or a NaN has scale NaN and makes its outputs NaN.
+ * 1 <= K <= 65536, 1 <= N <= 2^20, and K * N below 2^32 bytes as packed;
+ * otherwise INCVIT_ERR_UNSUPPORTED. */
+
+/* Bytes of the packed weights (operand order, scales, biases); 0 if K or N is
+ * out of range. */
+size_t incvit_qlinear_weights_bytes(int32_t K, int32_t N);
+
+/* Types of the weights given to incvit_qlinear_pack_weights: incvit_dtype, or
+ * integers that are quantised already. */
+#define INCVIT_I8 2
+
+/* Quantise and pack W: value (k, n) is w[k * k_stride + n * n_stride] (elements,
+ * in [0, 2^40]; so [K][N] and [N][K] storage alike), of `dtype`.  INCVIT_I8: w
+ * holds the integers and scales (device fp32 [N]) is required; otherwise scales
+ * must be NULL.  bias: [N] of `dtype` (fp32 with INCVIT_I8), or NULL.  weights:
+ * incvit_qlinear_weights_bytes(K, N) bytes, 256-byte aligned.  Errors:
+ * INCVIT_ERR_ARG or INCVIT_ERR_UNSUPPORTED (text: incvit_last_error(NULL)).
+ * Asynchronous on `stream`. */
+incvit_status incvit_qlinear_pack_weights(int32_t dtype, int32_t K, int32_t N, const void* w,
+                                          int64_t k_stride, int64_t n_stride, const float* scales,
+                                          const void* bias, void* weights, void* stream);
+
+/* Bytes of `rows` quantised rows of K values (operand order, scales); 0 if out
+ * of range. */
+size_t incvit_qlinear_rows_bytes(int64_t rows, int32_t K);
+
+/* Quantise rows: row m is x[m * x_stride .. + K), of `dtype`.  gamma, beta: a
+ * LayerNorm over the K values before it (fp32 statistics in two passes, biased
+ * variance, eps >= 0; gamma NULL: none; beta NULL: zeros), [K] of `dtype`.
+ * qrows: incvit_qlinear_rows_bytes(rows, K) bytes, 256-byte aligned; it serves
+ * any number of products with the same K.  rows >= 0 (none: nothing is
+ * enqueued), rows < 2^31.  Errors and asynchrony as above. */
+incvit_status incvit_qlinear_quantize_rows(int32_t dtype, int64_t rows, int32_t K, const void* x,
+                                           int64_t x_stride, const void* gamma, const void* beta,
+                                           float eps, void* qrows, void* stream);
+
+/* The product of quantised rows with packed weights.  out: rows of N values of
+ * `dtype`, out_stride >= N elements apart; residual: likewise, added after act,
+ * or NULL; it may be `out` with the same stride.  gelu: 0 or 1.  Any strides and
+ * alignment of whole elements; multiples of four (and 16-byte aligned rows)
+ * take the fast path. */
+incvit_status incvit_qlinear_multiply(int32_t dtype, int64_t rows, int32_t K, int32_t N,
+                                      const void* qrows, const void* weights, int32_t gelu,
+                                      const void* residual, int64_t res_stride, void* out,
+                                      int64_t out_stride, void* stream);
+
+/* Both in one call: rows of `dtype` quantised into workspace
+ * (incvit_qlinear_rows_bytes(rows, K) bytes, 256-byte aligned, the call's own
+ * until it has run on `stream`), then multiplied. */
+incvit_status incvit_qlinear(int32_t dtype, int64_t rows, int32_t K, int32_t N, const void* x,
+                             int64_t x_stride, const void* weights, int32_t gelu,
+                             const void* residual, int64_t res_stride, void* out,
+                             int64_t out_stride, void* workspace, void* stream);
+
 /* ------------------------------------------------------------ HIP graphs -- */
 
 typedef struct incvit_graph incvit_graph;

@@ -166,7 +166,8 @@ struct RowsArgs {  // commit: ref/X0/Z0 of the refreshed rows, row map
   int* zpos;
 };
 
-enum Epi { EPI_QKV = 0, EPI_FC1 = 1, EPI_PART = 2, EPI_RES = 3, EPI_ATT = 4, EPI_DOWN = 5 };
+enum Epi { EPI_QKV = 0, EPI_FC1 = 1, EPI_PART = 2, EPI_RES = 3, EPI_ATT = 4, EPI_DOWN = 5,
+           EPI_QBF = 6, EPI_QF32 = 7 };  // 8-bit products, bf16 or fp32 output
 
 // Fields in the order the kernel's prologue needs them, so that its argument
 // loads go out together.
@@ -189,6 +190,14 @@ struct GemmArgs {
   int layer;
   Shape sh;
   CacheLayout cl;
+  // 8-bit products: A and W in 64-deep chunks; out, resid row-major
+  const float* row_scale;  // [mpad]
+  const float* col_scale;  // [Nout] (and bias, both padded to whole column blocks)
+  long res_ld, out_ld;     // strides of resid (null: none) and out
+  int m_host;              // rows, where meta is null
+  int n;                   // output columns (Nout: rounded up to 16)
+  int gelu;
+  int wide;                // out and resid take 4 columns at once (strides, addresses and n)
 };
 
 // Row kernel that finishes the split-K MLP down projection, one workgroup per
@@ -376,6 +385,7 @@ namespace incvit {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(4))) int i32x4_t;
 
 // Pointers read from memory (the row map) are generic to the compiler, which
 // then emits flat accesses; flat accesses count against both the vector-memory

@@ -88,6 +88,10 @@ __host__ __device__ constexpr bool ln_on_load() {
   return EPI == EPI_QKV || EPI == EPI_FC1;
 }
 template <int EPI>
+__host__ __device__ constexpr bool is_q8() {
+  return EPI == EPI_QBF || EPI == EPI_QF32;
+}
+template <int EPI>
 __host__ __device__ constexpr int gemm_waves() {
   return kGemmWaves;
 }
@@ -147,6 +151,50 @@ __device__ __forceinline__ void epilogue_store(const GemmArgs& a, int row, int c
     const float f = fmaf(rstd, x, fmaf(nmr, c1, bias));
     static_cast<T*>(a.out)[frag_off(row, col, a.ldo / 32)] = Elem<T>::cv(gelu_tanh(Elem<T>::rnd(f)));
   }
+}
+
+// 8-bit products: acc(16x16) += A(16x64) * B(64x16), lane l holding 16 values of
+// row (column) l % 16, exact in int32.
+__device__ __forceinline__ void mma_q8(i32x4_t& acc, u32x4_t a, u32x4_t b) {
+  acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), acc, 0, 0, 0);
+}
+
+// Columns col .. col + 3 (col % 4 == 0) of a row of an 8-bit product, row < M:
+// sum * (row scale * column scale) + bias, GELU, residual, all in fp32 with one
+// rounding at the end.  The last column block may end inside the four.
+template <class T>
+__device__ __forceinline__ void q8_store(const GemmArgs& a, int row, int col, const i32x4_t& acc, float rs, const float4& cs,
+                                         const float4& cb) {
+  const float sc[4] = {cs.x, cs.y, cs.z, cs.w}, bi[4] = {cb.x, cb.y, cb.z, cb.w};
+  float y[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    y[j] = fmaf((float)acc[j], rs * sc[j], bi[j]);
+    if (a.gelu) y[j] = gelu_tanh(y[j]);  // uniform
+  }
+  T* out = static_cast<T*>(a.out) + (size_t)row * a.out_ld + col;
+  const T* res = a.resid ? static_cast<const T*>(a.resid) + (size_t)row * a.res_ld + col : nullptr;
+  if (a.wide) {  // uniform: four columns at once, all or none of them below n
+    if (col >= a.n) return;
+    if constexpr (std::is_same<T, float>::value) {
+      if (res) {
+        const float4 v = *reinterpret_cast<const float4*>(res);
+        y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
+      }
+      *reinterpret_cast<float4*>(out) = make_float4(y[0], y[1], y[2], y[3]);
+    } else {
+      if (res) {
+        const uint2 v = *reinterpret_cast<const uint2*>(res);
+        y[0] += __uint_as_float(v.x << 16); y[1] += __uint_as_float(v.x & 0xffff0000u);
+        y[2] += __uint_as_float(v.y << 16); y[3] += __uint_as_float(v.y & 0xffff0000u);
+      }
+      *reinterpret_cast<uint2*>(out) = make_uint2(f2bf2(y[0], y[1]), f2bf2(y[2], y[3]));
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (col + j < a.n) out[j] = Elem<T>::cv(res ? y[j] + Elem<T>::f(res[j]) : y[j]);
 }
 
 template <class T, int EPI, int NB, int CPW>

@@ -43,6 +43,10 @@
 // reads alone at 240 B/clk; their sum is what bounds a 128 x 128 tile (no
 // products: 72 of its 75 us).
 //
+// The same loop multiplies 8-bit integers (EPI_QBF, EPI_QF32; v_mfma_i32_16x16x64_i8,
+// exact int32 sums): a fragment is 16 rows or columns by 64 values, again a
+// kilobyte, and the epilogue applies the rows' and columns' scales.
+//
 // bf16 models only (fp32 models use the small-M kernel).  Results do not
 // depend on the tile shape beyond the fp32 order of the MFMA accumulation,
 // which is fixed (k ascending); no atomics.
@@ -114,6 +118,8 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
   constexpr int LPW = LA + LW;
   constexpr int TR = TRB / WR, TC = CBB / WC;          // per wave
   constexpr bool LNA = ln_on_load<EPI>();
+  constexpr bool Q8 = is_q8<EPI>();
+  using Acc = std::conditional_t<Q8, i32x4_t, f32x4_t>;
   // A slot is multiplied in S steps of H row tiles x TC column blocks of one
   // chunk.  The fragments of a step are read while the step before it is
   // multiplied, into the other of two register sets (W: per chunk).
@@ -128,8 +134,8 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
   const int g = lane >> 4, n = lane & 15;
   const int wr = w / WC, wc = w % WC;
   const int D = a.sh.D;
-  const int M = a.meta->m;
-  const int nblocks = a.Nout / 16, kchunks = a.kchunks, akc = a.lda / 32;
+  const int M = Q8 && !a.meta ? a.m_host : a.meta->m;
+  const int nblocks = a.Nout / 16, kchunks = a.kchunks, akc = a.lda / (Q8 ? 64 : 32);
   const int mt = (M + BM - 1) / BM, nt = (nblocks + CBB - 1) / CBB;  // tiles that have rows
   const int per_split = mt * nt, total = per_split * a.ksplit;
   const int kper = (kchunks + a.ksplit - 1) / a.ksplit;
@@ -176,7 +182,7 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
     const uint64_t b = reinterpret_cast<uint64_t>(p);
     return u32x4_t{(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, bytes, 0x00020000u};
   };
-  const uint32_t sizeA = (uint32_t)a.mpad * a.lda * 2, sizeW = (uint32_t)nblocks * kchunks * 1024;
+  const uint32_t sizeA = (uint32_t)a.mpad * a.lda * (Q8 ? 1 : 2), sizeW = (uint32_t)nblocks * kchunks * 1024;
   u32x4_t rA = rsrc_of(a.A, sizeA), rW = rsrc_of(a.W, sizeW);
   const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   const int atiles = a.mpad / 16;
@@ -277,11 +283,11 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
   for (int idx = blockIdx.x; idx < total; idx += stride) {
     const Tile t = tile_of(idx);
     if (idx != (int)blockIdx.x) set_next(idx);
-    f32x4_t acc[TR][TC];
+    Acc acc[TR][TC];
 #pragma unroll
     for (int r = 0; r < TR; ++r)
 #pragma unroll
-      for (int b = 0; b < TC; ++b) acc[r][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int b = 0; b < TC; ++b) acc[r][b] = Acc{0, 0, 0, 0};
     f32x4_t accs[HS * SHA], accq[HS * SHA];  // row sums and sums of squares (LNA)
 #pragma unroll
     for (int i = 0; i < HS * SHA; ++i) accs[i] = accq[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -315,7 +321,8 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
             for (int b = 0; b < TC; ++b) {
               V8<T> y;
               y.v = __builtin_bit_cast(uint4, wf[cw][b]);
-              mma(acc[half * H + i][b], y, x);
+              if constexpr (Q8) mma_q8(acc[half * H + i][b], wf[cw][b], af[ca][i]);
+              else mma(acc[half * H + i][b], y, x);
             }
           }
 #pragma unroll
@@ -392,6 +399,33 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
       }
     }
 
+    if constexpr (Q8) {
+      // lane (g, n) holds columns 4g..4g+3 of row n of each 16x16 tile; the
+      // scales of its rows are loaded once, a column block's operands while the
+      // block before it is finished (below)
+      float rs[TR];
+#pragma unroll
+      for (int r = 0; r < TR; ++r) rs[r] = a.row_scale[min(t.m0 + (wr * TR + r) * 16 + n, M - 1)];
+      float4 cs[2], cb[2];
+      auto load_cols = [&](int b) {
+        const int col = min(t.cb0 + wc * TC + b, nblocks - 1) * 16 + 4 * g;
+        cs[b & 1] = *reinterpret_cast<const float4*>(a.col_scale + col);
+        cb[b & 1] = *reinterpret_cast<const float4*>(a.bias + col);
+      };
+      load_cols(0);
+#pragma unroll
+      for (int b = 0; b < TC; ++b) {
+        if (b + 1 < TC) load_cols(b + 1);
+        const int cblk = t.cb0 + wc * TC + b;
+#pragma unroll
+        for (int r = 0; r < TR; ++r) {
+          const int row = t.m0 + (wr * TR + r) * 16 + n;
+          if (row < M && cblk < nblocks)
+            q8_store<std::conditional_t<EPI == EPI_QBF, uint16_t, float>>(a, row, cblk * 16 + 4 * g, acc[r][b], rs[r], cs[b & 1],
+                                                                          cb[b & 1]);
+        }
+      }
+    } else {
     // ---- epilogue: lane (g, n) holds columns 4g..4g+3 of row n of each 16x16
     // tile.  Operations and rounding points are the small-M kernel's
     // (epilogue_store).  The rows' map entries are loaded once, and a column
@@ -496,6 +530,7 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
         }
       }
     }
+    }
   }
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // no load into this workgroup's LDS outlives it
 }
@@ -551,7 +586,7 @@ hipError_t launch_tiled_cfg(const GemmArgs& a, int rows, hipStream_t s) {
 //     rows within the 448x448 encode 20.1 -> 17.6; else two per CU.
 template <int EPI>
 hipError_t launch_tiled_epi(const GemmArgs& a, int expected, int rows, hipStream_t s) {
-  if (!a.sh.dtype || a.ksplit < 1 || a.sh.dh % 8) return hipErrorInvalidValue;
+  if (a.ksplit < 1 || (!is_q8<EPI>() && (!a.sh.dtype || a.sh.dh % 8))) return hipErrorInvalidValue;
   if (a.ksplit > 1) {
     const int kper = (a.kchunks + a.ksplit - 1) / a.ksplit;
     if (EPI != EPI_PART || kper * (a.ksplit - 1) >= a.kchunks) return hipErrorInvalidValue;
@@ -561,7 +596,7 @@ hipError_t launch_tiled_epi(const GemmArgs& a, int expected, int rows, hipStream
   if (tiles(64, 128) <= 256) return launch_tiled_cfg<EPI, 64, 128, 2, 2, 6>(a, rows, s);
   // at least `quarters` quarters of the places in all rounds of t tiles
   auto full = [](int t, int quarters) { return 4 * t >= quarters * 256 * ((t + 255) / 256); };
-  if constexpr (EPI == EPI_QKV || EPI == EPI_FC1) {
+  if constexpr (EPI == EPI_QKV || EPI == EPI_FC1 || is_q8<EPI>()) {
     const int x = tiles(256, 256);
     if (x >= 256 && full(x, 4)) return launch_tiled_cfg<EPI, 256, 256, 2, 1, 4>(a, rows, s);
   }

@@ -44,6 +44,97 @@ incvit_status check_heads(const incvit_qk& c, int64_t rows, int64_t out_rows, co
   return INCVIT_OK;
 }
 
+bool q_sizes(int32_t K, int32_t N) {
+  return K >= 1 && K <= 65536 && N >= 1 && N <= (1 << 20) &&
+         (uint64_t)((N + 15) / 16) * ((K + 63) / 64) * 1024 < ((uint64_t)1 << 32);
+}
+
+incvit_status check_q(int64_t rows, int32_t K, int32_t N) {
+  if (!q_sizes(K, N)) return op_fail(INCVIT_ERR_UNSUPPORTED, "K must be in [1, 65536], N in [1, 2^20] and the packed weights below 4 GiB");
+  if (rows < 0 || rows > INT32_MAX - 64) return op_fail(INCVIT_ERR_ARG, "rows must be in [0, 2^31 - 64)");
+  return INCVIT_OK;
+}
+
+incvit_status check_x(int32_t dtype, const void* x, int64_t x_stride, const void* qrows) {
+  if (!is_dtype(dtype)) return op_fail(INCVIT_ERR_UNSUPPORTED, "dtype must be INCVIT_F32 or INCVIT_BF16");
+  if (!x || !qrows) return op_fail(INCVIT_ERR_ARG, "null rows");
+  if ((uintptr_t)x % (dtype == INCVIT_BF16 ? 2 : 4)) return op_fail(INCVIT_ERR_ARG, "rows must be aligned to their elements");
+  if ((uintptr_t)qrows % 256) return op_fail(INCVIT_ERR_ARG, "quantised rows must be 256-byte aligned");
+  if (x_stride < 0 || x_stride > ((int64_t)1 << 40)) return op_fail(INCVIT_ERR_ARG, "x_stride must be in [0, 2^40] elements");
+  return INCVIT_OK;
+}
+
+incvit_status check_out(int32_t dtype, int64_t rows, int32_t N, const void* weights, int32_t gelu, const void* residual,
+                        int64_t res_stride, const void* out, int64_t out_stride) {
+  if (!is_dtype(dtype)) return op_fail(INCVIT_ERR_UNSUPPORTED, "dtype must be INCVIT_F32 or INCVIT_BF16");
+  if (!weights || !out) return op_fail(INCVIT_ERR_ARG, "null weights or output");
+  if ((uintptr_t)weights % 256) return op_fail(INCVIT_ERR_ARG, "weights must be 256-byte aligned");
+  if (((uintptr_t)out | (uintptr_t)residual) % (dtype == INCVIT_BF16 ? 2 : 4))
+    return op_fail(INCVIT_ERR_ARG, "out and residual must be aligned to their elements");
+  if (gelu != 0 && gelu != 1) return op_fail(INCVIT_ERR_ARG, "gelu must be 0 or 1");
+  const int64_t most = (int64_t)1 << 40;
+  if ((rows > 1 && out_stride < N) || out_stride < 0 || out_stride > most) return op_fail(INCVIT_ERR_SHAPE, "out_stride must be in [N, 2^40]");
+  if (residual && (res_stride < 0 || res_stride > most)) return op_fail(INCVIT_ERR_ARG, "res_stride must be in [0, 2^40]");
+  if (residual == out && residual && rows > 1 && res_stride != out_stride)
+    return op_fail(INCVIT_ERR_SHAPE, "a residual in place must have the output's stride");
+  return INCVIT_OK;
+}
+
+// Rows per launch: the large-row GEMM addresses its rows' integers with 32 bits.
+int64_t q_slab(int32_t K) { return (((int64_t)1 << 31) / ((K + 63) / 64 * 64)) / 256 * 256; }
+
+incvit_status q_rows(int32_t dtype, int64_t rows, int32_t K, const void* x, int64_t x_stride, const void* gamma, const void* beta,
+                     float eps, void* qrows, hipStream_t s) {
+  const QRowsLayout l(rows, K);
+  QRowsArgs a = {};
+  a.x = x;
+  a.ld = (long)x_stride;
+  a.gamma = gamma;
+  a.beta = beta;
+  a.eps = eps;
+  a.dst = static_cast<char*>(qrows);
+  a.scale = reinterpret_cast<float*>(a.dst + l.scale);
+  a.rows = (long)rows;
+  a.K = K;
+  a.dtype = dtype;
+  return launched(launch_q_rows(a, s), "qlinear_quantize_rows");
+}
+
+incvit_status q_multiply(int32_t dtype, int64_t rows, int32_t K, int32_t N, const void* qrows, const void* weights, int32_t gelu,
+                         const void* residual, int64_t res_stride, void* out, int64_t out_stride, hipStream_t s) {
+  const QRowsLayout rl(rows, K);
+  const QWeightsLayout wl(K, N);
+  const size_t eb = dtype == INCVIT_BF16 ? 2 : 4;
+  const char* w = static_cast<const char*>(weights);
+  GemmArgs a = {};
+  a.W = w;
+  a.col_scale = reinterpret_cast<const float*>(w + wl.scale);
+  a.bias = reinterpret_cast<const float*>(w + wl.bias);
+  a.lda = 64 * wl.kc;
+  a.kchunks = wl.kc;
+  a.Nout = 16 * wl.blocks;
+  a.n = N;
+  a.ksplit = 1;
+  a.gelu = gelu;
+  a.out_ld = (long)out_stride;
+  a.res_ld = (long)res_stride;
+  const uintptr_t bits = (uintptr_t)out | (uintptr_t)residual | (uintptr_t)(out_stride * eb) | (uintptr_t)(residual ? res_stride * eb : 0);
+  a.wide = N % 4 == 0 && bits % (4 * eb) == 0;
+  const int64_t slab = q_slab(K);
+  for (int64_t r = 0; r < rows; r += slab) {
+    const int m = (int)(rows - r < slab ? rows - r : slab);
+    a.A = static_cast<const char*>(qrows) + (size_t)(r / 16) * wl.kc * 1024;
+    a.row_scale = reinterpret_cast<const float*>(static_cast<const char*>(qrows) + rl.scale) + r;
+    a.out = static_cast<char*>(out) + (size_t)r * out_stride * eb;
+    a.resid = residual ? static_cast<const char*>(residual) + (size_t)r * res_stride * eb : nullptr;
+    a.m_host = m;
+    a.mpad = (m + 15) / 16 * 16;
+    const incvit_status st = launched(launch_q_gemm(a, dtype == INCVIT_F32, m, m, s), "qlinear_multiply");
+    if (st != INCVIT_OK) return st;
+  }
+  return INCVIT_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -148,6 +239,68 @@ incvit_status incvit_qk_norm_rope(const incvit_qk* c, int64_t rows, const incvit
   a.k_rows = k_rows;
   a.k_out_rows = (long)k_out_rows;
   return launched(launch_qk(a, static_cast<hipStream_t>(stream)), "qk_norm_rope");
+}
+
+size_t incvit_qlinear_weights_bytes(int32_t K, int32_t N) { return q_sizes(K, N) ? QWeightsLayout(K, N).total : 0; }
+
+size_t incvit_qlinear_rows_bytes(int64_t rows, int32_t K) {
+  if (rows < 0 || rows > INT32_MAX - 64 || K < 1 || K > 65536) return 0;
+  return QRowsLayout((long)rows, K).total;
+}
+
+incvit_status incvit_qlinear_pack_weights(int32_t dtype, int32_t K, int32_t N, const void* w, int64_t k_stride, int64_t n_stride,
+                                          const float* scales, const void* bias, void* weights, void* stream) {
+  const incvit_status st = check_q(0, K, N);
+  if (st != INCVIT_OK) return st;
+  if (!is_dtype(dtype) && dtype != INCVIT_I8) return op_fail(INCVIT_ERR_UNSUPPORTED, "dtype must be INCVIT_F32, INCVIT_BF16 or INCVIT_I8");
+  if (!w || !weights) return op_fail(INCVIT_ERR_ARG, "null weights");
+  if ((uintptr_t)weights % 256) return op_fail(INCVIT_ERR_ARG, "packed weights must be 256-byte aligned");
+  if ((dtype == INCVIT_I8) != (scales != nullptr)) return op_fail(INCVIT_ERR_ARG, "scales belong to INCVIT_I8 weights, and those need them");
+  const uintptr_t eb = dtype == INCVIT_F32 ? 4 : dtype == INCVIT_BF16 ? 2 : 1;
+  if ((uintptr_t)w % eb || (uintptr_t)bias % (dtype == INCVIT_BF16 ? 2 : 4) || (uintptr_t)scales % 4)
+    return op_fail(INCVIT_ERR_ARG, "weights, scales and bias must be aligned to their elements");
+  const int64_t most = (int64_t)1 << 40;
+  if (k_stride < 0 || n_stride < 0 || k_stride > most || n_stride > most)
+    return op_fail(INCVIT_ERR_ARG, "strides must be in [0, 2^40] elements");
+  const QPackArgs a = {w, (long)k_stride, (long)n_stride, scales, bias, static_cast<char*>(weights), K, N, dtype};
+  return launched(launch_q_pack(a, static_cast<hipStream_t>(stream)), "qlinear_pack_weights");
+}
+
+incvit_status incvit_qlinear_quantize_rows(int32_t dtype, int64_t rows, int32_t K, const void* x, int64_t x_stride,
+                                           const void* gamma, const void* beta, float eps, void* qrows, void* stream) {
+  incvit_status st = check_q(rows, K, 1);
+  if (st != INCVIT_OK) return st;
+  if (rows == 0) return INCVIT_OK;
+  if ((st = check_x(dtype, x, x_stride, qrows)) != INCVIT_OK) return st;
+  if (beta && !gamma) return op_fail(INCVIT_ERR_ARG, "beta is given without gamma");
+  if (((uintptr_t)gamma | (uintptr_t)beta) % (dtype == INCVIT_BF16 ? 2 : 4))
+    return op_fail(INCVIT_ERR_ARG, "gamma and beta must be aligned to their elements");
+  if (gamma && (!(eps >= 0.0f) || !std::isfinite(eps))) return op_fail(INCVIT_ERR_ARG, "eps must be >= 0 and finite");
+  return q_rows(dtype, rows, K, x, x_stride, gamma, beta, eps, qrows, static_cast<hipStream_t>(stream));
+}
+
+incvit_status incvit_qlinear_multiply(int32_t dtype, int64_t rows, int32_t K, int32_t N, const void* qrows, const void* weights,
+                                      int32_t gelu, const void* residual, int64_t res_stride, void* out, int64_t out_stride,
+                                      void* stream) {
+  incvit_status st = check_q(rows, K, N);
+  if (st != INCVIT_OK) return st;
+  if (rows == 0) return INCVIT_OK;
+  if (!qrows || (uintptr_t)qrows % 256) return op_fail(INCVIT_ERR_ARG, "quantised rows must be non-null and 256-byte aligned");
+  if ((st = check_out(dtype, rows, N, weights, gelu, residual, res_stride, out, out_stride)) != INCVIT_OK) return st;
+  return q_multiply(dtype, rows, K, N, qrows, weights, gelu, residual, res_stride, out, out_stride, static_cast<hipStream_t>(stream));
+}
+
+incvit_status incvit_qlinear(int32_t dtype, int64_t rows, int32_t K, int32_t N, const void* x, int64_t x_stride,
+                             const void* weights, int32_t gelu, const void* residual, int64_t res_stride, void* out,
+                             int64_t out_stride, void* workspace, void* stream) {
+  incvit_status st = check_q(rows, K, N);
+  if (st != INCVIT_OK) return st;
+  if (rows == 0) return INCVIT_OK;
+  if ((st = check_x(dtype, x, x_stride, workspace)) != INCVIT_OK) return st;
+  if ((st = check_out(dtype, rows, N, weights, gelu, residual, res_stride, out, out_stride)) != INCVIT_OK) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if ((st = q_rows(dtype, rows, K, x, x_stride, nullptr, nullptr, 0.0f, workspace, s)) != INCVIT_OK) return st;
+  return q_multiply(dtype, rows, K, N, workspace, weights, gelu, residual, res_stride, out, out_stride, s);
 }
 
 }  // extern "C"

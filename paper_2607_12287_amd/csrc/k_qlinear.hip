@@ -1,0 +1,315 @@
+// 8-bit products with a scale for each row (token) and each column (channel):
+//   out = act(sum_k q_mk w_kn * (s_m s_n) + b_n) + resid
+// with q = round(x / s), s = max |x| / 127 over a row's K values, and likewise
+// for the columns of W.  Sums of 8-bit products are exact in int32 (K <= 65536).
+//
+// Three kernels:
+//   * q_rows_kernel: a wave per row finds its largest magnitude and writes the
+//     row's integers in the matrix instruction's operand order (with a
+//     LayerNorm before it, whose statistics are two passes over registers);
+//   * q_gemm_kernel, few rows: weights stream past them once.  A workgroup owns
+//     16 columns; its waves take the K chunks in turn, so every wave has loads of
+//     its own in flight, and add their int32 partial tiles through LDS (in any
+//     order: integer sums are exact);
+//   * the large-row GEMM (gemm_tiled.hpp) otherwise.
+#include "gemm_tiled.hpp"
+#include "ops.hpp"
+
+namespace incvit {
+
+namespace {
+
+// ------------------------------------------------------------- quantisation --
+
+// scale of a largest magnitude given as fp32 bits; NaN where it is not finite
+__device__ __forceinline__ float q_scale(uint32_t top) {
+  const float s = __fdiv_rn(__uint_as_float(top), 127.0f);
+  return top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : s;
+}
+// x / s, rounded to fp32, then to the nearest integer (ties to even); 0 for a
+// row of zeros, and for one whose scale is NaN
+__device__ __forceinline__ int q_value(float x, float s) {
+  const float r = rintf(__fdiv_rn(x, s));
+  return s > 0.0f ? (int)fminf(fmaxf(r, -127.0f), 127.0f) : 0;
+}
+__device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+__device__ __forceinline__ uint32_t wave_max_u(uint32_t x) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, off, 64));
+  return x;
+}
+
+// 8 values of a row from k on (fewer where the row ends: zeros)
+template <class T, bool VEC>
+__device__ __forceinline__ void load8(const T* p, int k, int K, float* v) {
+  if constexpr (VEC) {  // K % 8 == 0, 16-byte aligned
+    if (k < K) {
+      if constexpr (std::is_same<T, float>::value) {
+        const float4 a = *reinterpret_cast<const float4*>(p + k), b = *reinterpret_cast<const float4*>(p + k + 4);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      } else {
+        const uint4 u = *reinterpret_cast<const uint4*>(p + k);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[2 * i] = __uint_as_float(w[i] << 16);
+          v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+      }
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = k + i < K ? Elem<T>::f(p[k + i]) : 0.0f;
+  }
+}
+
+// A wave per row, a workgroup per tile of 16 rows: the 16-byte pieces that its
+// waves write fill whole kilobytes, which meet in the L2.  A lane holds 8 values
+// of every 512 in registers (CH of them, K <= 512 CH); longer rows (CH = 0) are
+// read again for each pass.
+template <class T, int CH, bool VEC>
+__global__ __launch_bounds__(1024) void q_rows_kernel(QRowsArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int r = __builtin_amdgcn_readfirstlane(blockIdx.x * 16 + (threadIdx.x >> 6));
+  const long rows = a.meta ? a.meta->m : a.rows;
+  if (r >= rows) return;  // uniform per wave
+  const int K = a.K, kc = (K + 63) / 64, n8 = kc * 8;  // runs of 8, padding included
+  const T* x = static_cast<const T*>(a.x);
+  auto fetch = [&](int i, float* v) {  // the lane's i-th run
+    const int k = 8 * (lane + 64 * i);
+    if (a.frag) {  // uniform: 16-row x 32-column operand order
+      load8<T, true>(x + (k < K ? frag_off(r, k, (int)a.ld / 32) : 0) - k, k, K, v);
+    } else {
+      load8<T, VEC>(x + (size_t)r * a.ld, k, K, v);
+    }
+  };
+  constexpr int NH = CH > 0 ? CH : 1;
+  const int runs = CH > 0 ? CH : (n8 + 63) / 64;
+  float held[NH][8];
+  if constexpr (CH > 0) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) fetch(i, held[i]);
+  }
+  // f(run, its first k, its 8 values) for every run of the lane
+  auto each = [&](auto f) {
+    if constexpr (CH > 0) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) f(8 * (lane + 64 * i), held[i]);
+    } else {
+      for (int i = 0; i < runs; ++i) {
+        fetch(i, held[0]);
+        f(8 * (lane + 64 * i), held[0]);
+      }
+    }
+  };
+  float mean = 0.0f, rstd = 1.0f;
+  const bool ln = a.gamma != nullptr;
+  if (ln) {  // uniform
+    float s = 0.0f, q = 0.0f;
+    each([&](int, float* v) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s += v[j];  // zeros past K
+    });
+    mean = wave_sum(s) / (float)K;
+    each([&](int k, float* v) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float d = v[j] - mean;
+        q += k + j < K ? d * d : 0.0f;
+      }
+    });
+    rstd = 1.0f / sqrtf(wave_sum(q) / (float)K + a.eps);
+  }
+  auto param = [&](const void* p, int k) {
+    return a.param_f32 ? static_cast<const float*>(p)[k] : Elem<T>::f(static_cast<const T*>(p)[k]);
+  };
+  auto normed = [&](int k, float* v) {
+    if (!ln) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      v[j] = k + j < K ? fmaf((v[j] - mean) * rstd, param(a.gamma, k + j), a.beta ? param(a.beta, k + j) : 0.0f) : 0.0f;
+  };
+  uint32_t top = 0;
+  each([&](int k, float* v) {
+    normed(k, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, mag(v[j]));
+  });
+  const float s = q_scale(wave_max_u(top));
+  if (lane == 0) a.scale[r] = s;
+  each([&](int k, float* v) {
+    if constexpr (CH == 0) normed(k, v);
+    if (k >= 64 * kc) return;
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j >> 2] |= (uint32_t)(q_value(v[j], s) & 0xff) << (8 * (j & 3));
+    *reinterpret_cast<uint2*>(a.dst + q_off(r, k, kc)) = make_uint2(w[0], w[1]);
+  });
+}
+
+template <class T, bool VEC>
+hipError_t launch_rows_t(const QRowsArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.rows + 15) / 16)), block(1024);
+  if (a.K <= 1024) return launch_k(q_rows_kernel<T, 2, VEC>, grid, block, 0, s, a);
+  if (a.K <= 2048) return launch_k(q_rows_kernel<T, 4, VEC>, grid, block, 0, s, a);
+  return launch_k(q_rows_kernel<T, 0, VEC>, grid, block, 0, s, a);
+}
+
+// ------------------------------------------------------------------ weights --
+
+template <class T>
+__device__ __forceinline__ float w_value(T x) { return Elem<T>::f(x); }
+template <>
+__device__ __forceinline__ float w_value<int8_t>(int8_t x) { return (float)x; }
+
+// Scales and biases of 64 columns by 4 shares of K; columns past N: zeros.
+template <class T>
+__global__ __launch_bounds__(256) void q_scale_kernel(QPackArgs a) {
+  __shared__ uint32_t s_top[4][64];
+  const QWeightsLayout l(a.K, a.N);
+  const int c = threadIdx.x & 63, part = threadIdx.x >> 6, n = blockIdx.x * 64 + c;
+  const T* w = static_cast<const T*>(a.w);
+  uint32_t top = 0;
+  if (n < a.N && !a.scales)
+    for (int k = part; k < a.K; k += 4) top = max(top, mag(w_value<T>(w[k * a.wk + n * a.wn])));
+  s_top[part][c] = top;
+  __syncthreads();
+  if (part || n >= l.blocks * 16) return;
+  top = max(max(s_top[0][c], s_top[1][c]), max(s_top[2][c], s_top[3][c]));
+  float s = 0.0f, b = 0.0f;
+  if (n < a.N) {
+    s = a.scales ? a.scales[n] : q_scale(top);
+    if (a.bias) b = a.dtype == INCVIT_BF16 ? bf2f(static_cast<const uint16_t*>(a.bias)[n]) : static_cast<const float*>(a.bias)[n];
+  }
+  reinterpret_cast<float*>(a.dst + l.scale)[n] = s;
+  reinterpret_cast<float*>(a.dst + l.bias)[n] = b;
+}
+
+// One 16-byte lane of an operand kilobyte per thread.
+template <class T>
+__global__ __launch_bounds__(256) void q_pack_kernel(QPackArgs a) {
+  const QWeightsLayout l(a.K, a.N);
+  const T* w = static_cast<const T*>(a.w);
+  const float* scale = reinterpret_cast<const float*>(a.dst + l.scale);
+  const size_t total = (size_t)l.blocks * l.kc * 64;
+  for (size_t e = (size_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (size_t)gridDim.x * 256) {
+    const int lane = (int)(e & 63);
+    const size_t ch = e >> 6;
+    const int c = (int)(ch % l.kc), n = (int)(ch / l.kc) * 16 + (lane & 15), k0 = 64 * c + 16 * (lane >> 4);
+    uint32_t v[4] = {0, 0, 0, 0};
+    if (n < a.N) {
+      const float s = scale[n];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        if (k0 + j >= a.K) continue;
+        const T x = w[(k0 + j) * a.wk + n * a.wn];
+        int q;
+        if constexpr (std::is_same<T, int8_t>::value) q = x;
+        else q = q_value(w_value<T>(x), s);
+        v[j >> 2] |= (uint32_t)(q & 0xff) << (8 * (j & 3));
+      }
+    }
+    reinterpret_cast<uint4*>(a.dst)[e] = make_uint4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+template <class T>
+hipError_t launch_pack_t(const QPackArgs& a, hipStream_t s) {
+  const QWeightsLayout l(a.K, a.N);
+  hipError_t e = launch_k(q_scale_kernel<T>, dim3((l.blocks * 16 + 63) / 64), dim3(256), 0, s, a);
+  if (e != hipSuccess) return e;
+  const long blocks = ((long)l.blocks * l.kc * 64 + 255) / 256;
+  return launch_k(q_pack_kernel<T>, dim3((unsigned)std::min<long>(blocks, 4096)), dim3(256), 0, s, a);
+}
+
+// ----------------------------------------------------------------- few rows --
+
+constexpr int kQWaves = 8;
+
+// One block of 16 columns by RT tiles of 16 rows.  Wave w multiplies chunks w,
+// w + 8, ...; U of them are in flight together.
+template <int EPI, int RT, int U>
+__global__ __launch_bounds__(kQWaves * 64) void q_gemm_kernel(GemmArgs a) {
+  using T = std::conditional_t<EPI == EPI_QBF, uint16_t, float>;
+  __shared__ i32x4_t part[kQWaves][RT][64];
+  const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int M = a.meta ? a.meta->m : a.m_host;
+  const int m0 = blockIdx.y * RT * 16, cb = blockIdx.x, kc = a.kchunks;
+  if (m0 >= M) return;  // uniform
+  const int tiles = (M + 15) / 16;
+  const uint4* W = reinterpret_cast<const uint4*>(a.W) + (size_t)cb * kc * 64 + lane;
+  const uint4* A = reinterpret_cast<const uint4*>(a.A) + lane;
+  i32x4_t acc[RT];
+  const uint4* At[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    acc[r] = i32x4_t{0, 0, 0, 0};
+    At[r] = A + (size_t)min(m0 / 16 + r, tiles - 1) * kc * 64;
+  }
+  for (int c0 = w; c0 < kc; c0 += kQWaves * U) {
+    uint4 wf[U], af[U][RT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = min(c0 + kQWaves * u, kc - 1);
+      wf[u] = W[(size_t)c * 64];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) af[u][r] = At[r][(size_t)c * 64];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (c0 + kQWaves * u < kc) {  // uniform
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+          mma_q8(acc[r], __builtin_bit_cast(u32x4_t, wf[u]), __builtin_bit_cast(u32x4_t, af[u][r]));
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r) part[w][r][lane] = acc[r];
+  __syncthreads();
+  if (w >= RT) return;
+  const int row = m0 + 16 * w + n, col = cb * 16 + 4 * g;
+  i32x4_t sum = part[0][w][lane];
+#pragma unroll
+  for (int i = 1; i < kQWaves; ++i) sum += part[i][w][lane];
+  if (row < M)
+    q8_store<T>(a, row, col, sum, a.row_scale[row], *reinterpret_cast<const float4*>(a.col_scale + col),
+                *reinterpret_cast<const float4*>(a.bias + col));
+}
+
+template <int EPI>
+hipError_t launch_gemm_e(const GemmArgs& a, int expected, int rows, hipStream_t s) {
+  if (expected > 128) return launch_tiled_epi<EPI>(a, expected, rows, s);
+  const unsigned blocks = a.Nout / 16;
+  auto go = [&](auto rt) {
+    constexpr int RT = decltype(rt)::value;
+    return launch_k(q_gemm_kernel<EPI, RT, RT == 4 ? 2 : 4>, dim3(blocks, (rows + 16 * RT - 1) / (16 * RT)), dim3(kQWaves * 64), 0, s, a);
+  };
+  if (rows <= 16) return go(std::integral_constant<int, 1>{});
+  if (rows <= 32) return go(std::integral_constant<int, 2>{});
+  return go(std::integral_constant<int, 4>{});
+}
+
+}  // namespace
+
+hipError_t launch_q_rows(const QRowsArgs& a, hipStream_t s) {
+  const bool vec = a.frag || (a.K % 8 == 0 && a.ld % 8 == 0 && (uintptr_t)a.x % 16 == 0);
+  if (a.dtype) return vec ? launch_rows_t<uint16_t, true>(a, s) : launch_rows_t<uint16_t, false>(a, s);
+  return vec ? launch_rows_t<float, true>(a, s) : launch_rows_t<float, false>(a, s);
+}
+
+hipError_t launch_q_pack(const QPackArgs& a, hipStream_t s) {
+  if (a.dtype == 2) return launch_pack_t<int8_t>(a, s);
+  return a.dtype ? launch_pack_t<uint16_t>(a, s) : launch_pack_t<float>(a, s);
+}
+
+hipError_t launch_q_gemm(const GemmArgs& a, int out_f32, int expected, int rows, hipStream_t s) {
+  return out_f32 ? launch_gemm_e<EPI_QF32>(a, expected, rows, s) : launch_gemm_e<EPI_QBF>(a, expected, rows, s);
+}
+
+}  // namespace incvit

@@ -78,6 +78,67 @@ struct QkLayerArgs {
   float eps;
 };
 
+// ----------------------------------------------------------- 8-bit products --
+
+// Operands of the 8-bit matrix instruction (16 x 16 x 64): 16 rows (or weight
+// columns) by 64 values of K are one kilobyte, in which lane 16 g + n holds the
+// 16 values k = 16 g .. 16 g + 15 of row n.  kc: chunks of 64 along K.
+__host__ __device__ __forceinline__ size_t q_off(int r, int k, int kc) {
+  return ((size_t)(r >> 4) * kc + (k >> 6)) * 1024 + ((k >> 4) & 3) * 256 + (r & 15) * 16 + (k & 15);
+}
+
+__host__ __device__ constexpr size_t q_align(size_t x) { return (x + 255) / 256 * 256; }
+
+// Quantised rows: the operand kilobytes of ceil(rows / 16) row tiles, then the
+// rows' scales.
+struct QRowsLayout {
+  int kc;
+  size_t scale, total;
+  __host__ __device__ QRowsLayout(long rows, int K) : kc((K + 63) / 64) {
+    const size_t tiles = (size_t)(rows + 15) / 16;
+    scale = q_align(tiles * kc * 1024);
+    total = scale + q_align(tiles * 64);
+  }
+};
+// Packed weights: the operand kilobytes of ceil(N / 16) column blocks, then the
+// columns' scales and biases (fp32, zero past N).
+struct QWeightsLayout {
+  int kc, blocks;
+  size_t scale, bias, total;
+  __host__ __device__ QWeightsLayout(int K, int N) : kc((K + 63) / 64), blocks((N + 15) / 16) {
+    scale = q_align((size_t)blocks * kc * 1024);
+    bias = scale + q_align((size_t)blocks * 64);
+    total = bias + q_align((size_t)blocks * 64);
+  }
+};
+
+struct QPackArgs {
+  const void* w;        // value (k, n) at k * wk + n * wn
+  long wk, wn;
+  const float* scales;  // given scales (int8 weights), else null
+  const void* bias;     // [N], or null
+  char* dst;            // QWeightsLayout
+  int K, N, dtype;      // dtype 2: int8 weights, fp32 bias
+};
+
+struct QRowsArgs {
+  const void* x;        // [rows][ld], or with `frag` 16 x 32 operand order (frag_off) of `ld` columns
+  long ld;
+  const void* gamma;    // LayerNorm before the quantisation, or null
+  const void* beta;     // (fp32 where param_f32, else the rows' type)
+  float eps;
+  char* dst;            // QRowsLayout's kilobytes
+  float* scale;
+  const Meta* meta;     // rows on the device, or null
+  long rows;
+  int K, dtype, frag, param_f32;
+};
+
+hipError_t launch_q_pack(const QPackArgs& a, hipStream_t s);
+hipError_t launch_q_rows(const QRowsArgs& a, hipStream_t s);
+// out = act(rows x weights) (+ resid): `expected` rows to tune for, at most `rows`
+hipError_t launch_q_gemm(const GemmArgs& a, int out_f32, int expected, int rows, hipStream_t s);
+
 hipError_t launch_qk(const QkArgs& a, hipStream_t s);
 hipError_t launch_qk_layer(const QkLayerArgs& a, int rows, hipStream_t s);
 

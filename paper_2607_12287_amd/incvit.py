@@ -21,7 +21,7 @@ LIB_PATH = os.environ.get("INCVIT_LIB") or os.path.join(_HERE, "libincvit.so")
 INCVIT_OK, INCVIT_ERR_ARG, INCVIT_ERR_SHAPE, INCVIT_ERR_UNSUPPORTED, INCVIT_ERR_STATE, INCVIT_ERR_HIP = 0, -1, -2, -3, -4, -5
 STATUS_NAMES = {0: "INCVIT_OK", -1: "INCVIT_ERR_ARG", -2: "INCVIT_ERR_SHAPE", -3: "INCVIT_ERR_UNSUPPORTED",
                 -4: "INCVIT_ERR_STATE", -5: "INCVIT_ERR_HIP"}
-INCVIT_F32, INCVIT_BF16 = 0, 1
+INCVIT_F32, INCVIT_BF16, INCVIT_I8 = 0, 1, 2
 INCVIT_SCORE_EMBED, INCVIT_SCORE_KEY = 0, 1
 SCORES = {"embed": INCVIT_SCORE_EMBED, "key": INCVIT_SCORE_KEY}
 KERNEL_KINDS = ("embed", "sim", "select", "commit", "qkv", "attn", "oproj", "fc1", "fc2", "res_ln1",
@@ -40,7 +40,8 @@ EXPORTS = ("incvit_canonical_weights_bytes", "incvit_packed_weights_bytes", "inc
            "incvit_profile_read", "incvit_step_graph_create", "incvit_full_graph_create",
            "incvit_graph_launch", "incvit_graph_destroy", "incvit_set_tuning", "incvit_encode_frame",
            "incvit_flow_two_anchor", "incvit_step_noalloc", "incvit_rope_table", "incvit_rope_table_grids",
-           "incvit_qk_norm_rope")
+           "incvit_qk_norm_rope", "incvit_qlinear_weights_bytes", "incvit_qlinear_rows_bytes",
+           "incvit_qlinear_pack_weights", "incvit_qlinear_quantize_rows", "incvit_qlinear_multiply", "incvit_qlinear")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 
 
@@ -124,6 +125,12 @@ def lib() -> ctypes.CDLL:
             "incvit_rope_table": (I32, [P, I64, P, I64, I64, P, P]),
             "incvit_rope_table_grids": (I32, [P, I32, P, I32, P, P]),
             "incvit_qk_norm_rope": (I32, [P, I64, P, P, P, I64, P, P, I64, P]),
+            "incvit_qlinear_weights_bytes": (S, [I32, I32]),
+            "incvit_qlinear_rows_bytes": (S, [I64, I32]),
+            "incvit_qlinear_pack_weights": (I32, [I32, I32, I32, P, I64, I64, P, P, P, P]),
+            "incvit_qlinear_quantize_rows": (I32, [I32, I64, I32, P, I64, P, P, F32, P, P]),
+            "incvit_qlinear_multiply": (I32, [I32, I64, I32, I32, P, P, I32, P, I64, P, I64, P]),
+            "incvit_qlinear": (I32, [I32, I64, I32, I32, P, I64, P, I32, P, I64, P, I64, P, P]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -352,6 +359,121 @@ def qk_norm_rope(q=None, k=None, table=None, pairing: str = "halves", norm: Opti
                index.data_ptr() if index is not None else None, k_rows.data_ptr() if k_rows is not None else None,
                k_out.shape[0] if k_rows is not None else 0))
     return q_out, k_out
+
+
+def incvit_qlinear_weights_bytes(K: int, N: int) -> int:
+    return lib().incvit_qlinear_weights_bytes(K, N)
+
+
+def incvit_qlinear_rows_bytes(rows: int, K: int) -> int:
+    return lib().incvit_qlinear_rows_bytes(rows, K)
+
+
+def incvit_qlinear_pack_weights(dtype: int, K: int, N: int, w: int, k_stride: int, n_stride: int, scales: int, bias: int,
+                                weights: int, stream: int = 0) -> int:
+    return lib().incvit_qlinear_pack_weights(dtype, K, N, w, k_stride, n_stride, scales, bias, weights, stream)
+
+
+def incvit_qlinear_quantize_rows(dtype: int, rows: int, K: int, x: int, x_stride: int, gamma: int, beta: int, eps: float,
+                                 qrows: int, stream: int = 0) -> int:
+    return lib().incvit_qlinear_quantize_rows(dtype, rows, K, x, x_stride, gamma, beta, eps, qrows, stream)
+
+
+def incvit_qlinear_multiply(dtype: int, rows: int, K: int, N: int, qrows: int, weights: int, gelu: int, residual: int,
+                            res_stride: int, out: int, out_stride: int, stream: int = 0) -> int:
+    return lib().incvit_qlinear_multiply(dtype, rows, K, N, qrows, weights, gelu, residual, res_stride, out, out_stride,
+                                         stream)
+
+
+def incvit_qlinear(dtype: int, rows: int, K: int, N: int, x: int, x_stride: int, weights: int, gelu: int, residual: int,
+                   res_stride: int, out: int, out_stride: int, workspace: int, stream: int = 0) -> int:
+    return lib().incvit_qlinear(dtype, rows, K, N, x, x_stride, weights, gelu, residual, res_stride, out, out_stride,
+                                workspace, stream)
+
+
+def _dtype_of(t) -> int:
+    import torch
+    code = {torch.float32: INCVIT_F32, torch.bfloat16: INCVIT_BF16, torch.int8: INCVIT_I8}.get(t.dtype)
+    _need(code is not None and t.is_cuda, "device tensors, fp32 or bf16")
+    return code
+
+
+class QRows:
+    """Rows quantised to 8 bits (quantize_rows), for any number of products."""
+
+    def __init__(self, rows: int, K: int, dtype, buf):
+        self.rows, self.K, self.dtype, self.buf = rows, K, dtype, buf
+
+
+def quantize_rows(x, gamma=None, beta=None, eps: float = 1e-6) -> QRows:
+    """The rows of x [rows][K] in 8-bit integers with a scale each; with gamma
+    (and beta), [K] of x's type, after a LayerNorm."""
+    import torch
+    code = _dtype_of(x)
+    _need(code != INCVIT_I8 and x.dim() == 2 and x.stride(1) == 1, "x: fp32 or bf16 [rows][K], the values of a row one after another")
+    for t, n in ((gamma, "gamma"), (beta, "beta")):
+        _need(t is None or (t.device == x.device and t.dtype == x.dtype and t.is_contiguous() and t.numel() == x.shape[1]),
+              f"{n}: [K] of x's type and device")
+    rows, K = x.shape
+    buf = torch.empty(incvit_qlinear_rows_bytes(rows, K), dtype=torch.uint8, device=x.device)
+    _check(_on(x, incvit_qlinear_quantize_rows, code, rows, K, x.data_ptr(), x.stride(0),
+               gamma.data_ptr() if gamma is not None else None, beta.data_ptr() if beta is not None else None, eps,
+               buf.data_ptr()))
+    return QRows(rows, K, x.dtype, buf)
+
+
+class QLinear:
+    """y = x W + b in 8-bit integers: W [K][N] (any strides: pass linear.weight.t()
+    for one stored [N][K]) is quantised and packed once.  W fp32 or bf16, bias [N]
+    of its type; or W int8 with `scales` (fp32 [N]) and an fp32 bias."""
+
+    def __init__(self, weight, bias=None, scales=None):
+        import torch
+        code = _dtype_of(weight)
+        _need(weight.dim() == 2, "weight: [K][N]")
+        self.K, self.N = weight.shape
+        _need((code == INCVIT_I8) == (scales is not None), "scales: with int8 weights, and only with them")
+        for t, n, dt in ((bias, "bias", torch.float32 if code == INCVIT_I8 else weight.dtype), (scales, "scales", torch.float32)):
+            _need(t is None or (t.device == weight.device and t.dtype == dt and t.is_contiguous() and t.numel() == self.N),
+                  f"{n}: {dt} [N] on the weights' device")
+        n = incvit_qlinear_weights_bytes(self.K, self.N)
+        if n == 0:
+            raise IncvitError(INCVIT_ERR_UNSUPPORTED, f"a product of K = {self.K}, N = {self.N}")
+        self.device = weight.device
+        self.weights = torch.empty(n, dtype=torch.uint8, device=self.device)
+        _check(_on(weight, incvit_qlinear_pack_weights, code, self.K, self.N, weight.data_ptr(), weight.stride(0),
+                   weight.stride(1), scales.data_ptr() if scales is not None else None,
+                   bias.data_ptr() if bias is not None else None, self.weights.data_ptr()))
+
+    def __call__(self, x, gelu: bool = False, residual=None, out=None):
+        """act(x W + b) + residual for x [rows][K] (fp32 or bf16, the values of a row
+        one after another) or QRows; residual and out [rows][N] of x's type (out may
+        be residual).  Returns out."""
+        import torch
+        q = isinstance(x, QRows)
+        if q:
+            rows, K, src = x.rows, x.K, x.buf
+            code = INCVIT_BF16 if x.dtype == torch.bfloat16 else INCVIT_F32
+        else:
+            code, src = _dtype_of(x), x
+            _need(code != INCVIT_I8 and x.dim() == 2 and x.stride(1) == 1,
+                  "x: fp32 or bf16 [rows][K], the values of a row one after another")
+            rows, K = x.shape
+        _need(K == self.K and src.device == self.device, "x: rows of K values on the weights' device")
+        if out is None:
+            out = torch.empty((rows, self.N), dtype=x.dtype, device=self.device)
+        for t, n in ((out, "out"), (residual, "residual")):
+            _need(t is None or (t.dtype == x.dtype and t.device == self.device and t.shape == (rows, self.N) and
+                                (t.stride(1) == 1 or self.N == 1)), f"{n}: [rows][N] of x's type, the values of a row one after another")
+        r, rs = (residual.data_ptr(), residual.stride(0)) if residual is not None else (None, 0)
+        if q:
+            _check(_on(src, incvit_qlinear_multiply, code, rows, K, self.N, src.data_ptr(), self.weights.data_ptr(), int(gelu),
+                       r, rs, out.data_ptr(), out.stride(0)))
+        else:
+            ws = torch.empty(incvit_qlinear_rows_bytes(rows, K), dtype=torch.uint8, device=self.device)
+            _check(_on(src, incvit_qlinear, code, rows, K, self.N, x.data_ptr(), x.stride(0), self.weights.data_ptr(), int(gelu),
+                       r, rs, out.data_ptr(), out.stride(0), ws.data_ptr()))
+        return out
 
 
 def incvit_cache_export(h, cache: int, dst: int, stream: int = 0) -> int:

@@ -63,3 +63,19 @@ def rotate(n, cos, sin, pairing):
     out[..., a] = n[..., a] * c - n[..., b] * s
     out[..., b] = n[..., b] * c + n[..., a] * s
     return out
+
+
+def quantized(x, axis):
+    """(integers, scales) of values along `axis`, all as float64: s = max|x| / 127 and x / s each rounded to fp32, then to the
+    nearest integer with ties to even."""
+    x = np.asarray(x, dtype=np.float64)
+    with np.errstate(invalid="ignore"):
+        top = np.abs(x).max(axis=axis, keepdims=True)
+        s = np.where(np.isfinite(top), top / 127.0, np.nan).astype(np.float32).astype(np.float64)
+        ratio = (x / np.where(s > 0, s, 1.0)).astype(np.float32).astype(np.float64)
+        q = np.where(s > 0, np.clip(np.rint(ratio), -127, 127), 0.0)
+    return q, s
+
+
+def gelu(x):
+    return 0.5 * x * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (x + 0.044715 * x ** 3)))

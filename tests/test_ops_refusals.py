@@ -117,3 +117,51 @@ def test_make_rope_checks_its_sizes():
         incvit.make_rope(64, (16, 16), scale=(1.0,))
     with pytest.raises(KeyError):
         incvit.make_rope(64, (16, 16), ladder="both")
+
+
+def test_qlinear_sizes():
+    w, r = incvit.incvit_qlinear_weights_bytes, incvit.incvit_qlinear_rows_bytes
+    for K, N in [(0, 5), (5, 0), (65537, 5), (5, 2 ** 20 + 1), (65536, 65536), (-1, 5)]:
+        assert w(K, N) == 0
+        assert incvit.incvit_qlinear_pack_weights(0, K, N, A, N, 1, 0, 0, B) == UNSUPPORTED
+        assert incvit.incvit_qlinear(0, 5, K, N, A, K, B, 0, 0, 0, T, N, X) == UNSUPPORTED
+    assert w(64, 16) >= 64 * 16 + 2 * 64 and w(65, 17) >= 2 * 128 * 16
+    for rows, K in [(-1, 5), (5, 0), (5, 65537), (2 ** 31, 5)]:
+        assert r(rows, K) == 0
+    assert r(0, 64) == 0 and r(1, 64) >= 1024 + 64 and r(17, 65) >= 2 * 2048
+
+
+def test_qlinear_pack_refusals():
+    f = incvit.incvit_qlinear_pack_weights
+    ok = dict(dtype=0, K=64, N=16, w=A, k_stride=16, n_stride=1, scales=0, bias=0, weights=B)
+    for kw, status in [(dict(dtype=3), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED), (dict(w=0), ARG), (dict(weights=0), ARG),
+                       (dict(weights=B + 64), ARG), (dict(scales=T), ARG), (dict(dtype=2), ARG), (dict(w=A + 2), ARG),
+                       (dict(bias=T + 2), ARG), (dict(dtype=2, scales=T + 2), ARG), (dict(k_stride=-1), ARG),
+                       (dict(n_stride=2 ** 41), ARG)]:
+        assert f(*{**ok, **kw}.values()) == status, kw
+
+
+def test_qlinear_row_refusals():
+    f = incvit.incvit_qlinear_quantize_rows
+    ok = dict(dtype=1, rows=5, K=64, x=A, x_stride=64, gamma=0, beta=0, eps=1e-6, qrows=B)
+    for kw, status in [(dict(dtype=2), UNSUPPORTED), (dict(rows=-1), ARG), (dict(rows=2 ** 31), ARG), (dict(x=0), ARG), (dict(x=A + 1), ARG),
+                       (dict(x_stride=-1), ARG), (dict(qrows=0), ARG), (dict(qrows=B + 128), ARG), (dict(beta=T), ARG),
+                       (dict(gamma=T + 1), ARG), (dict(gamma=T, eps=-1.0), ARG), (dict(gamma=T, eps=math.nan), ARG)]:
+        assert f(*{**ok, **kw}.values()) == status, kw
+    assert f(1, 0, 64, 0, 64, 0, 0, 1e-6, 0) == OK
+
+
+def test_qlinear_product_refusals():
+    two, one = incvit.incvit_qlinear_multiply, incvit.incvit_qlinear
+    ok = dict(dtype=1, rows=5, K=64, N=16, x=A, weights=B, gelu=0, residual=0, res_stride=0, out=T, out_stride=16)
+    for kw, status in [(dict(dtype=2), UNSUPPORTED), (dict(rows=-1), ARG), (dict(x=0), ARG), (dict(x=A + 1), ARG), (dict(weights=0), ARG),
+                       (dict(weights=B + 16), ARG), (dict(gelu=2), ARG), (dict(residual=X + 1, res_stride=16), ARG),
+                       (dict(residual=X, res_stride=-1), ARG), (dict(out=0), ARG), (dict(out=T + 1), ARG), (dict(out_stride=15), SHAPE),
+                       (dict(residual=T, res_stride=32), SHAPE)]:
+        d = {**ok, **kw}
+        assert two(*d.values()) == status, kw
+        v = list(d.values())
+        assert one(*v[:5], 64, *v[5:], X) == status, kw
+    assert one(1, 5, 64, 16, A, 64, B, 0, 0, 0, T, 16, X + 16) == ARG
+    assert one(1, 5, 64, 16, A, -1, B, 0, 0, 0, T, 16, X) == ARG
+    assert two(1, 0, 64, 16, 0, 0, 0, 0, 0, 0, 0) == OK and one(1, 0, 64, 16, 0, 0, 0, 0, 0, 0, 0, 0, 0) == OK
