@@ -100,6 +100,21 @@ typedef struct {
   int32_t score;       /* incvit_score; part of the cache identity */
   int32_t mlp_all;     /* 0: exact reuse (default); 1: every row through the MLP
                           each frame (see above); part of the cache identity */
+  /* Encoders without the learned positions' monopoly (all zero: as above; each
+   * is part of the cache identity): */
+  int32_t rope;        /* 0: none; 1, 2: queries and keys of every layer are rotated
+                          by their token's row and column in the patch grid, pairs
+                          as INCVIT_PAIR_HALVES (1) or INCVIT_PAIR_ADJACENT (2) of
+                          the whole head, d_h / 4 pairs for the rows and then d_h / 4
+                          for the columns, each on a ladder of its own (incvit_rope
+                          with axes = 2, INCVIT_LADDER_AXIS, INCVIT_LAYOUT_BLOCKS) */
+  float rope_theta;    /* the ladder's base, in [1, 1e12] (read with rope only) */
+  int32_t qk_norm;     /* incvit_norm over each head of the queries and keys, with
+                          ln_eps, before the rotation */
+  int32_t mlp_int8;    /* 1: the MLP's products in 8-bit integers (incvit_qlinear's
+                          arithmetic): G = S(GELU(LN2(H) W_1 + b_1)) and
+                          H + S(G W_2 + b_2) with LN2(H), G and the weights
+                          quantised; mlp_dim <= 65536 */
 } incvit_config;
 
 typedef struct incvit_handle incvit_handle;
@@ -111,8 +126,9 @@ typedef struct incvit_handle incvit_handle;
  *   W_pe [P][D] (row (c*p + dy)*p + dx), b_pe [D], Pos [N][D],
  *   per layer l = 0..L-1: ln1_g [D], ln1_b [D], W_qkv [D][3D] (columns
  *     [0,D) Q, [D,2D) K, [2D,3D) V; head j owns columns [j*d_h,(j+1)*d_h) of
- *     each block), b_qkv [3D], W_o [D][D], b_o [D], ln2_g [D], ln2_b [D],
- *     W_1 [D][F], b_1 [F], W_2 [F][D], b_2 [D],
+ *     each block), b_qkv [3D], with qk_norm the queries' gamma [d_h], with LAYER
+ *     their beta [d_h], and then the same of the keys, W_o [D][D], b_o [D],
+ *     ln2_g [D], ln2_b [D], W_1 [D][F], b_1 [F], W_2 [F][D], b_2 [D],
  *   lnf_g [D], lnf_b [D].
  * Every linear layer computes y = x W + b.  Returns 0 for an invalid config. */
 size_t incvit_canonical_weights_bytes(const incvit_config* cfg);
@@ -533,6 +549,8 @@ typedef enum {
   INCVIT_K_KEY_LN,    /* key score: LayerNorm 1 of layer 0, all tokens    */
   INCVIT_K_KEY_PROJ,  /* key score: key projection, all tokens            */
   INCVIT_K_HSUM,      /* mlp_all: H = X + cached attention branch, all rows */
+  INCVIT_K_QK_NORM,   /* qk_norm, rope: queries and new keys, in place     */
+  INCVIT_K_QUANT,     /* mlp_int8: the MLP's inputs in 8-bit integers      */
   INCVIT_K_COUNT
 } incvit_kernel_kind;
 

@@ -60,6 +60,12 @@ applied to the output of every operation of the layer and nowhere else:
     A2 = S(LN2(H))            F     = S(A2 W_1 + b_1)      G = S(GELU(F))
     M  = S(G W_2 + b_2)       X'    = S(H + M)             Y = S(LN_f(X^L))
 
+With the options of a model shape, (Q, K) = S(rotate(norm(Q, K))) follows the
+projection as one operation (``head_norm_rotate``), and the MLP in 8-bit
+integers (``linear_int8``) is G = S(GELU(LN2(H) W_1 + b_1)), M = S(G W_2 + b_2):
+its integers come from the unrounded LN2(H) and from G, and GELU belongs to the
+first product.
+
 and X^0 = S(T^0).  A linear layer with its bias is one operation, as is the
 attention.  The two MLP readings share this block exactly (the "all" reading
 caches B per layer), so their full encodes are identical.  The test
@@ -114,6 +120,51 @@ def layer_norm(x: np.ndarray, g: np.ndarray, b: np.ndarray, eps: float) -> np.nd
 def gelu_tanh(x: np.ndarray) -> np.ndarray:
     """GELU, tanh form: 0.5 x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3)))."""
     return 0.5 * x * (1.0 + np.tanh(math.sqrt(2.0 / math.pi) * (x + 0.044715 * x ** 3)))
+
+
+def head_norm_rotate(x: np.ndarray, heads: int, norm: Optional[str], g, b, eps: float, rope: Optional[str],
+                     theta: float, tok: np.ndarray, grid_w: int) -> np.ndarray:
+    """Norm of every head of the rows x [m][D] (gains g, shifts b) and its rotation
+    by the rows' tokens `tok` of a grid `grid_w` wide: the first half of the pairs
+    turns with the grid row, the second with the column, pair j of either by
+    position * theta^(-j / (d_h / 4)); pairs are (i, i + d_h / 2) ("halves") or
+    (2i, 2i + 1) ("adjacent")."""
+    m, d = x.shape
+    dh = d // heads
+    h = x.reshape(m, heads, dh)
+    if norm == "layer":
+        h = layer_norm(h, g, b, eps)
+    elif norm == "rms":
+        h = h / np.sqrt((h ** 2).mean(axis=-1, keepdims=True) + eps) * g
+    if rope is not None:
+        n = dh // 4
+        ladder = float(theta) ** (-np.arange(n) / n)
+        ang = np.concatenate([np.outer(tok // grid_w, ladder), np.outer(tok % grid_w, ladder)], axis=1)
+        turn = np.exp(1j * ang)[:, None, :]
+        if rope == "halves":
+            z = (h[..., :dh // 2] + 1j * h[..., dh // 2:]) * turn
+            h = np.concatenate([z.real, z.imag], axis=-1)
+        else:
+            z = (h[..., 0::2] + 1j * h[..., 1::2]) * turn
+            h = np.stack([z.real, z.imag], axis=-1).reshape(m, heads, dh)
+    return h.reshape(m, d)
+
+
+def quantize_int8(x: np.ndarray, axis: int):
+    """8-bit integers and scales of values along `axis`: scale = largest magnitude
+    / 127 in fp32, the quotient in fp32 and then to the nearest integer, ties to
+    even; zeros where the scale is zero."""
+    s = (np.abs(x).max(axis=axis, keepdims=True) / 127.0).astype(np.float32)
+    live = s > 0
+    q = (x / np.where(live, s, 1.0).astype(np.float64)).astype(np.float32)
+    return np.where(live, np.clip(np.rint(q), -127, 127), 0.0).astype(np.float64), s.astype(np.float64)
+
+
+def linear_int8(x: np.ndarray, w: np.ndarray, b: np.ndarray) -> np.ndarray:
+    """x W + b with the rows of x and the columns of W in 8-bit integers."""
+    xq, xs = quantize_int8(x, 1)
+    wq, ws = quantize_int8(w, 0)
+    return (xq @ wq) * (xs * ws) + b
 
 
 def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, heads: int) -> np.ndarray:
@@ -262,9 +313,14 @@ def attn_branch(model: Model, l: int, Z: np.ndarray, U: np.ndarray, K: np.ndarra
     D = m.dim
     A = S(layer_norm(Z, model.p(l, "ln1_g"), model.p(l, "ln1_b"), model.eps), dt)
     qkv = S(A @ model.p(l, "w_qkv") + model.p(l, "b_qkv"), dt)     # eq. 4
-    K[U] = qkv[:, D:2 * D]
+    Q, Knew = qkv[:, :D], qkv[:, D:2 * D]
+    if m.rope is not None or m.qk_norm is not None:
+        Q, Knew = (S(head_norm_rotate(x, m.heads, m.qk_norm, model.w.get(f"l{l}.{n}_g"), model.w.get(f"l{l}.{n}_b"),
+                                      model.eps, m.rope, m.rope_theta, np.asarray(U), m.grid_w), dt)
+                   for x, n in ((Q, "qn"), (Knew, "kn")))
+    K[U] = Knew
     V[U] = qkv[:, 2 * D:]
-    O = S(attention(qkv[:, :D], K, V, m.heads), dt)
+    O = S(attention(Q, K, V, m.heads), dt)
     if trace is not None:
         trace.setdefault("O", []).append(O)
     return S(O @ model.p(l, "w_o") + model.p(l, "b_o"), dt)
@@ -277,6 +333,10 @@ def mlp_block(model: Model, l: int, X: np.ndarray, Bo: np.ndarray, trace: Option
     Hres = S(X + Bo, dt)
     if trace is not None:
         trace.setdefault("H", []).append(Hres)
+    if model.shape.mlp_int8:
+        A2 = layer_norm(Hres, model.p(l, "ln2_g"), model.p(l, "ln2_b"), model.eps)
+        G = S(gelu_tanh(linear_int8(A2, model.p(l, "w_1"), model.p(l, "b_1"))), dt)
+        return S(Hres + S(linear_int8(G, model.p(l, "w_2"), model.p(l, "b_2")), dt), dt)
     A2 = S(layer_norm(Hres, model.p(l, "ln2_g"), model.p(l, "ln2_b"), model.eps), dt)
     F1 = S(A2 @ model.p(l, "w_1") + model.p(l, "b_1"), dt)
     G = S(gelu_tanh(F1), dt)

@@ -36,6 +36,9 @@ struct Shape {
   float eps;
   int score;  // 0: the cosine compares embedded tokens; 1: first-layer keys
   int mlp_all;  // 1: every row through the MLP each frame (cached attention branch)
+  int rope;     // 0: none, 1: halves, 2: adjacent pairs rotated by row and column
+  int qk_norm;  // incvit_norm of the query and key heads
+  int q8;       // 1: the MLP's products in 8-bit integers
 };
 
 // Byte offsets inside one stream's cache.

@@ -29,11 +29,14 @@ struct PackedLayer {
   // LN1 folded into W_qkv and LN2 into W_1 (packed only): column sums of the
   // folded weights and beta^T W + b
   size_t qkv_c1, qkv_c2b, fc1_c1, fc1_c2b;
+  // norms of the query and key heads (with qk_norm)
+  size_t qn_g, qn_b, kn_g, kn_b;
 };
 
 struct PackedLayout {
   size_t w_pe, b_pe, pos, lnf_g, lnf_b, total;
   size_t w_key;  // W_K of layer 0, packed like w_pe (key score)
+  size_t rope;   // cosines and sines [N][d_h / 2][2] (with rope)
   std::vector<PackedLayer> layers;
 };
 
@@ -45,6 +48,7 @@ struct CanonLayout {  // element offsets into the canonical buffer
 struct WsLayout {
   size_t meta, rows, count, idx, sim, t0, kn, key, z, q, o, h, g, part, total;
   size_t valid, zpos, rows_all, meta_all;  // all-rows MLP reading
+  size_t q8;                               // quantised MLP inputs (mlp_int8)
   int Mpad;
 };
 
@@ -65,6 +69,10 @@ bool make_shape(const incvit_config* c, Shape& sh, incvit_status& st, std::strin
   if (c->dtype != INCVIT_F32 && c->dtype != INCVIT_BF16) { st = INCVIT_ERR_UNSUPPORTED; err = "dtype must be INCVIT_F32 or INCVIT_BF16"; return false; }
   if (c->score != INCVIT_SCORE_EMBED && c->score != INCVIT_SCORE_KEY) { st = INCVIT_ERR_ARG; err = "score must be INCVIT_SCORE_EMBED or INCVIT_SCORE_KEY"; return false; }
   if (c->mlp_all != 0 && c->mlp_all != 1) { st = INCVIT_ERR_ARG; err = "mlp_all must be 0 or 1"; return false; }
+  if (c->rope < 0 || c->rope > 2) { st = INCVIT_ERR_ARG; err = "rope must be 0, 1 or 2"; return false; }
+  if (c->rope && !(c->rope_theta >= 1.0f && c->rope_theta <= 1e12f)) { st = INCVIT_ERR_ARG; err = "rope_theta must be in [1, 1e12]"; return false; }
+  if (c->qk_norm < INCVIT_NORM_NONE || c->qk_norm > INCVIT_NORM_LAYER) { st = INCVIT_ERR_ARG; err = "qk_norm must be an incvit_norm"; return false; }
+  if (c->mlp_int8 != 0 && c->mlp_int8 != 1) { st = INCVIT_ERR_ARG; err = "mlp_int8 must be 0 or 1"; return false; }
   sh.N = (c->img_h / c->patch) * (c->img_w / c->patch);
   sh.P = c->channels * c->patch * c->patch;
   sh.D = c->dim;
@@ -80,12 +88,16 @@ bool make_shape(const incvit_config* c, Shape& sh, incvit_status& st, std::strin
   sh.eps = c->ln_eps;
   sh.score = c->score;
   sh.mlp_all = c->mlp_all;
+  sh.rope = c->rope;
+  sh.qk_norm = c->qk_norm;
+  sh.q8 = c->mlp_int8;
   st = INCVIT_ERR_UNSUPPORTED;
   if (sh.D % 32) { err = "dim must be a multiple of 32"; return false; }
   if (sh.D > kMaxDim) { snprintf(buf, sizeof buf, "dim must be <= %d", kMaxDim); err = buf; return false; }
   if (sh.dh % 8 || sh.dh > kMaxHeadDim) { err = "head dim must be a multiple of 8 and <= 128"; return false; }
   if (sh.N > kMaxTokens) { snprintf(buf, sizeof buf, "at most %d tokens", kMaxTokens); err = buf; return false; }
   if (c->max_streams < 1 || c->max_streams > kMaxViews) { snprintf(buf, sizeof buf, "max_streams must be in [1, %d]", kMaxViews); err = buf; return false; }
+  if (sh.q8 && sh.F > 65536) { err = "mlp_dim must be <= 65536 with mlp_int8"; return false; }
   // Kernels address each buffer through 32-bit offsets (buffer resources and
   // 32-bit index products), so the largest buffer one launch can touch must
   // stay below 4 GiB: a stream's patches, W_pe, a packed GEMM matrix, and the
@@ -127,19 +139,25 @@ PackedLayout packed_layout(const Shape& sh) {
     L.b_o = take(D * 4);
     L.ln2_g = take(D * 4);
     L.ln2_b = take(D * 4);
-    L.w_1 = take(packed_gemm_bytes(D, sh.Fpad, eb));
+    L.w_1 = take(sh.q8 ? QWeightsLayout(D, sh.F).total : packed_gemm_bytes(D, sh.Fpad, eb));
     L.b_1 = take((size_t)sh.Fpad * 4);
-    L.w_2 = take(packed_gemm_bytes(sh.Fpad, D, eb));
+    L.w_2 = take(sh.q8 ? QWeightsLayout(sh.F, D).total : packed_gemm_bytes(sh.Fpad, D, eb));
     L.b_2 = take(D * 4);
     L.qkv_c1 = take(3 * D * 4);
     L.qkv_c2b = take(3 * D * 4);
     L.fc1_c1 = take((size_t)sh.Fpad * 4);
     L.fc1_c2b = take((size_t)sh.Fpad * 4);
+    const size_t head = sh.qk_norm ? (size_t)sh.dh * 4 : 0;
+    L.qn_g = take(head);
+    L.qn_b = take(head);
+    L.kn_g = take(head);
+    L.kn_b = take(head);
     p.layers.push_back(L);
   }
   p.lnf_g = take(D * 4);
   p.lnf_b = take(D * 4);
   p.w_key = take((size_t)D * D * eb);
+  p.rope = take(sh.rope ? (size_t)sh.N * sh.dh * 4 : 0);
   p.total = off;
   return p;
 }
@@ -158,6 +176,11 @@ CanonLayout canon_layout(const Shape& sh) {
     L.ln1_b = take(D);
     L.w_qkv = take(D * 3 * D);
     L.b_qkv = take(3 * D);
+    const size_t gain = sh.qk_norm ? sh.dh : 0, shift = sh.qk_norm == INCVIT_NORM_LAYER ? sh.dh : 0;
+    L.qn_g = take(gain);
+    L.qn_b = take(shift);
+    L.kn_g = take(gain);
+    L.kn_b = take(shift);
     L.w_o = take(D * D);
     L.b_o = take(D);
     L.ln2_g = take(D);
@@ -204,6 +227,11 @@ uint32_t config_hash(const incvit_config& c) {
   uint32_t e;
   memcpy(&e, &c.ln_eps, 4);
   mix(e);
+  if (c.rope || c.qk_norm || c.mlp_int8) {  // caches of models without them keep their identity
+    float theta = c.rope ? c.rope_theta : 0.0f;
+    memcpy(&e, &theta, 4);
+    for (uint32_t x : {(uint32_t)c.rope, e, (uint32_t)c.qk_norm, (uint32_t)c.mlp_int8}) mix(x);
+  }
   return h == 0 ? 1u : h;
 }
 
@@ -332,6 +360,7 @@ WsLayout ws_layout(const Shape& sh, int B) {
   w.zpos = take(sh.mlp_all ? (size_t)M * 4 : 0);
   w.rows_all = take(sh.mlp_all ? (size_t)w.Mpad * sizeof(RowInfo) : 0);
   w.meta_all = take(sh.mlp_all ? sizeof(Meta) : 0);
+  w.q8 = take(sh.q8 ? QRowsLayout(w.Mpad, std::max(sh.D, sh.F)).total : 0);
   w.total = off;
   return w;
 }
@@ -482,7 +511,7 @@ incvit_status run_layers(incvit_handle* h, const Views& views, int B, const WsLa
     if (kind == G_FC1) return ((known && r >= 192) || (r >= 96 && sh.Fpad / 16 > 256)) && tiles64(r, sh.Fpad) >= 128;
     return kind == G_QKV && known && r >= 192 && tiles64(r, 3 * sh.D) >= 128;
   };
-  const bool tiled_fc2 = tiled_of(G_FC2);
+  const bool tiled_fc2 = !sh.q8 && tiled_of(G_FC2);
   // The large-row MLP down projection runs over K = F: its workgroup's chunks
   // follow one another, so while 64 x 128 tiles leave more than half of the CUs
   // idle it is split over K like the small-M form (partial sums added by the
@@ -508,7 +537,8 @@ incvit_status run_layers(incvit_handle* h, const Views& views, int B, const WsLa
     // sums of every row no longer go through memory), so by default only when
     // M is known on the host and at least 192; the large-row form whenever it
     // is not split over K (above)
-    const bool down = !all && l + 1 < sh.L &&
+    // (the 8-bit down projection always leaves its fp32 sums to the row kernel)
+    const bool down = !sh.q8 && !all && l + 1 < sh.L &&
                       (tiled_fc2 ? fc2_split == 1
                                  : h->fc2_mode == 2 || (h->fc2_mode == 0 && exact_m && mmax >= 192));
     auto gemm = [&](int kind, int kernel_kind) -> incvit_status {
@@ -578,7 +608,7 @@ incvit_status run_layers(incvit_handle* h, const Views& views, int B, const WsLa
       r.sh = sh;
       r.layer = l;
       r.part = reinterpret_cast<const float*>(ws + wl.part);
-      r.ksplit = tiled_fc2 ? fc2_split : g.ksplit;
+      r.ksplit = sh.q8 ? 1 : tiled_fc2 ? fc2_split : g.ksplit;
       r.mpad = wl.Mpad;
       r.ahead = mlp_known ? mlp_rows : 32;
       r.N = sh.N;
@@ -598,9 +628,78 @@ incvit_status run_layers(incvit_handle* h, const Views& views, int B, const WsLa
       return run(h, kernel_kind, s, [&] { return launch_res(r, mlp_rows, s); });
     };
 
+    // One MLP projection in 8-bit integers: the rows (LN2 of H, in operand order,
+    // or G) quantised, then multiplied; G = S(GELU(.)) row-major, or the fp32 sums
+    // of the down projection, to which the row kernel adds the bias.
+    auto mlp_q8 = [&](int kind, int kernel_kind) -> incvit_status {
+      const bool up = kind == G_FC1;
+      const int K = up ? sh.D : sh.F, Nout = up ? sh.F : sh.D;
+      const QRowsLayout ql(wl.Mpad, K);
+      const QWeightsLayout qw(K, Nout);
+      QRowsArgs qa = {};
+      qa.x = ws + (up ? wl.h : wl.g);
+      qa.ld = up ? sh.D : sh.Fpad;
+      qa.frag = up;
+      if (up) {
+        qa.gamma = fptr(h, P.ln2_g);
+        qa.beta = fptr(h, P.ln2_b);
+        qa.param_f32 = 1;
+        qa.eps = sh.eps;
+      }
+      qa.dst = ws + wl.q8;
+      qa.scale = reinterpret_cast<float*>(ws + wl.q8 + ql.scale);
+      qa.meta = mmeta;
+      qa.rows = mlp_rows;
+      qa.K = K;
+      qa.dtype = sh.dtype;
+      const incvit_status st = run(h, INCVIT_K_QUANT, s, [&] { return launch_q_rows(qa, s); });
+      if (st != INCVIT_OK) return st;
+      const char* w = h->packed + (up ? P.w_1 : P.w_2);
+      GemmArgs a = {};
+      a.A = qa.dst;
+      a.W = w;
+      a.bias = reinterpret_cast<const float*>(w + qw.bias);
+      a.meta = mmeta;
+      a.out = ws + (up ? wl.g : wl.part);
+      a.lda = 64 * qw.kc;
+      a.kchunks = qw.kc;
+      a.Nout = 16 * qw.blocks;
+      a.ksplit = 1;
+      a.mpad = wl.Mpad;
+      a.row_scale = qa.scale;
+      a.col_scale = reinterpret_cast<const float*>(w + qw.scale);
+      a.out_ld = up ? sh.Fpad : sh.D;
+      a.n = Nout;
+      a.gelu = up;
+      a.wide = Nout % 4 == 0;
+      return run(h, kernel_kind, s, [&] { return launch_q_gemm(a, !up || !sh.dtype, exp_mlp, mlp_rows, s); });
+    };
+
     incvit_status st;
     if (mmax > 0) {  // attention part: the refreshed rows only
       if ((st = gemm(G_QKV, INCVIT_K_QKV)) != INCVIT_OK) return st;
+      if (sh.rope || sh.qk_norm) {
+        QkLayerArgs qa = {};
+        qa.rows = rows;
+        qa.meta = meta;
+        qa.sh = sh;
+        qa.cl = h->cl;
+        qa.layer = l;
+        qa.q = ws + wl.q;
+        if (sh.qk_norm) {
+          qa.q_gamma = fptr(h, P.qn_g);
+          qa.k_gamma = fptr(h, P.kn_g);
+          if (sh.qk_norm == INCVIT_NORM_LAYER) {
+            qa.q_beta = fptr(h, P.qn_b);
+            qa.k_beta = fptr(h, P.kn_b);
+          }
+        }
+        if (sh.rope) qa.table = fptr(h, h->pl.rope);
+        qa.adjacent = sh.rope == 2;
+        qa.norm = sh.qk_norm;
+        qa.eps = sh.eps;
+        if ((st = run(h, INCVIT_K_QK_NORM, s, [&] { return launch_qk_layer(qa, mmax, s); })) != INCVIT_OK) return st;
+      }
       AttnArgs aa;
       memset(&aa, 0, sizeof aa);
       aa.meta = meta;
@@ -622,8 +721,9 @@ incvit_status run_layers(incvit_handle* h, const Views& views, int B, const WsLa
       HsumArgs ha{mrows, h->cl, sh, l, mall, ws + wl.h};
       if ((st = run(h, INCVIT_K_HSUM, s, [&] { return launch_hsum(ha, s); })) != INCVIT_OK) return st;
     }
-    if ((st = gemm(G_FC1, INCVIT_K_FC1)) != INCVIT_OK) return st;
-    if ((st = gemm(G_FC2, INCVIT_K_FC2)) != INCVIT_OK) return st;
+    auto mlp = [&](int kind, int kernel_kind) { return sh.q8 ? mlp_q8(kind, kernel_kind) : gemm(kind, kernel_kind); };
+    if ((st = mlp(G_FC1, INCVIT_K_FC1)) != INCVIT_OK) return st;
+    if ((st = mlp(G_FC2, INCVIT_K_FC2)) != INCVIT_OK) return st;
     if (!down && (st = rowk(INCVIT_K_RES_LN1)) != INCVIT_OK) return st;
   }
   return INCVIT_OK;
@@ -787,6 +887,11 @@ incvit_status incvit_pack_weights(const incvit_config* cfg, const void* canonica
                K, Ncols, round_up(K, 32) / 32, round_up(Npadc, 16) / 16, sh.dtype};
     e = launch_fold(a, s);
   };
+  // W [K][N] in 8-bit integers (bias: canonical [N], or null)
+  auto quantize = [&](size_t coff, size_t poff, const char* bias, int K, int N) {
+    if (e != hipSuccess) return;
+    e = launch_q_pack(QPackArgs{src + coff * eb, N, 1, nullptr, bias, dst + poff, K, N, sh.dtype}, s);
+  };
   const int D = sh.D;
   e = launch_fixed_pack(FixedPackArgs{src + cn.w_pe * eb, dst + pl.w_pe, sh.P, D, D, sh.dtype}, s);
   conv(cn.b_pe, pl.b_pe, D, D);
@@ -803,17 +908,41 @@ incvit_status incvit_pack_weights(const incvit_config* cfg, const void* canonica
     conv(C.b_o, P.b_o, D, D);
     conv(C.ln2_g, P.ln2_g, D, D);
     conv(C.ln2_b, P.ln2_b, D, D);
-    pack(C.w_1, P.w_1, D, sh.F, D, sh.Fpad);
-    fold(C.w_1, P.w_1, C.ln2_g, C.ln2_b, C.b_1, P.fc1_c1, P.fc1_c2b, D, sh.F, sh.Fpad);
+    if (sh.q8) {
+      quantize(C.w_1, P.w_1, src + C.b_1 * eb, D, sh.F);
+      quantize(C.w_2, P.w_2, nullptr, sh.F, D);
+    } else {
+      pack(C.w_1, P.w_1, D, sh.F, D, sh.Fpad);
+      fold(C.w_1, P.w_1, C.ln2_g, C.ln2_b, C.b_1, P.fc1_c1, P.fc1_c2b, D, sh.F, sh.Fpad);
+      pack(C.w_2, P.w_2, sh.F, D, sh.Fpad, D);
+    }
     conv(C.b_1, P.b_1, sh.F, sh.Fpad);
-    pack(C.w_2, P.w_2, sh.F, D, sh.Fpad, D);
     conv(C.b_2, P.b_2, D, D);
+    if (sh.qk_norm) {
+      conv(C.qn_g, P.qn_g, sh.dh, sh.dh);
+      conv(C.kn_g, P.kn_g, sh.dh, sh.dh);
+      if (sh.qk_norm == INCVIT_NORM_LAYER) {
+        conv(C.qn_b, P.qn_b, sh.dh, sh.dh);
+        conv(C.kn_b, P.kn_b, sh.dh, sh.dh);
+      }
+    }
   }
   conv(cn.lnf_g, pl.lnf_g, D, D);
   conv(cn.lnf_b, pl.lnf_b, D, D);
   // W_K of layer 0 (columns D..2D-1 of W_qkv) for the key score
   if (e == hipSuccess)
     e = launch_fixed_pack(FixedPackArgs{src + (cn.layers[0].w_qkv + D) * eb, dst + pl.w_key, D, D, 3 * (long)D, sh.dtype}, s);
+  // the rotation of every token, by its row and column
+  if (e == hipSuccess && sh.rope) {
+    RopeArgs a = {};
+    const incvit_rope r = {2, {sh.dh / 4, sh.dh / 4, 0}, INCVIT_LADDER_AXIS, INCVIT_LAYOUT_BLOCKS, cfg->rope_theta, {1.0, 1.0, 1.0}};
+    if (!rope_pairs(r, a)) return fail(nullptr, INCVIT_ERR_ARG, "rope out of range");
+    a.tokens = sh.N;
+    a.n_grids = a.merge = 1;
+    a.grid[0] = RopeGrid{1, cfg->img_h / cfg->patch, cfg->img_w / cfg->patch, 0, 0, 0, 0};
+    a.table = reinterpret_cast<float*>(dst + pl.rope);
+    e = launch_rope(a, s);
+  }
   if (e != hipSuccess) return fail(nullptr, INCVIT_ERR_HIP, std::string("pack: ") + hipGetErrorString(e));
   return INCVIT_OK;
 }

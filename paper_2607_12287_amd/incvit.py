@@ -25,7 +25,7 @@ INCVIT_F32, INCVIT_BF16, INCVIT_I8 = 0, 1, 2
 INCVIT_SCORE_EMBED, INCVIT_SCORE_KEY = 0, 1
 SCORES = {"embed": INCVIT_SCORE_EMBED, "key": INCVIT_SCORE_KEY}
 KERNEL_KINDS = ("embed", "sim", "select", "commit", "qkv", "attn", "oproj", "fc1", "fc2", "res_ln1",
-                "key_ln", "key_proj", "hsum")
+                "key_ln", "key_proj", "hsum", "qk_norm", "quant")
 MLPS = {"reuse": 0, "all": 1}
 LADDERS = {"axis": 0, "head": 1}
 LAYOUTS = {"blocks": 0, "cycle": 1}
@@ -50,7 +50,8 @@ class incvit_config(ctypes.Structure):
                 ("patch", ctypes.c_int32), ("dim", ctypes.c_int32), ("depth", ctypes.c_int32),
                 ("heads", ctypes.c_int32), ("mlp_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("ln_eps", ctypes.c_float), ("max_streams", ctypes.c_int32), ("score", ctypes.c_int32),
-                ("mlp_all", ctypes.c_int32)]
+                ("mlp_all", ctypes.c_int32), ("rope", ctypes.c_int32), ("rope_theta", ctypes.c_float),
+                ("qk_norm", ctypes.c_int32), ("mlp_int8", ctypes.c_int32)]
 
 
 class incvit_tuning(ctypes.Structure):
@@ -540,12 +541,17 @@ def incvit_set_tuning(h, cols: Optional[Sequence[int]] = None, attn_qtiles: int 
 
 def make_config(shape, max_streams: int = 1, score: str = "embed", mlp: str = "reuse") -> incvit_config:
     """Config from a model shape with attributes img_h, img_w, channels, patch,
-    dim, depth, heads, mlp_dim, dtype ('f32'/'bf16'), ln_eps; score is 'embed'
-    or 'key' (what the cosine compares); mlp is 'reuse' (exact) or 'all' (every
-    row through the MLP each frame)."""
+    dim, depth, heads, mlp_dim, dtype ('f32'/'bf16'), ln_eps, and where it has
+    them rope (None, 'halves' or 'adjacent'), rope_theta, qk_norm (None, 'rms'
+    or 'layer') and mlp_int8; score is 'embed' or 'key' (what the cosine
+    compares); mlp is 'reuse' (exact) or 'all' (every row through the MLP each
+    frame)."""
+    rope = getattr(shape, "rope", None)
     return incvit_config(shape.img_h, shape.img_w, shape.channels, shape.patch, shape.dim, shape.depth,
                          shape.heads, shape.mlp_dim, INCVIT_BF16 if shape.dtype == "bf16" else INCVIT_F32,
-                         float(shape.ln_eps), int(max_streams), SCORES[score], MLPS[mlp])
+                         float(shape.ln_eps), int(max_streams), SCORES[score], MLPS[mlp],
+                         0 if rope is None else 1 + PAIRINGS[rope], float(getattr(shape, "rope_theta", 0.0)),
+                         NORMS[getattr(shape, "qk_norm", None)], int(getattr(shape, "mlp_int8", False)))
 
 
 class Encoder:

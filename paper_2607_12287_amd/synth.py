@@ -42,6 +42,11 @@ class ModelShape:
     mlp_dim: int
     dtype: str  # "f32" or "bf16": storage of weights, caches and activations
     ln_eps: float = 1e-6
+    # options of encoders beyond the paper's (defaults: none of them)
+    rope: Optional[str] = None      # "halves" or "adjacent": queries and keys rotated by row and column
+    rope_theta: float = 10000.0
+    qk_norm: Optional[str] = None   # "rms" or "layer": norm of every query and key head
+    mlp_int8: bool = False          # the MLP's products in 8-bit integers
 
     @property
     def grid_h(self) -> int:
@@ -79,7 +84,8 @@ LAYER_PARAMS = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o",
 
 
 def param_shapes(m: ModelShape) -> List[tuple]:
-    """Canonical parameter list: (name, shape) in storage order.
+    """Canonical parameter list: (name, shape) in storage order.  With qk_norm the
+    gains (and shifts) of the query and key heads follow b_qkv.
 
     Matrices are stored [in][out] (y = x @ W).  W_pe rows are indexed by the
     patch feature (c*p + dy)*p + dx.  W_qkv columns [0,D) are Q, [D,2D) K,
@@ -90,9 +96,12 @@ def param_shapes(m: ModelShape) -> List[tuple]:
     per = {"ln1_g": (D,), "ln1_b": (D,), "w_qkv": (D, 3 * D), "b_qkv": (3 * D,),
            "w_o": (D, D), "b_o": (D,), "ln2_g": (D,), "ln2_b": (D,),
            "w_1": (D, F), "b_1": (F,), "w_2": (F, D), "b_2": (D,)}
+    heads = {None: (), "rms": ("qn_g", "kn_g"), "layer": ("qn_g", "qn_b", "kn_g", "kn_b")}[m.qk_norm]
     for l in range(m.depth):
         for name in LAYER_PARAMS:
             out.append((f"l{l}.{name}", per[name]))
+            if name == "b_qkv":
+                out += [(f"l{l}.{n}", (m.head_dim,)) for n in heads]
     out += [("lnf_g", (D,)), ("lnf_b", (D,))]
     return out
 
@@ -339,9 +348,10 @@ RHO_SWEEP = (0.02, 0.05, 0.10, 0.25, 0.50, 1.00)
 
 
 def small_model(dim: int = 64, depth: int = 2, heads: int = 2, mlp: int = 96, img: int = 32,
-                patch: int = 8, channels: int = 3, dtype: str = "f32") -> ModelShape:
-    """A small model for tests that must run in seconds on a CPU."""
-    return ModelShape(img, img, channels, patch, dim, depth, heads, mlp, dtype)
+                patch: int = 8, channels: int = 3, dtype: str = "f32", **options) -> ModelShape:
+    """A small model for tests that must run in seconds on a CPU; options: rope,
+    rope_theta, qk_norm, mlp_int8."""
+    return ModelShape(img, img, channels, patch, dim, depth, heads, mlp, dtype, **options)
 
 
 def random_patches(m: ModelShape, seed: int, views: int = 1) -> np.ndarray:

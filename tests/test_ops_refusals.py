@@ -165,3 +165,26 @@ def test_qlinear_product_refusals():
     assert one(1, 5, 64, 16, A, 64, B, 0, 0, 0, T, 16, X + 16) == ARG
     assert one(1, 5, 64, 16, A, -1, B, 0, 0, 0, T, 16, X) == ARG
     assert two(1, 0, 64, 16, 0, 0, 0, 0, 0, 0, 0) == OK and one(1, 0, 64, 16, 0, 0, 0, 0, 0, 0, 0, 0, 0) == OK
+
+
+@pytest.mark.parametrize("kw,status", [(dict(rope=3, rope_theta=10.0), ARG), (dict(rope=-1), ARG), (dict(rope=1), ARG),
+                                       (dict(rope=1, rope_theta=math.nan), ARG), (dict(rope=2, rope_theta=0.5), ARG),
+                                       (dict(qk_norm=3), ARG), (dict(mlp_int8=2), ARG), (dict(mlp_int8=1, mlp_dim=65537), UNSUPPORTED)])
+def test_encoder_options_out_of_range(kw, status):
+    from paper_2607_12287_amd import synth
+    cfg = incvit.make_config(synth.small_model(dtype="bf16"), 1)
+    cfg.rope_theta = 0.0
+    for k, v in kw.items():
+        setattr(cfg, k, v)
+    assert incvit.incvit_canonical_weights_bytes(cfg) == 0
+    assert incvit.incvit_pack_weights(cfg, 256, 256, 0) == status
+
+
+def test_encoder_options_in_the_sizes():
+    from paper_2607_12287_amd import synth
+    for o in (dict(), dict(rope="halves"), dict(qk_norm="rms"), dict(qk_norm="layer", mlp_int8=True)):
+        m = synth.small_model(dtype="bf16", **o)
+        assert incvit.incvit_canonical_weights_bytes(incvit.make_config(m, 1)) == 2 * synth.canonical_weight_count(m)
+    m, q = synth.SO400M, synth.ModelShape(**{**synth.SO400M.__dict__, "mlp_int8": True})
+    f = incvit.incvit_packed_weights_bytes
+    assert f(incvit.make_config(q, 1)) < 0.7 * f(incvit.make_config(m, 1))
