@@ -266,102 +266,6 @@ def make_rope(head_dim: int, pairs: Sequence[int], theta: float = 10000.0, ladde
                        (ctypes.c_double * 3)(*(scale or (1.0,) * n)))
 
 
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
-
-
-def _on(t, f, *args):
-    """f(*args, stream) with t's device current and on its current stream."""
-    import torch
-    if t.device.index == torch.cuda.current_device():
-        return f(*args, torch.cuda.current_stream().cuda_stream)
-    with torch.cuda.device(t.device):
-        return f(*args, torch.cuda.current_stream().cuda_stream)
-
-
-def rope_table(rope: incvit_rope, positions=None, grids=None, merge: int = 1, out=None, device=None):
-    """[tokens][pairs][2] fp32 cosines and sines.  positions: device int32
-    [axes][tokens], any strides; or grids: (t, h, w[, t0[, y0[, x0]]]) on the host, whose tokens
-    follow one another (frame by frame, in merge x merge windows)."""
-    import torch
-    _need((positions is None) != (grids is None), "either positions or grids")
-    n = sum(rope.pairs[a] for a in range(rope.axes))
-    if positions is not None:
-        _need(positions.is_cuda and positions.dtype == torch.int32 and positions.dim() == 2 and
-              positions.shape[0] == rope.axes, "positions: device int32 [axes][tokens]")
-        tokens, device = positions.shape[1], positions.device
-    else:
-        arr = (incvit_grid * len(grids))(*grids)
-        tokens = sum(g.t * g.h * g.w for g in arr)
-        device = out.device if out is not None else device or torch.device("cuda", torch.cuda.current_device())
-    if out is None:
-        out = torch.empty((max(tokens, 0), n, 2), dtype=torch.float32, device=device)
-    _need(out.is_cuda and out.device == torch.device(device) and out.dtype == torch.float32 and out.is_contiguous() and
-          out.numel() == tokens * n * 2, "out: device fp32 [tokens][pairs][2]")
-    if positions is not None:
-        _check(_on(out, incvit_rope_table, rope, tokens, positions.data_ptr(), positions.stride(0),
-                   positions.stride(1), out.data_ptr()))
-    else:
-        _check(_on(out, incvit_rope_table_grids, rope, arr, merge, out.data_ptr()))
-    return out
-
-
-def _heads(x, out, gamma, beta, head_dim: int, who: str) -> incvit_heads:
-    for t, n in ((gamma, "gamma"), (beta, "beta")):
-        _need(t is None or (t.device == x.device and t.dtype == x.dtype and t.is_contiguous() and t.numel() == head_dim),
-              f"{who}_{n}: [head_dim] of the rows' type and device")
-    _need(out.dtype == x.dtype and out.device == x.device and out.dim() == 3 and out.shape[1:] == x.shape[1:],
-          f"{who}_out: rows of the same heads, type and device")
-    s, o = x.stride(), out.stride()
-    _need(s[2] == 1 and o[2] == 1, f"{who}: the values of a head lie one after another")
-    return incvit_heads(x.data_ptr(), out.data_ptr(), gamma.data_ptr() if gamma is not None else None,
-                        beta.data_ptr() if beta is not None else None, s[0], s[1], o[0], o[1], x.shape[1])
-
-
-def qk_norm_rope(q=None, k=None, table=None, pairing: str = "halves", norm: Optional[str] = "rms", q_gamma=None, k_gamma=None,
-                 q_beta=None, k_beta=None, eps: float = 1e-6, index=None, k_rows=None, q_out=None, k_out=None):
-    """Norm of every head of q [rows][q heads][d] and k [rows][k heads][d] (views
-    with any row and head strides; either may be None), then the rotation by the
-    table rows `index` (device int32 [rows]; without it row r % table rows) of
-    `table` (rope_table's; None: no rotation).  k_rows (device int32 [rows]): the
-    rows of k_out (a cache [..][k heads][d], then required) that the new keys go
-    to.  q_out, k_out may be q and k (in place).  Returns (q_out, k_out)."""
-    import torch
-    x = q if q is not None else k
-    _need(x is not None, "q or k")
-    rows, d = x.shape[0], x.shape[-1]
-    _need(x.is_cuda and x.dtype in (torch.float32, torch.bfloat16), "rows: device tensors, fp32 or bf16")
-    for t in (q, k):
-        _need(t is None or (t.dim() == 3 and t.shape[0] == rows and t.shape[2] == d and t.dtype == x.dtype and
-                            t.device == x.device), "q and k: [rows][heads][d] of one type on one device")
-    rot = 0
-    if table is not None:
-        _need(table.device == x.device and table.dtype == torch.float32 and table.is_contiguous() and table.dim() == 3 and
-              table.shape[2] == 2, "table: device fp32 [rows][pairs][2]")
-        rot = 2 * table.shape[1]
-    for t, n in ((index, "index"), (k_rows, "k_rows")):
-        _need(t is None or (t.device == x.device and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == rows),
-              f"{n}: device int32 [rows]")
-    _need(k_rows is None or (k is not None and k_out is not None), "k_rows: rows of k_out, which has to be given")
-    hq = hk = None
-    if q is not None:
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _need(q_out.shape[0] == rows, "q_out: as many rows as q")
-        hq = _heads(q, q_out, q_gamma if norm else None, q_beta, d, "q")
-    if k is not None:
-        if k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        _need(k_rows is not None or k_out.shape[0] == rows, "k_out: as many rows as k")
-        hk = _heads(k, k_out, k_gamma if norm else None, k_beta, d, "k")
-    c = incvit_qk(INCVIT_BF16 if x.dtype == torch.bfloat16 else INCVIT_F32, d, rot, PAIRINGS[pairing], NORMS[norm], eps)
-    _check(_on(x, incvit_qk_norm_rope, c, rows, hq, hk, table.data_ptr() if rot else None, table.shape[0] if rot else 0,
-               index.data_ptr() if index is not None else None, k_rows.data_ptr() if k_rows is not None else None,
-               k_out.shape[0] if k_rows is not None else 0))
-    return q_out, k_out
-
-
 def incvit_qlinear_weights_bytes(K: int, N: int) -> int:
     return lib().incvit_qlinear_weights_bytes(K, N)
 
@@ -390,91 +294,6 @@ def incvit_qlinear(dtype: int, rows: int, K: int, N: int, x: int, x_stride: int,
                    res_stride: int, out: int, out_stride: int, workspace: int, stream: int = 0) -> int:
     return lib().incvit_qlinear(dtype, rows, K, N, x, x_stride, weights, gelu, residual, res_stride, out, out_stride,
                                 workspace, stream)
-
-
-def _dtype_of(t) -> int:
-    import torch
-    code = {torch.float32: INCVIT_F32, torch.bfloat16: INCVIT_BF16, torch.int8: INCVIT_I8}.get(t.dtype)
-    _need(code is not None and t.is_cuda, "device tensors, fp32 or bf16")
-    return code
-
-
-class QRows:
-    """Rows quantised to 8 bits (quantize_rows), for any number of products."""
-
-    def __init__(self, rows: int, K: int, dtype, buf):
-        self.rows, self.K, self.dtype, self.buf = rows, K, dtype, buf
-
-
-def quantize_rows(x, gamma=None, beta=None, eps: float = 1e-6) -> QRows:
-    """The rows of x [rows][K] in 8-bit integers with a scale each; with gamma
-    (and beta), [K] of x's type, after a LayerNorm."""
-    import torch
-    code = _dtype_of(x)
-    _need(code != INCVIT_I8 and x.dim() == 2 and x.stride(1) == 1, "x: fp32 or bf16 [rows][K], the values of a row one after another")
-    for t, n in ((gamma, "gamma"), (beta, "beta")):
-        _need(t is None or (t.device == x.device and t.dtype == x.dtype and t.is_contiguous() and t.numel() == x.shape[1]),
-              f"{n}: [K] of x's type and device")
-    rows, K = x.shape
-    buf = torch.empty(incvit_qlinear_rows_bytes(rows, K), dtype=torch.uint8, device=x.device)
-    _check(_on(x, incvit_qlinear_quantize_rows, code, rows, K, x.data_ptr(), x.stride(0),
-               gamma.data_ptr() if gamma is not None else None, beta.data_ptr() if beta is not None else None, eps,
-               buf.data_ptr()))
-    return QRows(rows, K, x.dtype, buf)
-
-
-class QLinear:
-    """y = x W + b in 8-bit integers: W [K][N] (any strides: pass linear.weight.t()
-    for one stored [N][K]) is quantised and packed once.  W fp32 or bf16, bias [N]
-    of its type; or W int8 with `scales` (fp32 [N]) and an fp32 bias."""
-
-    def __init__(self, weight, bias=None, scales=None):
-        import torch
-        code = _dtype_of(weight)
-        _need(weight.dim() == 2, "weight: [K][N]")
-        self.K, self.N = weight.shape
-        _need((code == INCVIT_I8) == (scales is not None), "scales: with int8 weights, and only with them")
-        for t, n, dt in ((bias, "bias", torch.float32 if code == INCVIT_I8 else weight.dtype), (scales, "scales", torch.float32)):
-            _need(t is None or (t.device == weight.device and t.dtype == dt and t.is_contiguous() and t.numel() == self.N),
-                  f"{n}: {dt} [N] on the weights' device")
-        n = incvit_qlinear_weights_bytes(self.K, self.N)
-        if n == 0:
-            raise IncvitError(INCVIT_ERR_UNSUPPORTED, f"a product of K = {self.K}, N = {self.N}")
-        self.device = weight.device
-        self.weights = torch.empty(n, dtype=torch.uint8, device=self.device)
-        _check(_on(weight, incvit_qlinear_pack_weights, code, self.K, self.N, weight.data_ptr(), weight.stride(0),
-                   weight.stride(1), scales.data_ptr() if scales is not None else None,
-                   bias.data_ptr() if bias is not None else None, self.weights.data_ptr()))
-
-    def __call__(self, x, gelu: bool = False, residual=None, out=None):
-        """act(x W + b) + residual for x [rows][K] (fp32 or bf16, the values of a row
-        one after another) or QRows; residual and out [rows][N] of x's type (out may
-        be residual).  Returns out."""
-        import torch
-        q = isinstance(x, QRows)
-        if q:
-            rows, K, src = x.rows, x.K, x.buf
-            code = INCVIT_BF16 if x.dtype == torch.bfloat16 else INCVIT_F32
-        else:
-            code, src = _dtype_of(x), x
-            _need(code != INCVIT_I8 and x.dim() == 2 and x.stride(1) == 1,
-                  "x: fp32 or bf16 [rows][K], the values of a row one after another")
-            rows, K = x.shape
-        _need(K == self.K and src.device == self.device, "x: rows of K values on the weights' device")
-        if out is None:
-            out = torch.empty((rows, self.N), dtype=x.dtype, device=self.device)
-        for t, n in ((out, "out"), (residual, "residual")):
-            _need(t is None or (t.dtype == x.dtype and t.device == self.device and t.shape == (rows, self.N) and
-                                (t.stride(1) == 1 or self.N == 1)), f"{n}: [rows][N] of x's type, the values of a row one after another")
-        r, rs = (residual.data_ptr(), residual.stride(0)) if residual is not None else (None, 0)
-        if q:
-            _check(_on(src, incvit_qlinear_multiply, code, rows, K, self.N, src.data_ptr(), self.weights.data_ptr(), int(gelu),
-                       r, rs, out.data_ptr(), out.stride(0)))
-        else:
-            ws = torch.empty(incvit_qlinear_rows_bytes(rows, K), dtype=torch.uint8, device=self.device)
-            _check(_on(src, incvit_qlinear, code, rows, K, self.N, x.data_ptr(), x.stride(0), self.weights.data_ptr(), int(gelu),
-                       r, rs, out.data_ptr(), out.stride(0), ws.data_ptr()))
-        return out
 
 
 def incvit_cache_export(h, cache: int, dst: int, stream: int = 0) -> int:
@@ -535,6 +354,20 @@ def incvit_set_tuning(h, cols: Optional[Sequence[int]] = None, attn_qtiles: int 
     t = incvit_tuning((ctypes.c_int32 * 4)(*[int(k) for k in (cols or (0, 0, 0, 0))]), int(attn_qtiles),
                       int(row_groups), int(attn_waves), int(fc2_mode), int(tiled))
     return lib().incvit_set_tuning(h, ctypes.byref(t))
+
+
+# --- operators on torch tensors ------------------------------------------------
+
+# They live in ops.py, which needs torch to be imported; this module does not.
+_OPS = ("rope_table", "qk_norm_rope", "quantize_rows", "QRows", "QLinear")
+
+
+def __getattr__(name: str):
+    if name in _OPS:
+        from . import ops
+        globals().update({n: getattr(ops, n) for n in _OPS})
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 # --- convenience wrapper -------------------------------------------------------

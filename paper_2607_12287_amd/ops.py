@@ -1,0 +1,232 @@
+"""The library's stand-alone operators on torch tensors (reached as attributes of
+:mod:`paper_2607_12287_amd.incvit`).  Argument checks and memory only: a call is
+one or two kernels of a few microseconds, so the checks build nothing that they do
+not need.  Work goes to the current stream of the tensors' device.
+"""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import incvit as _c
+
+_BF16, _F32 = torch.bfloat16, torch.float32
+_CODES = {_F32: _c.INCVIT_F32, _BF16: _c.INCVIT_BF16, torch.int8: _c.INCVIT_I8}
+_stream_of = torch._C._cuda_getCurrentRawStream
+_current = torch._C._cuda_getDevice
+
+
+def _call(f, device, *args):
+    """f(*args, stream) with `device` current, on its current stream."""
+    i = device.index
+    if i == _current():
+        st = f(*args, _stream_of(i))
+    else:
+        with torch.cuda.device(device):
+            st = f(*args, _stream_of(i))
+    if st:
+        _c._check(st)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+# ------------------------------------------------------- rotary positions --
+
+
+def rope_table(rope: _c.incvit_rope, positions=None, grids=None, merge: int = 1, out=None, device=None):
+    """[tokens][pairs][2] fp32 cosines and sines.  positions: device int32
+    [axes][tokens], any strides; or grids: (t, h, w[, t0[, y0[, x0]]]) on the host,
+    whose tokens follow one another (frame by frame, in merge x merge windows)."""
+    n = sum(rope.pairs[:rope.axes])
+    if (positions is None) == (grids is None):
+        raise ValueError("either positions or grids")
+    if positions is not None:
+        if not (positions.is_cuda and positions.dtype == torch.int32 and positions.dim() == 2 and positions.shape[0] == rope.axes):
+            raise ValueError("positions: device int32 [axes][tokens]")
+        tokens, device = positions.shape[1], positions.device
+    else:
+        arr = (_c.incvit_grid * len(grids))(*grids)
+        tokens = 0
+        for g in grids:
+            tokens += g[0] * g[1] * g[2]
+        if device is None:
+            device = out.device if out is not None else torch.device("cuda", _current())
+        elif not isinstance(device, torch.device) or device.index is None:
+            device = torch.empty(0, device=device).device
+    if out is None:
+        out = torch.empty((max(tokens, 0), n, 2), dtype=_F32, device=device)
+    elif not (out.device == device and out.is_cuda and out.dtype == _F32 and out.is_contiguous() and out.numel() == tokens * n * 2):
+        raise ValueError("out: device fp32 [tokens][pairs][2]")
+    if positions is not None:
+        _call(_c.lib().incvit_rope_table, device, _c.ctypes.byref(rope), tokens, positions.data_ptr(), *positions.stride(),
+              out.data_ptr())
+    else:
+        _call(_c.lib().incvit_rope_table_grids, device, _c.ctypes.byref(rope), len(arr), arr, merge, out.data_ptr())
+    return out
+
+
+# ------------------------------------------- head norms with the rotation --
+
+
+def _heads(x, out, gamma, beta, who: str) -> _c.incvit_heads:
+    for t in (gamma, beta):
+        if t is not None and not (t.dtype == x.dtype and t.device == x.device and t.is_contiguous() and t.numel() == x.shape[2]):
+            raise ValueError(f"{who}_gamma, {who}_beta: [head_dim] of the rows' type and device")
+    s, o = x.stride(), out.stride()
+    if not (out.dtype == x.dtype and out.device == x.device and out.dim() == 3 and out.shape[1:] == x.shape[1:]):
+        raise ValueError(f"{who}_out: rows of the same heads, type and device")
+    if s[2] != 1 or o[2] != 1:
+        raise ValueError(f"{who}, {who}_out: the values of a head lie one after another")
+    return _c.incvit_heads(x.data_ptr(), out.data_ptr(), _ptr(gamma), _ptr(beta), s[0], s[1], o[0], o[1], x.shape[1])
+
+
+def qk_norm_rope(q=None, k=None, table=None, pairing: str = "halves", norm: Optional[str] = "rms", q_gamma=None, k_gamma=None,
+                 q_beta=None, k_beta=None, eps: float = 1e-6, index=None, k_rows=None, q_out=None, k_out=None):
+    """Norm of every head of q [rows][q heads][d] and k [rows][k heads][d] (views
+    with any row and head strides; either may be None), then the rotation by the
+    table rows `index` (device int32 [rows]; without it row r % table rows) of
+    `table` (rope_table's; None: no rotation).  k_rows (device int32 [rows]): the
+    rows of k_out (a cache [..][k heads][d], then required) that the new keys go
+    to.  q_out, k_out may be q and k (in place).  Returns (q_out, k_out)."""
+    x = q if q is not None else k
+    if x is None:
+        raise ValueError("q or k")
+    dt, dev = x.dtype, x.device
+    if not (x.is_cuda and x.dim() == 3 and (dt == _BF16 or dt == _F32)):
+        raise ValueError("q, k: device tensors [rows][heads][d], fp32 or bf16")
+    rows, _, d = x.shape
+    if q is not None and k is not None and not (k.dim() == 3 and k.shape[0] == rows and k.shape[2] == d and k.dtype == dt and
+                                                k.device == dev):
+        raise ValueError("q and k: [rows][heads][d] of one type on one device")
+    rot = trows = 0
+    if table is not None:
+        if not (table.device == dev and table.dtype == _F32 and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous()):
+            raise ValueError("table: device fp32 [rows][pairs][2]")
+        trows, rot = table.shape[0], 2 * table.shape[1]
+    for t in (index, k_rows):
+        if t is not None and not (t.dtype == torch.int32 and t.device == dev and t.is_contiguous() and t.numel() == rows):
+            raise ValueError("index, k_rows: device int32 [rows]")
+    if not norm:
+        q_gamma = k_gamma = None
+    hq = hk = None
+    k_out_rows = 0
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        elif q_out.shape[0] != rows:
+            raise ValueError("q_out: as many rows as q")
+        hq = _c.ctypes.byref(_heads(q, q_out, q_gamma, q_beta, "q"))
+    if k is not None:
+        if k_rows is not None:
+            if k_out is None:
+                raise ValueError("k_rows: rows of k_out, which has to be given")
+            k_out_rows = k_out.shape[0]
+        elif k_out is None:
+            k_out = torch.empty(k.shape, dtype=dt, device=dev)
+        elif k_out.shape[0] != rows:
+            raise ValueError("k_out: as many rows as k")
+        hk = _c.ctypes.byref(_heads(k, k_out, k_gamma, k_beta, "k"))
+    elif k_rows is not None:
+        raise ValueError("k_rows: rows of k_out, without k")
+    c = _c.incvit_qk(_CODES[dt], d, rot, _c.PAIRINGS[pairing], _c.NORMS[norm], eps)
+    _call(_c.lib().incvit_qk_norm_rope, dev, _c.ctypes.byref(c), rows, hq, hk, _ptr(table), trows, _ptr(index), _ptr(k_rows),
+          k_out_rows)
+    return q_out, k_out
+
+
+# ----------------------------------------------------------- 8-bit products --
+
+
+def _rows_of(x):
+    """(type code, rows, K) of rows that the 8-bit operators take."""
+    code = _CODES.get(x.dtype, _c.INCVIT_I8)
+    if not (x.is_cuda and code != _c.INCVIT_I8 and x.dim() == 2 and (x.stride(1) == 1 or x.shape[1] == 1)):
+        raise ValueError("x: device fp32 or bf16 [rows][K], the values of a row one after another")
+    return code, x.shape[0], x.shape[1]
+
+
+def _buffer(n: int, device):
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+class QRows:
+    """Rows quantised to 8 bits (quantize_rows), for any number of products."""
+
+    def __init__(self, rows: int, K: int, dtype, buf):
+        self.rows, self.K, self.dtype, self.buf = rows, K, dtype, buf
+
+
+def quantize_rows(x, gamma=None, beta=None, eps: float = 1e-6) -> QRows:
+    """The rows of x [rows][K] in 8-bit integers with a scale each; with gamma
+    (and beta), [K] of x's type, after a LayerNorm."""
+    code, rows, K = _rows_of(x)
+    for t in (gamma, beta):
+        if t is not None and not (t.device == x.device and t.dtype == x.dtype and t.is_contiguous() and t.numel() == K):
+            raise ValueError("gamma, beta: [K] of x's type and device")
+    L = _c.lib()
+    buf = _buffer(L.incvit_qlinear_rows_bytes(rows, K), x.device)
+    _call(L.incvit_qlinear_quantize_rows, x.device, code, rows, K, x.data_ptr(), x.stride(0), _ptr(gamma), _ptr(beta), eps,
+          buf.data_ptr())
+    return QRows(rows, K, x.dtype, buf)
+
+
+class QLinear:
+    """y = x W + b in 8-bit integers: W [K][N] (any strides: pass linear.weight.t()
+    for one stored [N][K]) is quantised and packed once.  W fp32 or bf16, bias [N]
+    of its type; or W int8 with `scales` (fp32 [N]) and an fp32 bias."""
+
+    def __init__(self, weight, bias=None, scales=None):
+        code = _CODES.get(weight.dtype)
+        if code is None or not weight.is_cuda or weight.dim() != 2:
+            raise ValueError("weight: device [K][N], fp32, bf16 or int8")
+        self.K, self.N = weight.shape
+        self.device = weight.device
+        if (code == _c.INCVIT_I8) != (scales is not None):
+            raise ValueError("scales: with int8 weights, and only with them")
+        for t, dt in ((bias, _F32 if code == _c.INCVIT_I8 else weight.dtype), (scales, _F32)):
+            if t is not None and not (t.device == self.device and t.dtype == dt and t.is_contiguous() and t.numel() == self.N):
+                raise ValueError("bias: [N] of the weights' type (fp32 with int8 weights); scales: fp32 [N]; on the weights' device")
+        L = _c.lib()
+        n = L.incvit_qlinear_weights_bytes(self.K, self.N)
+        if n == 0:
+            raise _c.IncvitError(_c.INCVIT_ERR_UNSUPPORTED, f"a product of K = {self.K}, N = {self.N}")
+        self.weights = _buffer(n, self.device)
+        _call(L.incvit_qlinear_pack_weights, self.device, code, self.K, self.N, weight.data_ptr(), *weight.stride(), _ptr(scales),
+              _ptr(bias), self.weights.data_ptr())
+
+    def __call__(self, x, gelu: bool = False, residual=None, out=None):
+        """act(x W + b) + residual for x [rows][K] (fp32 or bf16, the values of a row
+        one after another) or QRows; residual and out [rows][N] of x's type (out may
+        be residual).  Returns out."""
+        q = isinstance(x, QRows)
+        if q:
+            code, rows, K, dev = _CODES[x.dtype], x.rows, x.K, x.buf.device
+        else:
+            code, rows, K = _rows_of(x)
+            dev = x.device
+        if K != self.K or dev != self.device:
+            raise ValueError("x: rows of K values on the weights' device")
+        N, dt = self.N, x.dtype
+        if out is None:
+            out = torch.empty((rows, N), dtype=dt, device=dev)
+        elif not (out.dtype == dt and out.device == dev and out.shape == (rows, N) and (out.stride(1) == 1 or N == 1)):
+            raise ValueError("out: [rows][N] of x's type, the values of a row one after another")
+        r = None
+        rs = 0
+        if residual is not None:
+            if not (residual.dtype == dt and residual.device == dev and residual.shape == (rows, N) and
+                    (residual.stride(1) == 1 or N == 1)):
+                raise ValueError("residual: [rows][N] of x's type, the values of a row one after another")
+            r, rs = residual.data_ptr(), residual.stride(0)
+        L = _c.lib()
+        if q:
+            _call(L.incvit_qlinear_multiply, dev, code, rows, K, N, x.buf.data_ptr(), self.weights.data_ptr(), bool(gelu), r, rs,
+                  out.data_ptr(), out.stride(0))
+        else:
+            ws = _buffer(L.incvit_qlinear_rows_bytes(rows, K), dev)
+            _call(L.incvit_qlinear, dev, code, rows, K, N, x.data_ptr(), x.stride(0), self.weights.data_ptr(), bool(gelu), r, rs,
+                  out.data_ptr(), out.stride(0), ws.data_ptr())
+        return out
