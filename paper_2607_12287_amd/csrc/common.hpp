@@ -170,7 +170,8 @@ struct RowsArgs {  // commit: ref/X0/Z0 of the refreshed rows, row map
 };
 
 enum Epi { EPI_QKV = 0, EPI_FC1 = 1, EPI_PART = 2, EPI_RES = 3, EPI_ATT = 4, EPI_DOWN = 5,
-           EPI_QBF = 6, EPI_QF32 = 7 };  // 8-bit products, bf16 or fp32 output
+           // 8-bit products, bf16 or fp32 output: 16 bytes at once, or any strides and width
+           EPI_QBF = 6, EPI_QF32 = 7, EPI_QBF_ANY = 8, EPI_QF32_ANY = 9 };
 
 // Fields in the order the kernel's prologue needs them, so that its argument
 // loads go out together.
@@ -200,7 +201,6 @@ struct GemmArgs {
   int m_host;              // rows, where meta is null
   int n;                   // output columns (Nout: rounded up to 16)
   int gelu;
-  int wide;                // out and resid take 4 columns at once (strides, addresses and n)
 };
 
 // Row kernel that finishes the split-K MLP down projection, one workgroup per

@@ -89,8 +89,14 @@ __host__ __device__ constexpr bool ln_on_load() {
 }
 template <int EPI>
 __host__ __device__ constexpr bool is_q8() {
+  return EPI == EPI_QBF || EPI == EPI_QF32 || EPI == EPI_QBF_ANY || EPI == EPI_QF32_ANY;
+}
+template <int EPI>
+__host__ __device__ constexpr bool q8_wide() {
   return EPI == EPI_QBF || EPI == EPI_QF32;
 }
+template <int EPI>
+using q8_out = std::conditional_t<EPI == EPI_QBF || EPI == EPI_QBF_ANY, uint16_t, float>;
 template <int EPI>
 __host__ __device__ constexpr int gemm_waves() {
   return kGemmWaves;
@@ -159,42 +165,75 @@ __device__ __forceinline__ void mma_q8(i32x4_t& acc, u32x4_t a, u32x4_t b) {
   acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), acc, 0, 0, 0);
 }
 
-// Columns col .. col + 3 (col % 4 == 0) of a row of an 8-bit product, row < M:
-// sum * (row scale * column scale) + bias, GELU, residual, all in fp32 with one
-// rounding at the end.  The last column block may end inside the four.
-template <class T>
-__device__ __forceinline__ void q8_store(const GemmArgs& a, int row, int col, const i32x4_t& acc, float rs, const float4& cs,
-                                         const float4& cb) {
-  const float sc[4] = {cs.x, cs.y, cs.z, cs.w}, bi[4] = {cb.x, cb.y, cb.z, cb.w};
-  float y[4];
+// Two 16x16 tiles of neighbouring column blocks, whose lane (g, n) holds columns
+// 4g .. 4g + 3 of row n of each, to columns 8g .. 8g + 7 of the 32: the lanes of
+// one row exchange their values by gfx950's half and row swaps.
+__device__ __forceinline__ void join_blocks(i32x4_t& x, i32x4_t& y) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    y[j] = fmaf((float)acc[j], rs * sc[j], bi[j]);
-    if (a.gelu) y[j] = gelu_tanh(y[j]);  // uniform
+  for (int i = 0; i < 4; ++i) {
+    const auto h = __builtin_amdgcn_permlane32_swap((uint32_t)x[i], (uint32_t)y[i], false, false);
+    const auto r = __builtin_amdgcn_permlane16_swap(h[0], h[1], false, false);
+    x[i] = (int)r[0];
+    y[i] = (int)r[1];
+  }
+}
+
+// NC consecutive columns from col on (multiples of NC) of a row of an 8-bit
+// product: sum * (row scale * column scale) + bias, GELU and residual, all in
+// fp32 with one rounding at the end.  With WIDE a run is inside the output or
+// outside it as a whole and takes 16 bytes (8 of bf16 with NC = 4) at once, and
+// its residual `res` has been loaded; else each column is looked at.
+template <class T, int NC>
+struct ResRun {
+  uint32_t w[NC * sizeof(T) / 4];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (sizeof(w) == 8) *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(p);
+    else *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(p);
+  }
+  __device__ __forceinline__ float get(int j) const {
+    if constexpr (std::is_same<T, float>::value) return __uint_as_float(w[j]);
+    else return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+  }
+  __device__ __forceinline__ void store(T* p, const float* y) {
+    if constexpr (std::is_same<T, float>::value) {
+      *reinterpret_cast<float4*>(p) = make_float4(y[0], y[1], y[2], y[3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NC / 2; ++j) w[j] = f2bf2(y[2 * j], y[2 * j + 1]);
+      if constexpr (sizeof(w) == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+      else *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+};
+template <class T, int NC, bool WIDE>
+__device__ __forceinline__ void q8_store(const GemmArgs& a, int row, int col, bool ok, const i32x4_t* acc, float rs,
+                                         const float4* cs, const float4* cb, const ResRun<T, NC>& res) {
+  float y[NC];
+#pragma unroll
+  for (int q = 0; q < NC / 4; ++q) {
+    const float sc[4] = {cs[q].x, cs[q].y, cs[q].z, cs[q].w}, bi[4] = {cb[q].x, cb[q].y, cb[q].z, cb[q].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[4 * q + j] = fmaf((float)acc[q][j], rs * sc[j], bi[j]);
+  }
+  if (a.gelu) {  // uniform
+#pragma unroll
+    for (int j = 0; j < NC; ++j) y[j] = gelu_tanh(y[j]);
   }
   T* out = static_cast<T*>(a.out) + (size_t)row * a.out_ld + col;
-  const T* res = a.resid ? static_cast<const T*>(a.resid) + (size_t)row * a.res_ld + col : nullptr;
-  if (a.wide) {  // uniform: four columns at once, all or none of them below n
-    if (col >= a.n) return;
-    if constexpr (std::is_same<T, float>::value) {
-      if (res) {
-        const float4 v = *reinterpret_cast<const float4*>(res);
-        y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
-      }
-      *reinterpret_cast<float4*>(out) = make_float4(y[0], y[1], y[2], y[3]);
-    } else {
-      if (res) {
-        const uint2 v = *reinterpret_cast<const uint2*>(res);
-        y[0] += __uint_as_float(v.x << 16); y[1] += __uint_as_float(v.x & 0xffff0000u);
-        y[2] += __uint_as_float(v.y << 16); y[3] += __uint_as_float(v.y & 0xffff0000u);
-      }
-      *reinterpret_cast<uint2*>(out) = make_uint2(f2bf2(y[0], y[1]), f2bf2(y[2], y[3]));
-    }
-    return;
-  }
+  if constexpr (WIDE) {
+    if (a.resid) {  // uniform
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (col + j < a.n) out[j] = Elem<T>::cv(res ? y[j] + Elem<T>::f(res[j]) : y[j]);
+      for (int j = 0; j < NC; ++j) y[j] += res.get(j);
+    }
+    ResRun<T, NC> o;
+    if (ok) o.store(out, y);
+  } else {
+    if (!ok) return;
+    const T* rp = static_cast<const T*>(a.resid) + (size_t)row * a.res_ld + col;
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+      if (col + j < a.n) out[j] = Elem<T>::cv(a.resid ? y[j] + Elem<T>::f(rp[j]) : y[j]);
+  }
 }
 
 template <class T, int EPI, int NB, int CPW>

@@ -671,7 +671,6 @@ incvit_status run_layers(incvit_handle* h, const Views& views, int B, const WsLa
       a.out_ld = up ? sh.Fpad : sh.D;
       a.n = Nout;
       a.gelu = up;
-      a.wide = Nout % 4 == 0;
       return run(h, kernel_kind, s, [&] { return launch_q_gemm(a, !up || !sh.dtype, exp_mlp, mlp_rows, s); });
     };
 

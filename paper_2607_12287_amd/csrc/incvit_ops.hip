@@ -118,8 +118,6 @@ incvit_status q_multiply(int32_t dtype, int64_t rows, int32_t K, int32_t N, cons
   a.gelu = gelu;
   a.out_ld = (long)out_stride;
   a.res_ld = (long)res_stride;
-  const uintptr_t bits = (uintptr_t)out | (uintptr_t)residual | (uintptr_t)(out_stride * eb) | (uintptr_t)(residual ? res_stride * eb : 0);
-  a.wide = N % 4 == 0 && bits % (4 * eb) == 0;
   const int64_t slab = q_slab(K);
   for (int64_t r = 0; r < rows; r += slab) {
     const int m = (int)(rows - r < slab ? rows - r : slab);

@@ -4,8 +4,8 @@
 // for the columns of W.  Sums of 8-bit products are exact in int32 (K <= 65536).
 //
 // Three kernels:
-//   * q_rows_kernel: a wave per row finds its largest magnitude and writes the
-//     row's integers in the matrix instruction's operand order (with a
+//   * q_rows_kernel: one or four waves per row find its largest magnitude and
+//     write the row's integers in the matrix instruction's operand order (with a
 //     LayerNorm before it, whose statistics are two passes over registers);
 //   * q_gemm_kernel, few rows: weights stream past them once.  A workgroup owns
 //     16 columns; its waves take the K chunks in turn, so every wave has loads of
@@ -31,6 +31,24 @@ __device__ __forceinline__ float q_scale(uint32_t top) {
 __device__ __forceinline__ int q_value(float x, float s) {
   const float r = rintf(__fdiv_rn(x, s));
   return s > 0.0f ? (int)fminf(fmaxf(r, -127.0f), 127.0f) : 0;
+}
+// The same in the low byte of the result, without a division, for scales whose
+// reciprocal and quotients stay normal (q_plain).  inv = 1 / s, correctly
+// rounded: x * inv is within 2 ulp of the quotient, one residual step makes it
+// faithful and the second correctly rounded (Markstein's theorem: a faithful
+// quotient, its exact residual and the correctly rounded reciprocal).  Adding
+// 1.5 * 2^23 rounds to an integer, ties to even, in the low bits; |x / s| is
+// below 127.5, so no clamp.
+__device__ __forceinline__ bool q_plain(float s) { return s > 0x1p-90f && s < 0x1p90f; }
+__device__ __forceinline__ uint32_t q_byte(float x, float s, float inv) {
+  float q = x * inv;
+  q = fmaf(fmaf(-q, s, x), inv, q);
+  q = fmaf(fmaf(-q, s, x), inv, q);
+  return __float_as_uint(q + 12582912.0f);
+}
+// low bytes of four words in one
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
@@ -67,44 +85,57 @@ __device__ __forceinline__ void load8(const T* p, int k, int K, float* v) {
   }
 }
 
-// A wave per row, a workgroup per tile of 16 rows: the 16-byte pieces that its
-// waves write fill whole kilobytes, which meet in the L2.  A lane holds 8 values
-// of every 512 in registers (CH of them, K <= 512 CH); longer rows (CH = 0) are
-// read again for each pass.
-template <class T, int CH, bool VEC>
-__global__ __launch_bounds__(1024) void q_rows_kernel(QRowsArgs a) {
+// Four rows to a workgroup, WPR waves to a row.  A lane holds 8 values of every
+// 512 WPR in registers, CH times (K <= 512 WPR CH); longer rows (CH = 0) are
+// read again for each pass.  The four rows' 16-byte pieces of a chunk are 64
+// consecutive bytes.
+template <class T, int CH, int WPR, bool VEC>
+__global__ __launch_bounds__(256 * WPR) void q_rows_kernel(QRowsArgs a) {
+  __shared__ float s_sum[4][WPR], s_sq[4][WPR];
+  __shared__ uint32_t s_top[4][WPR];
   const int lane = threadIdx.x & 63;
-  const int r = __builtin_amdgcn_readfirstlane(blockIdx.x * 16 + (threadIdx.x >> 6));
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = w / WPR, wk = w % WPR;
+  const long r = (long)blockIdx.x * 4 + wr;
   const long rows = a.meta ? a.meta->m : a.rows;
-  if (r >= rows) return;  // uniform per wave
-  const int K = a.K, kc = (K + 63) / 64, n8 = kc * 8;  // runs of 8, padding included
+  if ((long)blockIdx.x * 4 >= rows) return;  // uniform
+  const bool live = r < rows;                // uniform per wave
+  const int K = a.K, kc = (K + 63) / 64;
   const T* x = static_cast<const T*>(a.x);
-  auto fetch = [&](int i, float* v) {  // the lane's i-th run
-    const int k = 8 * (lane + 64 * i);
-    if (a.frag) {  // uniform: 16-row x 32-column operand order
-      load8<T, true>(x + (k < K ? frag_off(r, k, (int)a.ld / 32) : 0) - k, k, K, v);
-    } else {
-      load8<T, VEC>(x + (size_t)r * a.ld, k, K, v);
-    }
+  auto fetch = [&](int i, float* v) {  // the lane's i-th run of 8
+    const int k = live ? 8 * (lane + 64 * (wk + WPR * i)) : K;
+    if (a.frag) load8<T, true>(x + (k < K ? frag_off((int)r, k, (int)a.ld / 32) : 0) - k, k, K, v);  // uniform
+    else load8<T, VEC>(x + (size_t)r * a.ld, k, K, v);
   };
   constexpr int NH = CH > 0 ? CH : 1;
-  const int runs = CH > 0 ? CH : (n8 + 63) / 64;
+  const int runs = CH > 0 ? CH : (kc * 8 + 64 * WPR - 1) / (64 * WPR);
   float held[NH][8];
   if constexpr (CH > 0) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) fetch(i, held[i]);
   }
-  // f(run, its first k, its 8 values) for every run of the lane
+  // f(its first k, its 8 values) for every run of the lane
   auto each = [&](auto f) {
     if constexpr (CH > 0) {
 #pragma unroll
-      for (int i = 0; i < CH; ++i) f(8 * (lane + 64 * i), held[i]);
+      for (int i = 0; i < CH; ++i) f(8 * (lane + 64 * (wk + WPR * i)), held[i]);
     } else {
       for (int i = 0; i < runs; ++i) {
         fetch(i, held[0]);
-        f(8 * (lane + 64 * i), held[0]);
+        f(8 * (lane + 64 * (wk + WPR * i)), held[0]);
       }
     }
+  };
+  // sums over the row's waves, in wave order
+  auto row_sum = [&](float v, float (&sh)[4][WPR]) {
+    v = wave_sum(v);
+    if constexpr (WPR > 1) {
+      if (lane == 0) sh[wr][wk] = v;
+      __syncthreads();
+      v = sh[wr][0];
+#pragma unroll
+      for (int i = 1; i < WPR; ++i) v += sh[wr][i];
+    }
+    return v;
   };
   float mean = 0.0f, rstd = 1.0f;
   const bool ln = a.gamma != nullptr;
@@ -114,7 +145,7 @@ __global__ __launch_bounds__(1024) void q_rows_kernel(QRowsArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) s += v[j];  // zeros past K
     });
-    mean = wave_sum(s) / (float)K;
+    mean = row_sum(s, s_sum) / (float)K;
     each([&](int k, float* v) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -122,7 +153,7 @@ __global__ __launch_bounds__(1024) void q_rows_kernel(QRowsArgs a) {
         q += k + j < K ? d * d : 0.0f;
       }
     });
-    rstd = 1.0f / sqrtf(wave_sum(q) / (float)K + a.eps);
+    rstd = 1.0f / sqrtf(row_sum(q, s_sq) / (float)K + a.eps);
   }
   auto param = [&](const void* p, int k) {
     return a.param_f32 ? static_cast<const float*>(p)[k] : Elem<T>::f(static_cast<const T*>(p)[k]);
@@ -139,24 +170,34 @@ __global__ __launch_bounds__(1024) void q_rows_kernel(QRowsArgs a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = max(top, mag(v[j]));
   });
-  const float s = q_scale(wave_max_u(top));
-  if (lane == 0) a.scale[r] = s;
+  top = wave_max_u(top);
+  if constexpr (WPR > 1) {
+    if (lane == 0) s_top[wr][wk] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WPR; ++i) top = max(top, s_top[wr][i]);
+  }
+  if (!live) return;
+  const float s = q_scale(top), inv = __fdiv_rn(1.0f, s);
+  const bool plain = q_plain(s);  // uniform per wave
+  if (lane == 0 && wk == 0) a.scale[r] = s;
   each([&](int k, float* v) {
     if constexpr (CH == 0) normed(k, v);
     if (k >= 64 * kc) return;
-    uint32_t w[2] = {0, 0};
+    uint32_t b[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j >> 2] |= (uint32_t)(q_value(v[j], s) & 0xff) << (8 * (j & 3));
-    *reinterpret_cast<uint2*>(a.dst + q_off(r, k, kc)) = make_uint2(w[0], w[1]);
+    for (int j = 0; j < 8; ++j) b[j] = plain ? q_byte(v[j], s, inv) : (uint32_t)q_value(v[j], s);
+    *reinterpret_cast<uint2*>(a.dst + q_off((int)r, k, kc)) = make_uint2(low_bytes(b[0], b[1], b[2], b[3]), low_bytes(b[4], b[5], b[6], b[7]));
   });
 }
 
 template <class T, bool VEC>
 hipError_t launch_rows_t(const QRowsArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.rows + 15) / 16)), block(1024);
-  if (a.K <= 1024) return launch_k(q_rows_kernel<T, 2, VEC>, grid, block, 0, s, a);
-  if (a.K <= 2048) return launch_k(q_rows_kernel<T, 4, VEC>, grid, block, 0, s, a);
-  return launch_k(q_rows_kernel<T, 0, VEC>, grid, block, 0, s, a);
+  const dim3 grid((unsigned)((a.rows + 3) / 4));
+  if (a.K <= 1024) return launch_k(q_rows_kernel<T, 2, 1, VEC>, grid, dim3(256), 0, s, a);
+  if (a.K <= 2048) return launch_k(q_rows_kernel<T, 1, 4, VEC>, grid, dim3(1024), 0, s, a);
+  if (a.K <= 6144) return launch_k(q_rows_kernel<T, 3, 4, VEC>, grid, dim3(1024), 0, s, a);
+  return launch_k(q_rows_kernel<T, 0, 4, VEC>, grid, dim3(1024), 0, s, a);
 }
 
 // ------------------------------------------------------------------ weights --
@@ -166,20 +207,22 @@ __device__ __forceinline__ float w_value(T x) { return Elem<T>::f(x); }
 template <>
 __device__ __forceinline__ float w_value<int8_t>(int8_t x) { return (float)x; }
 
-// Scales and biases of 64 columns by 4 shares of K; columns past N: zeros.
+// Scales and biases of 64 columns by 16 shares of K; columns past N: zeros.
 template <class T>
-__global__ __launch_bounds__(256) void q_scale_kernel(QPackArgs a) {
-  __shared__ uint32_t s_top[4][64];
+__global__ __launch_bounds__(1024) void q_scale_kernel(QPackArgs a) {
+  __shared__ uint32_t s_top[16][64];
   const QWeightsLayout l(a.K, a.N);
   const int c = threadIdx.x & 63, part = threadIdx.x >> 6, n = blockIdx.x * 64 + c;
   const T* w = static_cast<const T*>(a.w);
   uint32_t top = 0;
-  if (n < a.N && !a.scales)
-    for (int k = part; k < a.K; k += 4) top = max(top, mag(w_value<T>(w[k * a.wk + n * a.wn])));
+  if (n < a.N && !a.scales) {
+#pragma unroll 8
+    for (int k = part; k < a.K; k += 16) top = max(top, mag(w_value<T>(w[k * a.wk + n * a.wn])));
+  }
   s_top[part][c] = top;
   __syncthreads();
   if (part || n >= l.blocks * 16) return;
-  top = max(max(s_top[0][c], s_top[1][c]), max(s_top[2][c], s_top[3][c]));
+  for (int i = 1; i < 16; ++i) top = max(top, s_top[i][c]);
   float s = 0.0f, b = 0.0f;
   if (n < a.N) {
     s = a.scales ? a.scales[n] : q_scale(top);
@@ -220,7 +263,7 @@ __global__ __launch_bounds__(256) void q_pack_kernel(QPackArgs a) {
 template <class T>
 hipError_t launch_pack_t(const QPackArgs& a, hipStream_t s) {
   const QWeightsLayout l(a.K, a.N);
-  hipError_t e = launch_k(q_scale_kernel<T>, dim3((l.blocks * 16 + 63) / 64), dim3(256), 0, s, a);
+  hipError_t e = launch_k(q_scale_kernel<T>, dim3((l.blocks * 16 + 63) / 64), dim3(1024), 0, s, a);
   if (e != hipSuccess) return e;
   const long blocks = ((long)l.blocks * l.kc * 64 + 255) / 256;
   return launch_k(q_pack_kernel<T>, dim3((unsigned)std::min<long>(blocks, 4096)), dim3(256), 0, s, a);
@@ -234,7 +277,7 @@ constexpr int kQWaves = 8;
 // w + 8, ...; U of them are in flight together.
 template <int EPI, int RT, int U>
 __global__ __launch_bounds__(kQWaves * 64) void q_gemm_kernel(GemmArgs a) {
-  using T = std::conditional_t<EPI == EPI_QBF, uint16_t, float>;
+  using T = q8_out<EPI>;
   __shared__ i32x4_t part[kQWaves][RT][64];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -277,9 +320,11 @@ __global__ __launch_bounds__(kQWaves * 64) void q_gemm_kernel(GemmArgs a) {
   i32x4_t sum = part[0][w][lane];
 #pragma unroll
   for (int i = 1; i < kQWaves; ++i) sum += part[i][w][lane];
-  if (row < M)
-    q8_store<T>(a, row, col, sum, a.row_scale[row], *reinterpret_cast<const float4*>(a.col_scale + col),
-                *reinterpret_cast<const float4*>(a.bias + col));
+  if (row >= M || col >= a.n) return;
+  const float4 cs = *reinterpret_cast<const float4*>(a.col_scale + col), bi = *reinterpret_cast<const float4*>(a.bias + col);
+  ResRun<T, 4> res;
+  if (q8_wide<EPI>() && a.resid) res.load(static_cast<const T*>(a.resid) + (size_t)row * a.res_ld + col);
+  q8_store<T, 4, q8_wide<EPI>()>(a, row, col, true, &sum, a.row_scale[row], &cs, &bi, res);
 }
 
 template <int EPI>
@@ -309,7 +354,12 @@ hipError_t launch_q_pack(const QPackArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_q_gemm(const GemmArgs& a, int out_f32, int expected, int rows, hipStream_t s) {
-  return out_f32 ? launch_gemm_e<EPI_QF32>(a, expected, rows, s) : launch_gemm_e<EPI_QBF>(a, expected, rows, s);
+  const uintptr_t eb = out_f32 ? 4 : 2;
+  uintptr_t bits = (uintptr_t)a.out | (uintptr_t)a.resid | (uintptr_t)a.n * eb | (uintptr_t)a.out_ld * eb;
+  if (a.resid) bits |= (uintptr_t)a.res_ld * eb;
+  if (bits % 16 == 0)
+    return out_f32 ? launch_gemm_e<EPI_QF32>(a, expected, rows, s) : launch_gemm_e<EPI_QBF>(a, expected, rows, s);
+  return out_f32 ? launch_gemm_e<EPI_QF32_ANY>(a, expected, rows, s) : launch_gemm_e<EPI_QBF_ANY>(a, expected, rows, s);
 }
 
 }  // namespace incvit
