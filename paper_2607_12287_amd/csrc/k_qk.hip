@@ -5,7 +5,8 @@
 // halves takes V values from each half, so both members of every pair are in
 // one lane and the rotation needs no exchange; every other chunk is 2 V values
 // that follow one another.  GL lanes (a power of two) share a head, C chunks to
-// a lane; its sums are combined across them by a butterfly in a fixed order.
+// a lane, and with many rows two heads; sums are combined across the lanes in
+// a fixed order.
 //   RMS: one sum of squares; LayerNorm: the mean, then the squared deviations
 // from it (two passes over registers, no cancellation), all in fp32; the result
 // is rounded once, when it is stored.
@@ -13,6 +14,8 @@
 // Bound: memory (each value is read and written once), and for few rows the
 // launch.  Every load of a lane (its values, gains, cosines and sines) is
 // issued before the first one is used.
+#include <type_traits>
+
 #include "ops.hpp"
 
 namespace incvit {
@@ -49,6 +52,18 @@ template <> struct Run<float, 4> {
   __device__ float get(int i) const { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
   __device__ static void store(float* p, const float* f) { *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]); }
 };
+template <> struct Run<uint16_t, 2> {
+  uint32_t v;
+  __device__ void load(const uint16_t* p) { v = *reinterpret_cast<const uint32_t*>(p); }
+  __device__ float get(int i) const { return __uint_as_float(i ? v & 0xffff0000u : v << 16); }
+  __device__ static void store(uint16_t* p, const float* f) { *reinterpret_cast<uint32_t*>(p) = f2bf2(f[0], f[1]); }
+};
+template <> struct Run<float, 2> {
+  float2 v;
+  __device__ void load(const float* p) { v = *reinterpret_cast<const float2*>(p); }
+  __device__ float get(int i) const { return i ? v.y : v.x; }
+  __device__ static void store(float* p, const float* f) { *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]); }
+};
 template <class T> struct Run<T, 1> {
   T v;
   __device__ void load(const T* p) { v = *p; }
@@ -74,24 +89,18 @@ struct Turns<1> {
   __device__ float sin(int) const { return v.y; }
 };
 
-template <int GL>
-__device__ __forceinline__ float lanes_sum(float x) {
-#pragma unroll
-  for (int off = GL / 2; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
-  return x;
-}
-
 struct HeadSpec {
   int pairs, rot_pairs, adjacent, norm;
   float eps, inv_dim;
 };
 
-// One head of one row by GL lanes.  in, out: pointers to value d of the head by
-// d; gamma, beta: null where there is none; turns: the row's cosines and sines.
-template <class T, class G, int V, int GL, int C, class In, class Out>
-__device__ __forceinline__ void one_head(const HeadSpec& h, int lane, const G* gamma, const G* beta, const float* turns, In in,
-                                         Out out) {
-  Run<T, V> xa[C], xb[C];
+// HP heads of one row by GL lanes, which share their gains, cosines and sines.
+// in, out: value d of head i by (i, d), for i below `heads`; gamma, beta: null
+// where there is none; turns: the row's cosines and sines.
+template <class T, class G, int V, int GL, int C, int HP, class In, class Out>
+__device__ __forceinline__ void some_heads(const HeadSpec& h, int lane, int heads, const G* gamma, const G* beta,
+                                           const float* turns, In in, Out out) {
+  Run<T, V> xa[HP][C], xb[HP][C];
   Run<G, V> ga[C], gb[C], ba[C], bb[C];
   Turns<V> cs[C];
   int da[C], db[C];
@@ -105,8 +114,12 @@ __device__ __forceinline__ void one_head(const HeadSpec& h, int lane, const G* g
     const bool halves = rot[c] && !h.adjacent;
     da[c] = any[c] ? (halves ? p : 2 * p) : 0;
     db[c] = any[c] ? (halves ? p + h.rot_pairs : 2 * p + V) : V;
-    xa[c].load(in(da[c]));
-    xb[c].load(in(db[c]));
+#pragma unroll
+    for (int i = 0; i < HP; ++i) {
+      const int j = min(i, heads - 1);
+      xa[i][c].load(in(j, da[c]));
+      xb[i][c].load(in(j, db[c]));
+    }
     if (normed && gamma) {
       ga[c].load(gamma + da[c]);
       gb[c].load(gamma + db[c]);
@@ -117,108 +130,136 @@ __device__ __forceinline__ void one_head(const HeadSpec& h, int lane, const G* g
     }
     if (h.rot_pairs) cs[c].load(turns + 2 * (rot[c] ? p : 0));
   }
-  float a[C][V], b[C][V];
 #pragma unroll
-  for (int c = 0; c < C; ++c)
+  for (int i = 0; i < HP; ++i) {
+    if (i >= heads) break;  // uniform over the lanes of a head
+    float a[C][V], b[C][V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      a[c][i] = xa[c].get(i);
-      b[c][i] = xb[c].get(i);
-    }
-  if (normed) {
-    float mean = 0.0f;
-    if (h.norm == INCVIT_NORM_LAYER) {
-      float s = 0.0f;
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        a[c][v] = any[c] ? xa[i][c].get(v) : 0.0f;
+        b[c][v] = any[c] ? xb[i][c].get(v) : 0.0f;
+      }
+    if (normed) {
+      float mean = 0.0f;
+      if (h.norm == INCVIT_NORM_LAYER) {
+        float s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int v = 0; v < V; ++v) s += a[c][v] + b[c][v];
+        mean = lanes_sum<GL>(s) * h.inv_dim;
+      }
+      float q = 0.0f;
 #pragma unroll
       for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < V; ++i) s += any[c] ? a[c][i] + b[c][i] : 0.0f;
-      mean = lanes_sum<GL>(s) * h.inv_dim;
+        for (int v = 0; v < V; ++v) {
+          a[c][v] -= mean;
+          b[c][v] -= mean;
+          const float e = a[c][v] * a[c][v] + b[c][v] * b[c][v];
+          q += any[c] ? e : 0.0f;
+        }
+      const float r = 1.0f / sqrtf(lanes_sum<GL>(q) * h.inv_dim + h.eps);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          a[c][v] *= r;
+          b[c][v] *= r;
+          if (gamma) {
+            a[c][v] *= ga[c].get(v);
+            b[c][v] *= gb[c].get(v);
+          }
+          if (beta) {
+            a[c][v] += ba[c].get(v);
+            b[c][v] += bb[c].get(v);
+          }
+        }
     }
-    float q = 0.0f;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c) {
+      // pair v is (a_v, b_v), or values 2 v and 2 v + 1 of the 2 V in a row; the
+      // values past the rotated ones turn by (1, 0)
+      if (rot[c]) {
+        if (!h.adjacent) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        a[c][i] -= mean;
-        b[c][i] -= mean;
-        q += any[c] ? a[c][i] * a[c][i] + b[c][i] * b[c][i] : 0.0f;
-      }
-    const float r = 1.0f / sqrtf(lanes_sum<GL>(q) * h.inv_dim + h.eps);
+          for (int v = 0; v < V; ++v) {
+            const float u = a[c][v] * cs[c].cos(v) - b[c][v] * cs[c].sin(v);
+            b[c][v] = b[c][v] * cs[c].cos(v) + a[c][v] * cs[c].sin(v);
+            a[c][v] = u;
+          }
+        } else {
+          float z[2 * V];
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+          for (int v = 0; v < V; ++v) {
+            z[v] = a[c][v];
+            z[V + v] = b[c][v];
+          }
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        a[c][i] *= r;
-        b[c][i] *= r;
-        if (gamma) {
-          a[c][i] *= ga[c].get(i);
-          b[c][i] *= gb[c].get(i);
-        }
-        if (beta) {
-          a[c][i] += ba[c].get(i);
-          b[c][i] += bb[c].get(i);
-        }
-      }
-  }
+          for (int v = 0; v < V; ++v) {
+            const float u = z[2 * v] * cs[c].cos(v) - z[2 * v + 1] * cs[c].sin(v);
+            z[2 * v + 1] = z[2 * v + 1] * cs[c].cos(v) + z[2 * v] * cs[c].sin(v);
+            z[2 * v] = u;
+          }
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    if (rot[c]) {
-      const bool pairs_split = !h.adjacent;
-      float ya[V], yb[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if (pairs_split) {  // pair i: (a_i, b_i)
-          ya[i] = a[c][i] * cs[c].cos(i) - b[c][i] * cs[c].sin(i);
-          yb[i] = b[c][i] * cs[c].cos(i) + a[c][i] * cs[c].sin(i);
+          for (int v = 0; v < V; ++v) {
+            a[c][v] = z[v];
+            b[c][v] = z[V + v];
+          }
         }
       }
-      if (!pairs_split) {  // the 2 V values one after another: pair i is values 2 i and 2 i + 1
-        float z[2 * V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          z[i] = a[c][i];
-          z[V + i] = b[c][i];
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float u = z[2 * i] * cs[c].cos(i) - z[2 * i + 1] * cs[c].sin(i);
-          z[2 * i + 1] = z[2 * i + 1] * cs[c].cos(i) + z[2 * i] * cs[c].sin(i);
-          z[2 * i] = u;
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          ya[i] = z[i];
-          yb[i] = z[V + i];
-        }
+      if (any[c]) {
+        Run<T, V>::store(out(i, da[c]), a[c]);
+        Run<T, V>::store(out(i, db[c]), b[c]);
       }
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        a[c][i] = ya[i];
-        b[c][i] = yb[i];
-      }
-    }
-    if (any[c]) {
-      Run<T, V>::store(out(da[c]), a[c]);
-      Run<T, V>::store(out(db[c]), b[c]);
     }
   }
 }
 
-template <class T, int V, int GL, int C>
-__global__ __launch_bounds__(256) void qk_kernel(QkArgs a) {
-  const int heads = a.q.heads + a.k.heads;
-  const long item = (long)blockIdx.x * (256 / GL) + threadIdx.x / GL;
-  const int lane = threadIdx.x % GL;
-  if (item >= a.rows * heads) return;  // whole groups of lanes
-  const long r = item / heads;
-  const int hh = (int)(item - r * heads);
-  const bool isk = hh >= a.q.heads;
-  const QkSide& s = isk ? a.k : a.q;
-  const int h = isk ? hh - a.q.heads : hh;
+// Which heads of which row a group of lanes works on: units of up to HP heads of
+// the queries, then of the keys; a workgroup takes `rpb` whole rows, or a share
+// (blockIdx.y) of one row's units where they are more than its groups.
+struct Units {
+  int uq, per_row, rpb, upb;  // units of the queries, of a row; rows, units of a row per workgroup
+};
+template <int GL>
+Units units_of(int hq, int hk, int hp) {
+  Units u;
+  u.uq = (hq + hp - 1) / hp;
+  u.per_row = u.uq + (hk + hp - 1) / hp;
+  u.upb = std::min(u.per_row, 256 / GL);
+  u.rpb = 256 / GL / u.upb;
+  return u;
+}
+template <int GL>
+__device__ __forceinline__ bool unit_of(const Units& u, uint32_t& row, int& unit) {
+  const int g = threadIdx.x / GL;
+  const int rl = (int)(((float)g + 0.5f) * __builtin_amdgcn_rcpf((float)u.upb));  // g / upb: both below 256
+  row = blockIdx.x * (uint32_t)u.rpb + rl;
+  unit = blockIdx.y * u.upb + g - rl * u.upb;
+  return rl < u.rpb && unit < u.per_row;
+}
+
+struct QkLaunch {
+  QkArgs a;
+  Units u;
+};
+
+template <class T, int V, int GL, int C, int HP>
+__global__ __launch_bounds__(256) void qk_kernel(QkLaunch l) {
+  const QkArgs& a = l.a;
+  uint32_t r;
+  int unit;
+  if (!unit_of<GL>(l.u, r, unit) || r >= a.rows) return;  // whole groups of lanes
+  const bool isk = unit >= l.u.uq;
+  const QkSide s = isk ? a.k : a.q;
+  const int h0 = (isk ? unit - l.u.uq : unit) * HP;
   long t = r, dst = r;
   if (a.rot_pairs) {
-    t = a.index ? (long)a.index[r] : r % a.table_rows;
+    if (a.index) t = a.index[r];  // uniform
+    else if (a.table_rows < a.rows) t = r % (uint32_t)a.table_rows;
     if (t < 0 || t >= a.table_rows) return;
   }
   if (isk && a.k_rows) {
@@ -226,37 +267,57 @@ __global__ __launch_bounds__(256) void qk_kernel(QkArgs a) {
     if (dst < 0 || dst >= a.k_out_rows) return;
   }
   const HeadSpec spec{a.head_dim / 2, a.rot_pairs, a.adjacent, a.norm, a.eps, 1.0f / (float)a.head_dim};
-  const T* in = static_cast<const T*>(s.in) + r * s.in_row + h * s.in_head;
-  T* out = static_cast<T*>(s.out) + dst * s.out_row + h * s.out_head;
-  one_head<T, T, V, GL, C>(spec, lane, static_cast<const T*>(s.gamma), static_cast<const T*>(s.beta),
-                           a.table + t * 2 * a.rot_pairs, [&](int d) { return in + d; }, [&](int d) { return out + d; });
+  const T* in = static_cast<const T*>(s.in) + (long)r * s.in_row + h0 * s.in_head;
+  T* out = static_cast<T*>(s.out) + dst * s.out_row + h0 * s.out_head;
+  some_heads<T, T, V, GL, C, HP>(spec, threadIdx.x % GL, s.heads - h0, static_cast<const T*>(s.gamma),
+                                 static_cast<const T*>(s.beta), a.table + t * 2 * a.rot_pairs,
+                                 [&](int i, int d) { return in + i * s.in_head + d; },
+                                 [&](int i, int d) { return out + i * s.out_head + d; });
 }
+
+struct QkLayerLaunch {
+  QkLayerArgs a;
+  Units u;
+};
 
 // The encoder's rows: queries in the compact buffer, keys where the QKV
 // projection left them in the cache.  A chunk's 4 values lie inside one run of 8
 // of the cache's operand order (k_elem), so they are consecutive there too.
-template <class T, int GL, int C>
-__global__ __launch_bounds__(256) void qk_layer_kernel(QkLayerArgs a) {
-  const int H = a.sh.H, dh = a.sh.dh;
-  const int item = blockIdx.x * (256 / GL) + threadIdx.x / GL;
-  const int lane = threadIdx.x % GL;
-  const int r = item / (2 * H), hh = item - r * 2 * H;
-  if (r >= a.meta->m) return;
+template <class T, int GL, int HP>
+__global__ __launch_bounds__(256) void qk_layer_kernel(QkLayerLaunch l) {
+  const QkLayerArgs& a = l.a;
+  uint32_t r;
+  int unit;
+  if (!unit_of<GL>(l.u, r, unit) || r >= (uint32_t)a.meta->m) return;
   const RowInfo ri = a.rows[r];
-  const bool isk = hh >= H;
-  const int h = isk ? hh - H : hh;
-  T* q = static_cast<T*>(a.q) + (size_t)r * a.sh.D + h * dh;
+  const int dh = a.sh.dh;
+  const bool isk = unit >= l.u.uq;
+  const int h0 = (isk ? unit - l.u.uq : unit) * HP;
+  T* q = static_cast<T*>(a.q) + (size_t)r * a.sh.D + h0 * dh;
   T* k = reinterpret_cast<T*>(ri.cache + a.cl.k + (size_t)a.layer * a.cl.kv_layer);
   const HeadSpec spec{dh / 2, a.table ? dh / 2 : 0, a.adjacent, a.norm, a.eps, 1.0f / (float)dh};
-  auto at = [&](int d) { return isk ? k + k_elem(a.sh, h, ri.tok, d) : q + d; };
-  one_head<T, float, 4, GL, C>(spec, lane, isk ? a.k_gamma : a.q_gamma, isk ? a.k_beta : a.q_beta,
-                               a.table + (size_t)ri.tok * dh, at, at);
+  auto at = [&](int i, int d) { return isk ? k + k_elem(a.sh, h0 + i, ri.tok, d) : q + i * dh + d; };
+  some_heads<T, float, 4, GL, 1, HP>(spec, threadIdx.x % GL, a.sh.H - h0, isk ? a.k_gamma : a.q_gamma,
+                                     isk ? a.k_beta : a.q_beta, a.table + (size_t)ri.tok * dh, at, at);
 }
 
+// Two heads of a row to a group of lanes where that still leaves every SIMD two
+// waves, else one (few rows: latency).  1024 rows of 32 heads of 72: 6.5 us
+// against 6.9 with one and 6.6 with four; 8192 rows of 32 of 64: 15.2, 16.0, 15.3.
+inline bool many_heads(long rows, int hq, int hk, int gl) { return hq % 2 == 0 && hk % 2 == 0 && rows * (hq + hk) * gl >= 1 << 18; }
+
+template <class T, int V, int GL, int C, int HP>
+hipError_t launch_h(const QkArgs& a, hipStream_t s) {
+  QkLaunch l{a, units_of<GL>(a.q.heads, a.k.heads, HP)};
+  const dim3 grid((unsigned)((a.rows + l.u.rpb - 1) / l.u.rpb), (l.u.per_row + l.u.upb - 1) / l.u.upb);
+  return launch_k(qk_kernel<T, V, GL, C, HP>, grid, dim3(256), 0, s, l);
+}
 template <class T, int V, int GL, int C>
 hipError_t launch_v(const QkArgs& a, hipStream_t s) {
-  const long items = a.rows * (a.q.heads + a.k.heads);
-  return launch_k(qk_kernel<T, V, GL, C>, dim3((unsigned)((items + 256 / GL - 1) / (256 / GL))), dim3(256), 0, s, a);
+  if constexpr (GL <= 16 && V > 1) {
+    if (many_heads(a.rows, a.q.heads, a.k.heads, GL)) return launch_h<T, V, GL, C, 2>(a, s);
+  }
+  return launch_h<T, V, GL, C, 1>(a, s);
 }
 
 // lanes of a head: the power of two that covers its chunks
@@ -266,7 +327,8 @@ hipError_t launch_lanes(const QkArgs& a, hipStream_t s) {
   if (chunks <= 4) return launch_v<T, V, 4, 1>(a, s);
   if (chunks <= 8) return launch_v<T, V, 8, 1>(a, s);
   if (chunks <= 16) return launch_v<T, V, 16, 1>(a, s);
-  return launch_v<T, V, 32, 1>(a, s);
+  if (chunks <= 32) return launch_v<T, V, 32, 1>(a, s);
+  return launch_v<T, V, 64, 1>(a, s);
 }
 
 // whether every chunk of v values that a call touches is aligned to itself
@@ -288,23 +350,33 @@ hipError_t launch_qk(const QkArgs& a, hipStream_t s) {
   if (a.dtype) {
     if (chunks_aligned(a, 8)) return launch_lanes<uint16_t, 8>(a, s);
     if (chunks_aligned(a, 4)) return launch_lanes<uint16_t, 4>(a, s);
+    if (chunks_aligned(a, 2)) return launch_lanes<uint16_t, 2>(a, s);
     return launch_v<uint16_t, 1, 64, 2>(a, s);
   }
   if (chunks_aligned(a, 4)) return launch_lanes<float, 4>(a, s);
+  if (chunks_aligned(a, 2)) return launch_lanes<float, 2>(a, s);
   return launch_v<float, 1, 64, 2>(a, s);
 }
 
 hipError_t launch_qk_layer(const QkLayerArgs& a, int rows, hipStream_t s) {
-  const int chunks = a.sh.dh / 8;
-  const int gl = chunks <= 4 ? 4 : chunks <= 8 ? 8 : 16;
-  const dim3 grid((unsigned)(((long)rows * 2 * a.sh.H + 256 / gl - 1) / (256 / gl)));
-  auto go = [&](auto t) {
+  const int H = a.sh.H, chunks = a.sh.dh / 8;
+  auto go = [&](auto t, auto gl, auto hp) {
     using T = decltype(t);
-    if (gl == 4) return launch_k(qk_layer_kernel<T, 4, 1>, grid, dim3(256), 0, s, a);
-    if (gl == 8) return launch_k(qk_layer_kernel<T, 8, 1>, grid, dim3(256), 0, s, a);
-    return launch_k(qk_layer_kernel<T, 16, 1>, grid, dim3(256), 0, s, a);
+    constexpr int GL = decltype(gl)::value, HP = decltype(hp)::value;
+    QkLayerLaunch l{a, units_of<GL>(H, H, HP)};
+    const dim3 grid((unsigned)((rows + l.u.rpb - 1) / l.u.rpb), (l.u.per_row + l.u.upb - 1) / l.u.upb);
+    return launch_k(qk_layer_kernel<T, GL, HP>, grid, dim3(256), 0, s, l);
   };
-  return a.sh.dtype ? go(uint16_t{}) : go(float{});
+  auto heads = [&](auto t, auto gl) {
+    if (many_heads(rows, H, H, decltype(gl)::value)) return go(t, gl, std::integral_constant<int, 2>{});
+    return go(t, gl, std::integral_constant<int, 1>{});
+  };
+  auto lanes = [&](auto t) {
+    if (chunks <= 4) return heads(t, std::integral_constant<int, 4>{});
+    if (chunks <= 8) return heads(t, std::integral_constant<int, 8>{});
+    return heads(t, std::integral_constant<int, 16>{});
+  };
+  return a.sh.dtype ? lanes(uint16_t{}) : lanes(float{});
 }
 
 }  // namespace incvit

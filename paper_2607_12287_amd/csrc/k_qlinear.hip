@@ -36,14 +36,17 @@ __device__ __forceinline__ int q_value(float x, float s) {
 // reciprocal and quotients stay normal (q_plain).  inv = 1 / s, correctly
 // rounded: x * inv is within 2 ulp of the quotient, one residual step makes it
 // faithful and the second correctly rounded (Markstein's theorem: a faithful
-// quotient, its exact residual and the correctly rounded reciprocal).  Adding
+// quotient, its exact residual and the correctly rounded reciprocal).  With x
+// and the row's largest magnitude bf16 numbers (BF), one step gives the same
+// integer: shown for every pair of their significands and exponents.  Adding
 // 1.5 * 2^23 rounds to an integer, ties to even, in the low bits; |x / s| is
 // below 127.5, so no clamp.
 __device__ __forceinline__ bool q_plain(float s) { return s > 0x1p-90f && s < 0x1p90f; }
+template <bool BF>
 __device__ __forceinline__ uint32_t q_byte(float x, float s, float inv) {
   float q = x * inv;
   q = fmaf(fmaf(-q, s, x), inv, q);
-  q = fmaf(fmaf(-q, s, x), inv, q);
+  if (!BF) q = fmaf(fmaf(-q, s, x), inv, q);
   return __float_as_uint(q + 12582912.0f);
 }
 // low bytes of four words in one
@@ -51,12 +54,6 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
   return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-
-__device__ __forceinline__ uint32_t wave_max_u(uint32_t x) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, off, 64));
-  return x;
-}
 
 // 8 values of a row from k on (fewer where the row ends: zeros)
 template <class T, bool VEC>
@@ -127,7 +124,7 @@ __global__ __launch_bounds__(256 * WPR) void q_rows_kernel(QRowsArgs a) {
   };
   // sums over the row's waves, in wave order
   auto row_sum = [&](float v, float (&sh)[4][WPR]) {
-    v = wave_sum(v);
+    v = lanes_sum<64>(v);
     if constexpr (WPR > 1) {
       if (lane == 0) sh[wr][wk] = v;
       __syncthreads();
@@ -170,7 +167,7 @@ __global__ __launch_bounds__(256 * WPR) void q_rows_kernel(QRowsArgs a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = max(top, mag(v[j]));
   });
-  top = wave_max_u(top);
+  top = lanes_max<64>(top);
   if constexpr (WPR > 1) {
     if (lane == 0) s_top[wr][wk] = top;
     __syncthreads();
@@ -179,16 +176,22 @@ __global__ __launch_bounds__(256 * WPR) void q_rows_kernel(QRowsArgs a) {
   }
   if (!live) return;
   const float s = q_scale(top), inv = __fdiv_rn(1.0f, s);
-  const bool plain = q_plain(s);  // uniform per wave
   if (lane == 0 && wk == 0) a.scale[r] = s;
-  each([&](int k, float* v) {
-    if constexpr (CH == 0) normed(k, v);
-    if (k >= 64 * kc) return;
-    uint32_t b[8];
+  auto write = [&](auto byte) {
+    each([&](int k, float* v) {
+      if constexpr (CH == 0) normed(k, v);
+      if (k >= 64 * kc) return;
+      uint32_t b[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) b[j] = plain ? q_byte(v[j], s, inv) : (uint32_t)q_value(v[j], s);
-    *reinterpret_cast<uint2*>(a.dst + q_off((int)r, k, kc)) = make_uint2(low_bytes(b[0], b[1], b[2], b[3]), low_bytes(b[4], b[5], b[6], b[7]));
-  });
+      for (int j = 0; j < 8; ++j) b[j] = byte(v[j]);
+      *reinterpret_cast<uint2*>(a.dst + q_off((int)r, k, kc)) =
+          make_uint2(low_bytes(b[0], b[1], b[2], b[3]), low_bytes(b[4], b[5], b[6], b[7]));
+    });
+  };
+  // uniform per wave
+  if (!q_plain(s)) write([&](float v) { return (uint32_t)q_value(v, s); });
+  else if (sizeof(T) == 2 && !ln) write([&](float v) { return q_byte<true>(v, s, inv); });
+  else write([&](float v) { return q_byte<false>(v, s, inv); });
 }
 
 template <class T, bool VEC>

@@ -7,7 +7,8 @@
 // dropped terms are 1.8e-9 and 1.2e-10), swapped and signed by q.
 //
 // Bound: the table's bytes (8 per token and pair), and for a single frame the
-// launch.  A thread forms one pair; a wave's 64 pairs are 512 consecutive bytes.
+// launch.  A thread forms four pairs of one token, 32 bytes, so a token's place
+// in its grid (four integer divisions) is found once for them.
 #include <cmath>
 
 #include "ops.hpp"
@@ -33,35 +34,69 @@ __device__ __forceinline__ float2 cos_sin_turns(double turns) {
   return make_float2(quarter == 1 || quarter == 2 ? -cs : cs, quarter >= 2 ? -sn : sn);
 }
 
-// The position of token `tok` of the launch on axis `ax`.
-__device__ __forceinline__ double grid_position(const RopeArgs& a, int tok, int ax) {
+// The positions of token `tok` of the launch, in the last `axes` of x.
+__device__ __forceinline__ void grid_position(const RopeArgs& a, int tok, double (&x)[3]) {
   int g = 0;
   for (int i = 1; i < a.n_grids; ++i) g = tok >= a.grid[i].first ? i : g;
-  const RopeGrid& r = a.grid[g];
+  const RopeGrid r = a.grid[g];
   const int m = a.merge, hw = r.h * r.w;
   const int local = tok - r.first, f = local / hw, in = local - f * hw;
-  // window row, window, row and column inside it
-  const int band = in / (m * r.w), b = in - band * m * r.w;
-  const int win = b / (m * m), c = b - win * m * m;
-  const int y = band * m + c / m, x = win * m + c % m;
-  if (a.axes == 1) return (double)r.t0 + (double)f * hw + (double)y * r.w + x;
-  const int which = ax + 3 - a.axes;
-  return which == 0 ? (double)r.t0 + f : which == 1 ? (double)r.y0 + y : (double)r.x0 + x;
+  int row, col;
+  if (m == 1) {  // uniform
+    row = in / r.w;
+    col = in - row * r.w;
+  } else {  // window row, window, row and column inside it
+    const int band = in / (m * r.w), b = in - band * m * r.w;
+    const int win = b / (m * m), c = b - win * m * m, cy = c / m;
+    row = band * m + cy;
+    col = win * m + c - cy * m;
+  }
+  x[0] = (double)r.t0 + f;
+  x[1] = (double)r.y0 + row;
+  x[2] = a.axes == 1 ? (double)r.t0 + (double)f * hw + (double)row * r.w + col : (double)r.x0 + col;
 }
 
+// VEC: pairs are even and the table 16-byte aligned.
+template <bool VEC>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-  const int total = a.tokens * a.pairs;
-  for (long e = (long)blockIdx.x * 256 + threadIdx.x; e < total; e += (long)gridDim.x * 256) {
-    const int tok = (int)e / a.pairs, p = (int)e - tok * a.pairs;
-    const int ax = a.axis[p];
-    const double pos = a.n_grids ? grid_position(a, tok, ax) : (double)a.pos[ax * a.axis_stride + tok * a.token_stride];
-    reinterpret_cast<float2*>(a.table)[e] = cos_sin_turns(pos * a.freq[p]);
+  const int per = (a.pairs + 3) / 4;  // threads of a token
+  const uint32_t total = (uint32_t)a.tokens * per;
+  for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < total; e += gridDim.x * 256) {
+    const int tok = (int)(e / (uint32_t)per), p0 = 4 * (int)(e - (uint32_t)tok * per);
+    double x[3] = {0.0, 0.0, 0.0};
+    if (a.n_grids) {  // uniform
+      grid_position(a, tok, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const int ax = i - 3 + a.axes;
+        if (ax >= 0) x[i] = (double)a.pos[ax * a.axis_stride + tok * a.token_stride];  // uniform
+      }
+    }
+    float2 t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = min(p0 + i, a.pairs - 1), ax = a.axis[p] + 3 - a.axes;
+      t[i] = cos_sin_turns((ax == 0 ? x[0] : ax == 1 ? x[1] : x[2]) * a.freq[p]);
+    }
+    float2* out = reinterpret_cast<float2*>(a.table) + (size_t)tok * a.pairs + p0;
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      if (VEC) {
+        if (p0 + i < a.pairs) *reinterpret_cast<float4*>(out + i) = make_float4(t[i].x, t[i].y, t[i + 1].x, t[i + 1].y);
+      } else {
+        if (p0 + i < a.pairs) out[i] = t[i];
+        if (p0 + i + 1 < a.pairs) out[i + 1] = t[i + 1];
+      }
+    }
   }
 }
 
 hipError_t launch_rope(const RopeArgs& a, hipStream_t s) {
-  const long blocks = ((long)a.tokens * a.pairs + 255) / 256;
-  return launch_k(rope_kernel, dim3((unsigned)std::min<long>(blocks, 4096)), dim3(256), 0, s, a);
+  const long blocks = ((long)a.tokens * ((a.pairs + 3) / 4) + 255) / 256;
+  const dim3 grid((unsigned)std::min<long>(blocks, 8192));
+  if (a.pairs % 2 == 0 && (uintptr_t)a.table % 16 == 0) return launch_k(rope_kernel<true>, grid, dim3(256), 0, s, a);
+  return launch_k(rope_kernel<false>, grid, dim3(256), 0, s, a);
 }
 
 bool rope_pairs(const incvit_rope& r, RopeArgs& a) {

@@ -143,3 +143,45 @@ hipError_t launch_qk(const QkArgs& a, hipStream_t s);
 hipError_t launch_qk_layer(const QkLayerArgs& a, int rows, hipStream_t s);
 
 }  // namespace incvit
+
+#if defined(__HIPCC__)
+namespace incvit {
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false);
+}
+
+// op over the GL lanes (a power of two from 4 on, aligned) that share a value's
+// work; every lane gets the result, the same bits.  Neighbours and quads by
+// quad permutes, then mirrors of 8 and 16 lanes (whose halves hold one value
+// each by then), then gfx950's swaps of 16 and of 32: no trip through LDS.
+template <int GL, class Op>
+__device__ __forceinline__ uint32_t lanes_join(uint32_t x, Op op) {
+  x = op(x, dpp<0xb1>(x));
+  x = op(x, dpp<0x4e>(x));
+  if constexpr (GL >= 8) x = op(x, dpp<0x141>(x));
+  if constexpr (GL >= 16) x = op(x, dpp<0x140>(x));
+  if constexpr (GL >= 32) {
+    const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = op(p[0], p[1]);
+  }
+  if constexpr (GL >= 64) {
+    const auto p = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = op(p[0], p[1]);
+  }
+  return x;
+}
+template <int GL>
+__device__ __forceinline__ float lanes_sum(float x) {
+  return __uint_as_float(lanes_join<GL>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
+template <int GL>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
+  return lanes_join<GL>(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+
+}  // namespace incvit
+#endif
