@@ -936,9 +936,8 @@ incvit_status incvit_pack_weights(const incvit_config* cfg, const void* canonica
     RopeArgs a = {};
     const incvit_rope r = {2, {sh.dh / 4, sh.dh / 4, 0}, INCVIT_LADDER_AXIS, INCVIT_LAYOUT_BLOCKS, cfg->rope_theta, {1.0, 1.0, 1.0}};
     if (!rope_pairs(r, a)) return fail(nullptr, INCVIT_ERR_ARG, "rope out of range");
-    a.tokens = sh.N;
-    a.n_grids = a.merge = 1;
-    a.grid[0] = RopeGrid{1, cfg->img_h / cfg->patch, cfg->img_w / cfg->patch, 0, 0, 0, 0};
+    a.merge = 1;
+    rope_grid(a, 0, incvit_grid{1, cfg->img_h / cfg->patch, cfg->img_w / cfg->patch, 0, 0, 0});
     a.table = reinterpret_cast<float*>(dst + pl.rope);
     e = launch_rope(a, s);
   }

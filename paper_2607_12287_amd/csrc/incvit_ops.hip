@@ -179,13 +179,7 @@ incvit_status incvit_rope_table_grids(const incvit_rope* r, int32_t n, const inc
   }
   a.merge = merge;
   for (int32_t i = 0; i < n; i += kGridsPerLaunch) {
-    a.n_grids = n - i < kGridsPerLaunch ? n - i : kGridsPerLaunch;
-    a.tokens = 0;
-    for (int j = 0; j < a.n_grids; ++j) {
-      const incvit_grid& g = grids[i + j];
-      a.grid[j] = RopeGrid{g.t, g.h, g.w, g.t0, g.y0, g.x0, a.tokens};
-      a.tokens += g.t * g.h * g.w;
-    }
+    for (int j = 0; j < kGridsPerLaunch && i + j < n; ++j) rope_grid(a, j, grids[i + j]);
     a.table = table;
     table += (size_t)a.tokens * a.pairs * 2;
     const incvit_status st = launched(launch_rope(a, static_cast<hipStream_t>(stream)), "rope_table_grids");

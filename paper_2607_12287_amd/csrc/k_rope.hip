@@ -7,8 +7,8 @@
 // dropped terms are 1.8e-9 and 1.2e-10), swapped and signed by q.
 //
 // Bound: the table's bytes (8 per token and pair), and for a single frame the
-// launch.  A thread forms four pairs of one token, 32 bytes, so a token's place
-// in its grid (four integer divisions) is found once for them.
+// launch.  A thread forms two pairs of one token, 16 bytes, and finds the token's
+// place in its grid by products with reciprocals in fp64.
 #include <cmath>
 
 #include "ops.hpp"
@@ -34,23 +34,21 @@ __device__ __forceinline__ float2 cos_sin_turns(double turns) {
   return make_float2(quarter == 1 || quarter == 2 ? -cs : cs, quarter >= 2 ? -sn : sn);
 }
 
+// n / d for 0 <= n < 2^31 and per = 1 / d in fp64: (n + 1/2) / d is at least
+// 1 / 2d from a whole number, 2^20 times the product's error.
+__device__ __forceinline__ int divided(int n, double per) { return (int)(((double)n + 0.5) * per); }
+
 // The positions of token `tok` of the launch, in the last `axes` of x.
 __device__ __forceinline__ void grid_position(const RopeArgs& a, int tok, double (&x)[3]) {
   int g = 0;
   for (int i = 1; i < a.n_grids; ++i) g = tok >= a.grid[i].first ? i : g;
   const RopeGrid r = a.grid[g];
   const int m = a.merge, hw = r.h * r.w;
-  const int local = tok - r.first, f = local / hw, in = local - f * hw;
-  int row, col;
-  if (m == 1) {  // uniform
-    row = in / r.w;
-    col = in - row * r.w;
-  } else {  // window row, window, row and column inside it
-    const int band = in / (m * r.w), b = in - band * m * r.w;
-    const int win = b / (m * m), c = b - win * m * m, cy = c / m;
-    row = band * m + cy;
-    col = win * m + c - cy * m;
-  }
+  const int local = tok - r.first, f = divided(local, r.per_frame), in = local - f * hw;
+  // window row, window, row and column inside it
+  const int band = divided(in, r.per_band), b = in - band * m * r.w;
+  const int win = divided(b, a.per_window), c = b - win * m * m, cy = divided(c, a.per_side);
+  const int row = band * m + cy, col = win * m + c - cy * m;
   x[0] = (double)r.t0 + f;
   x[1] = (double)r.y0 + row;
   x[2] = a.axes == 1 ? (double)r.t0 + (double)f * hw + (double)row * r.w + col : (double)r.x0 + col;
@@ -59,10 +57,10 @@ __device__ __forceinline__ void grid_position(const RopeArgs& a, int tok, double
 // VEC: pairs are even and the table 16-byte aligned.
 template <bool VEC>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-  const int per = (a.pairs + 3) / 4;  // threads of a token
+  const int per = (a.pairs + 1) / 2;  // threads of a token
   const uint32_t total = (uint32_t)a.tokens * per;
   for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < total; e += gridDim.x * 256) {
-    const int tok = (int)(e / (uint32_t)per), p0 = 4 * (int)(e - (uint32_t)tok * per);
+    const int tok = divided((int)e, a.per_token), p0 = 2 * ((int)e - tok * per);
     double x[3] = {0.0, 0.0, 0.0};
     if (a.n_grids) {  // uniform
       grid_position(a, tok, x);
@@ -73,15 +71,15 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
         if (ax >= 0) x[i] = (double)a.pos[ax * a.axis_stride + tok * a.token_stride];  // uniform
       }
     }
-    float2 t[4];
+    float2 t[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       const int p = min(p0 + i, a.pairs - 1), ax = a.axis[p] + 3 - a.axes;
       t[i] = cos_sin_turns((ax == 0 ? x[0] : ax == 1 ? x[1] : x[2]) * a.freq[p]);
     }
     float2* out = reinterpret_cast<float2*>(a.table) + (size_t)tok * a.pairs + p0;
 #pragma unroll
-    for (int i = 0; i < 4; i += 2) {
+    for (int i = 0; i < 2; i += 2) {
       if (VEC) {
         if (p0 + i < a.pairs) *reinterpret_cast<float4*>(out + i) = make_float4(t[i].x, t[i].y, t[i + 1].x, t[i + 1].y);
       } else {
@@ -92,8 +90,21 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   }
 }
 
-hipError_t launch_rope(const RopeArgs& a, hipStream_t s) {
-  const long blocks = ((long)a.tokens * ((a.pairs + 3) / 4) + 255) / 256;
+void rope_grid(RopeArgs& a, int i, const incvit_grid& g) {
+  const int first = i == 0 ? 0 : a.tokens;
+  a.grid[i] = RopeGrid{1.0 / ((double)g.h * g.w), 1.0 / ((double)a.merge * g.w), g.h, g.w, g.t0, g.y0, g.x0, first};
+  a.n_grids = i + 1;
+  a.tokens = first + g.t * g.h * g.w;
+}
+
+hipError_t launch_rope(const RopeArgs& a0, hipStream_t s) {
+  RopeArgs a = a0;
+  a.per_token = 1.0 / ((a.pairs + 1) / 2);
+  if (a.n_grids) {
+    a.per_side = 1.0 / a.merge;
+    a.per_window = 1.0 / ((double)a.merge * a.merge);
+  }
+  const long blocks = ((long)a.tokens * ((a.pairs + 1) / 2) + 255) / 256;
   const dim3 grid((unsigned)std::min<long>(blocks, 8192));
   if (a.pairs % 2 == 0 && (uintptr_t)a.table % 16 == 0) return launch_k(rope_kernel<true>, grid, dim3(256), 0, s, a);
   return launch_k(rope_kernel<false>, grid, dim3(256), 0, s, a);

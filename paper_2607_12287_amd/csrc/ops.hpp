@@ -16,7 +16,8 @@ constexpr int kMaxPairs = 128;   // pairs of one head: head dims up to 256
 constexpr int kGridsPerLaunch = 32;
 
 struct RopeGrid {
-  int t, h, w, t0, y0, x0;
+  double per_frame, per_band;  // 1 / (h w), 1 / (merge w)
+  int h, w, t0, y0, x0;
   int first;  // first token of the grid within the launch
 };
 
@@ -26,6 +27,7 @@ struct RopeArgs {
   int pairs, axes;
   int tokens;               // of this launch
   int n_grids, merge;       // n_grids == 0: positions from `pos`
+  double per_window, per_side, per_token;  // 1 / merge^2, 1 / merge, 1 / threads of a token
   const int* pos;           // axis ax, token k: pos[ax * axis_stride + k * token_stride]
   long axis_stride, token_stride;
   float* table;             // [tokens][pairs][2]
@@ -35,6 +37,8 @@ static_assert(sizeof(RopeArgs) <= 4096, "kernel arguments");
 
 // Fills freq, axis, pairs and axes; false for a description out of range.
 bool rope_pairs(const incvit_rope& r, RopeArgs& a);
+// The i-th grid of a launch, whose tokens follow those before it.
+void rope_grid(RopeArgs& a, int i, const incvit_grid& g);
 hipError_t launch_rope(const RopeArgs& a, hipStream_t s);
 
 // ------------------------------------------- head norms with the rotation --
