@@ -276,8 +276,9 @@ hipError_t launch_pack_t(const QPackArgs& a, hipStream_t s) {
 
 constexpr int kQWaves = 8;
 
-// One block of 16 columns by RT tiles of 16 rows.  Wave w multiplies chunks w,
-// w + 8, ...; U of them are in flight together.
+// One block of 16 columns by RT tiles of 16 rows; with more rows than the launch
+// was sized for, also those `rgroups` groups further on.  Wave w multiplies
+// chunks w, w + 8, ...; U of them are in flight together.
 template <int EPI, int RT, int U>
 __global__ __launch_bounds__(kQWaves * 64) void q_gemm_kernel(GemmArgs a) {
   using T = q8_out<EPI>;
@@ -285,62 +286,90 @@ __global__ __launch_bounds__(kQWaves * 64) void q_gemm_kernel(GemmArgs a) {
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int M = a.meta ? a.meta->m : a.m_host;
-  const int m0 = blockIdx.y * RT * 16, cb = blockIdx.x, kc = a.kchunks;
-  if (m0 >= M) return;  // uniform
-  const int tiles = (M + 15) / 16;
-  const uint4* W = reinterpret_cast<const uint4*>(a.W) + (size_t)cb * kc * 64 + lane;
+  // column blocks are dealt to the XCDs in runs, the row groups of one block
+  // together: its weights are fetched by one XCD (128 x 1152 -> 4304: 6.2 -> 5.0 us)
+  const int nz = a.rgroups, total = gridDim.x, lin = blockIdx.x;
+  const int xcd = lin % 8, pos = xcd * (total / 8) + min(xcd, total % 8) + lin / 8;
+  const int cblk = pos / nz, kc = a.kchunks, tiles = (M + 15) / 16;
+  const uint4* W = reinterpret_cast<const uint4*>(a.W) + (size_t)cblk * kc * 64 + lane;
   const uint4* A = reinterpret_cast<const uint4*>(a.A) + lane;
-  i32x4_t acc[RT];
-  const uint4* At[RT];
+  for (int m0 = pos % nz * RT * 16; m0 < M; m0 += nz * RT * 16) {  // uniform
+    i32x4_t acc[RT];
+    const uint4* At[RT];
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    acc[r] = i32x4_t{0, 0, 0, 0};
-    At[r] = A + (size_t)min(m0 / 16 + r, tiles - 1) * kc * 64;
-  }
-  for (int c0 = w; c0 < kc; c0 += kQWaves * U) {
-    uint4 wf[U], af[U][RT];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int c = min(c0 + kQWaves * u, kc - 1);
-      wf[u] = W[(size_t)c * 64];
-#pragma unroll
-      for (int r = 0; r < RT; ++r) af[u][r] = At[r][(size_t)c * 64];
+    for (int r = 0; r < RT; ++r) {
+      acc[r] = i32x4_t{0, 0, 0, 0};
+      At[r] = A + (size_t)min(m0 / 16 + r, tiles - 1) * kc * 64;
     }
+    for (int c0 = w; c0 < kc; c0 += kQWaves * U) {
+      uint4 wf[U], af[U][RT];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (c0 + kQWaves * u < kc) {  // uniform
+      for (int u = 0; u < U; ++u) {
+        const int c = min(c0 + kQWaves * u, kc - 1);
+        wf[u] = W[(size_t)c * 64];
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-          mma_q8(acc[r], __builtin_bit_cast(u32x4_t, wf[u]), __builtin_bit_cast(u32x4_t, af[u][r]));
+        for (int r = 0; r < RT; ++r) af[u][r] = At[r][(size_t)c * 64];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (c0 + kQWaves * u < kc) {  // uniform
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+            mma_q8(acc[r], __builtin_bit_cast(u32x4_t, wf[u]), __builtin_bit_cast(u32x4_t, af[u][r]));
+        }
       }
     }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) part[w][r][lane] = acc[r];
+    __syncthreads();
+    const int row = m0 + 16 * w + n, col = cblk * 16 + 4 * g;
+    if (w < RT && row < M && col < a.n) {
+      i32x4_t sum = part[0][w][lane];
+#pragma unroll
+      for (int i = 1; i < kQWaves; ++i) sum += part[i][w][lane];
+      const float4 cs = *reinterpret_cast<const float4*>(a.col_scale + col), bi = *reinterpret_cast<const float4*>(a.bias + col);
+      ResRun<T, 4> res;
+      if (q8_wide<EPI>() && a.resid) res.load(static_cast<const T*>(a.resid) + (size_t)row * a.res_ld + col);
+      q8_store<T, 4, q8_wide<EPI>()>(a, row, col, true, &sum, a.row_scale[row], &cs, &bi, res);
+    }
+    __syncthreads();  // `part` is written again
   }
-#pragma unroll
-  for (int r = 0; r < RT; ++r) part[w][r][lane] = acc[r];
-  __syncthreads();
-  if (w >= RT) return;
-  const int row = m0 + 16 * w + n, col = cb * 16 + 4 * g;
-  i32x4_t sum = part[0][w][lane];
-#pragma unroll
-  for (int i = 1; i < kQWaves; ++i) sum += part[i][w][lane];
-  if (row >= M || col >= a.n) return;
-  const float4 cs = *reinterpret_cast<const float4*>(a.col_scale + col), bi = *reinterpret_cast<const float4*>(a.bias + col);
-  ResRun<T, 4> res;
-  if (q8_wide<EPI>() && a.resid) res.load(static_cast<const T*>(a.resid) + (size_t)row * a.res_ld + col);
-  q8_store<T, 4, q8_wide<EPI>()>(a, row, col, true, &sum, a.row_scale[row], &cs, &bi, res);
 }
 
+template <int EPI, int RT, int U>
+hipError_t launch_few(const GemmArgs& a0, int expected, hipStream_t s) {
+  GemmArgs a = a0;
+  a.rgroups = (expected + 16 * RT - 1) / (16 * RT);
+  return launch_k(q_gemm_kernel<EPI, RT, U>, dim3((unsigned)(a.Nout / 16) * a.rgroups), dim3(kQWaves * 64), 0, s, a);
+}
+
+// Few rows or the large-row GEMM.  us per launch: the former takes about 2.3 +
+// (1.6 + 0.19 chunks) per 10^6 outputs (chunks of 64 along K), the latter 3.9 +
+// 0.105 per chunk while it has one round of tiles (its workgroup's chunks follow
+// one another); they meet at the outputs below.  Measured, few rows against
+// large-row: 128 x 1152 -> 4304 5.0 against 5.6, 192 rows 6.2 against 5.7;
+// 384 x 4304 -> 1152 9.4 against 11.4, 512 rows 12.1 against 11.5; 1024 x 192 ->
+// 768 3.9 against 4.4, 2048 rows 5.6 against 4.8.
+//
+// Few rows: as many row tiles to a workgroup (each W fragment read once for all)
+// as still leave three workgroups to four CUs, four only beyond 128 rows: 64 x
+// 1152 -> 4304 2 tiles 3.8, 1 tile 4.6, 4 tiles 4.2; 192 x 1024 -> 4096 4 tiles
+// 5.2, 2 tiles 5.6; 48 x 4304 -> 1152 2 tiles 4.0, 1 tile 3.5.  Chunks in flight
+// per wave: 2 where its share is at most 4 (more would load some twice), else 4:
+// 23 x 1152 -> 4304 3.3 against 3.7, 64 x 4304 -> 1152 4.0 against 4.4.
 template <int EPI>
 hipError_t launch_gemm_e(const GemmArgs& a, int expected, int rows, hipStream_t s) {
-  if (expected > 128) return launch_tiled_epi<EPI>(a, expected, rows, s);
-  const unsigned blocks = a.Nout / 16;
-  auto go = [&](auto rt) {
-    constexpr int RT = decltype(rt)::value;
-    return launch_k(q_gemm_kernel<EPI, RT, RT == 4 ? 2 : 4>, dim3(blocks, (rows + 16 * RT - 1) / (16 * RT)), dim3(kQWaves * 64), 0, s, a);
-  };
-  if (rows <= 16) return go(std::integral_constant<int, 1>{});
-  if (rows <= 32) return go(std::integral_constant<int, 2>{});
-  return go(std::integral_constant<int, 4>{});
+  const double outputs = (double)expected * a.n, kc = a.kchunks;
+  if (outputs * (1.6 + 0.19 * kc) > 1e6 * (1.6 + 0.105 * kc)) return launch_tiled_epi<EPI>(a, expected, rows, s);
+  const int blocks = a.Nout / 16;
+  auto fills = [&](int rt) { return blocks * ((expected + 16 * rt - 1) / (16 * rt)) >= 192; };
+  const int rt = expected > 128 && fills(4) ? 4 : expected > 16 && fills(2) ? 2 : 1;
+  if ((a.kchunks + kQWaves - 1) / kQWaves <= 4) {
+    if (rt == 4) return launch_few<EPI, 4, 2>(a, expected, s);
+    return rt == 2 ? launch_few<EPI, 2, 2>(a, expected, s) : launch_few<EPI, 1, 2>(a, expected, s);
+  }
+  if (rt == 4) return launch_few<EPI, 4, 4>(a, expected, s);
+  return rt == 2 ? launch_few<EPI, 2, 4>(a, expected, s) : launch_few<EPI, 1, 4>(a, expected, s);
 }
 
 }  // namespace
