@@ -89,14 +89,18 @@ __host__ __device__ constexpr bool ln_on_load() {
 }
 template <int EPI>
 __host__ __device__ constexpr bool is_q8() {
-  return EPI == EPI_QBF || EPI == EPI_QF32 || EPI == EPI_QBF_ANY || EPI == EPI_QF32_ANY;
+  return EPI >= EPI_QBF;
 }
 template <int EPI>
 __host__ __device__ constexpr bool q8_wide() {
-  return EPI == EPI_QBF || EPI == EPI_QF32;
+  return EPI != EPI_QBF_ANY && EPI != EPI_QF32_ANY;
 }
 template <int EPI>
-using q8_out = std::conditional_t<EPI == EPI_QBF || EPI == EPI_QBF_ANY, uint16_t, float>;
+__host__ __device__ constexpr bool q8_down() {
+  return EPI == EPI_QDOWN_BF || EPI == EPI_QDOWN_F32;
+}
+template <int EPI>
+using q8_out = std::conditional_t<EPI == EPI_QBF || EPI == EPI_QBF_ANY || EPI == EPI_QDOWN_BF, uint16_t, float>;
 template <int EPI>
 __host__ __device__ constexpr int gemm_waves() {
   return kGemmWaves;
@@ -183,6 +187,8 @@ __device__ __forceinline__ void join_blocks(i32x4_t& x, i32x4_t& y) {
 // fp32 with one rounding at the end.  With WIDE a run is inside the output or
 // outside it as a whole and takes 16 bytes (8 of bf16 with NC = 4) at once, and
 // its residual `res` has been loaded; else each column is looked at.
+// q8_down_store: the encoder's down projection, Z_{l+1} = S(H + S(sum * .. + b_2))
+// into the compact rows (operand order) and the cache's X^{l+1}.
 template <class T, int NC>
 struct ResRun {
   uint32_t w[NC * sizeof(T) / 4];
@@ -205,16 +211,37 @@ struct ResRun {
     }
   }
 };
-template <class T, int NC, bool WIDE>
-__device__ __forceinline__ void q8_store(const GemmArgs& a, int row, int col, bool ok, const i32x4_t* acc, float rs,
-                                         const float4* cs, const float4* cb, const ResRun<T, NC>& res) {
-  float y[NC];
+template <int NC>
+__device__ __forceinline__ void q8_scaled(float* y, const i32x4_t* acc, float rs, const float4* cs, const float4* cb) {
 #pragma unroll
   for (int q = 0; q < NC / 4; ++q) {
     const float sc[4] = {cs[q].x, cs[q].y, cs[q].z, cs[q].w}, bi[4] = {cb[q].x, cb[q].y, cb[q].z, cb[q].w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[4 * q + j] = fmaf((float)acc[q][j], rs * sc[j], bi[j]);
   }
+}
+template <class T, int NC>
+__device__ __forceinline__ const T* q8_res(const GemmArgs& a, bool down, int row, int col) {
+  const T* p = static_cast<const T*>(a.resid);
+  return down ? p + frag_off(row, col, a.ldo / 32) : p + (size_t)row * a.res_ld + col;
+}
+template <class T, int NC>
+__device__ __forceinline__ void q8_down_store(const GemmArgs& a, int row, int col, bool ok, const i32x4_t* acc, float rs,
+                                              const float4* cs, const float4* cb, const ResRun<T, NC>& res, const RowInfo& ri) {
+  float y[NC];
+  q8_scaled<NC>(y, acc, rs, cs, cb);
+#pragma unroll
+  for (int j = 0; j < NC; ++j) y[j] = res.get(j) + Elem<T>::rnd(y[j]);
+  if (!ok) return;
+  ResRun<T, NC> o;
+  o.store(static_cast<T*>(a.out) + frag_off(row, col, a.ldo / 32), y);
+  o.store(x_row<T>(ri.cache, a.cl, a.sh, a.layer + 1, ri.tok) + col, y);
+}
+template <class T, int NC, bool WIDE>
+__device__ __forceinline__ void q8_store(const GemmArgs& a, int row, int col, bool ok, const i32x4_t* acc, float rs,
+                                         const float4* cs, const float4* cb, const ResRun<T, NC>& res) {
+  float y[NC];
+  q8_scaled<NC>(y, acc, rs, cs, cb);
   if (a.gelu) {  // uniform
 #pragma unroll
     for (int j = 0; j < NC; ++j) y[j] = gelu_tanh(y[j]);

@@ -407,11 +407,16 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
       // residuals while the run before is worked on; loads run for every lane
       // (clamped) and only the stores are masked, as below.
       using TO = q8_out<EPI>;
-      constexpr bool WIDE = q8_wide<EPI>();
+      constexpr bool WIDE = q8_wide<EPI>(), DOWN = q8_down<EPI>();
       constexpr int PB = std::is_same<TO, uint16_t>::value && TC % 2 == 0 ? 2 : 1, NC = 4 * PB, NP = TC / PB;
       float rs[TR];
 #pragma unroll
       for (int r = 0; r < TR; ++r) rs[r] = a.row_scale[min(t.m0 + (wr * TR + r) * 16 + n, M - 1)];
+      RowInfo ri[DOWN ? TR : 1];
+      if constexpr (DOWN) {
+#pragma unroll
+        for (int r = 0; r < TR; ++r) ri[r] = a.rows[min(t.m0 + (wr * TR + r) * 16 + n, M - 1)];
+      }
       float4 cs[2][PB], cb[2][PB];
       ResRun<TO, NC> rv[2];
       const int cw = (t.cb0 + wc * TC) * 16 + NC * g;
@@ -425,8 +430,7 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
       };
       auto load_res = [&](int i) {  // run i: columns p = i / TR, rows r = i % TR
         if (WIDE && a.resid)        // uniform
-          rv[i & 1].load(static_cast<const TO*>(a.resid) + (size_t)min(t.m0 + (wr * TR + i % TR) * 16 + n, M - 1) * a.res_ld +
-                         min(cw + i / TR * PB * 16, a.n - NC));
+          rv[i & 1].load(q8_res<TO, NC>(a, DOWN, min(t.m0 + (wr * TR + i % TR) * 16 + n, M - 1), min(cw + i / TR * PB * 16, a.n - NC)));
       };
       load_cols(0);
       load_res(0);
@@ -440,7 +444,9 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
 #pragma unroll
         for (int q = 0; q < PB; ++q) v[q] = acc[r][p * PB + q];
         if constexpr (PB == 2) join_blocks(v[0], v[1]);
-        q8_store<TO, NC, WIDE>(a, row, col, row < M && col < a.n, v, rs[r], cs[p & 1], cb[p & 1], rv[i & 1]);
+        const bool ok = row < M && col < a.n;
+        if constexpr (DOWN) q8_down_store<TO, NC>(a, row, col, ok, v, rs[r], cs[p & 1], cb[p & 1], rv[i & 1], ri[r]);
+        else q8_store<TO, NC, WIDE>(a, row, col, ok, v, rs[r], cs[p & 1], cb[p & 1], rv[i & 1]);
       }
     } else {
     // ---- epilogue: lane (g, n) holds columns 4g..4g+3 of row n of each 16x16

@@ -537,10 +537,10 @@ incvit_status run_layers(incvit_handle* h, const Views& views, int B, const WsLa
     // sums of every row no longer go through memory), so by default only when
     // M is known on the host and at least 192; the large-row form whenever it
     // is not split over K (above)
-    // (the 8-bit down projection always leaves its fp32 sums to the row kernel)
-    const bool down = !sh.q8 && !all && l + 1 < sh.L &&
+    const bool down = !all && l + 1 < sh.L &&
+                      (sh.q8 ||
                       (tiled_fc2 ? fc2_split == 1
-                                 : h->fc2_mode == 2 || (h->fc2_mode == 0 && exact_m && mmax >= 192));
+                                 : h->fc2_mode == 2 || (h->fc2_mode == 0 && exact_m && mmax >= 192)));
     auto gemm = [&](int kind, int kernel_kind) -> incvit_status {
       GemmGeom g = gemm_geom(sh, kind);
       const bool mlp = kind == G_FC1 || kind == G_FC2;
@@ -629,8 +629,9 @@ incvit_status run_layers(incvit_handle* h, const Views& views, int B, const WsLa
     };
 
     // One MLP projection in 8-bit integers: the rows (LN2 of H, in operand order,
-    // or G) quantised, then multiplied; G = S(GELU(.)) row-major, or the fp32 sums
-    // of the down projection, to which the row kernel adds the bias.
+    // or G) quantised, then multiplied; G = S(GELU(.)) row-major; the down
+    // projection ends like the whole-K one above, or leaves its fp32 sums to the
+    // row kernel, which adds the bias.
     auto mlp_q8 = [&](int kind, int kernel_kind) -> incvit_status {
       const bool up = kind == G_FC1;
       const int K = up ? sh.D : sh.F, Nout = up ? sh.F : sh.D;
@@ -671,6 +672,17 @@ incvit_status run_layers(incvit_handle* h, const Views& views, int B, const WsLa
       a.out_ld = up ? sh.Fpad : sh.D;
       a.n = Nout;
       a.gelu = up;
+      if (!up && down) {
+        a.bias = fptr(h, P.b_2);
+        a.resid = ws + wl.h;
+        a.out = ws + wl.z;
+        a.ldo = sh.D;
+        a.rows = mrows;
+        a.sh = sh;
+        a.cl = h->cl;
+        a.layer = l;
+        return run(h, kernel_kind, s, [&] { return launch_q_down(a, !sh.dtype, exp_mlp, mlp_rows, s); });
+      }
       return run(h, kernel_kind, s, [&] { return launch_q_gemm(a, !up || !sh.dtype, exp_mlp, mlp_rows, s); });
     };
 

@@ -100,8 +100,7 @@ __global__ __launch_bounds__(256 * WPR) void q_rows_kernel(QRowsArgs a) {
   const T* x = static_cast<const T*>(a.x);
   auto fetch = [&](int i, float* v) {  // the lane's i-th run of 8
     const int k = live ? 8 * (lane + 64 * (wk + WPR * i)) : K;
-    if (a.frag) load8<T, true>(x + (k < K ? frag_off((int)r, k, (int)a.ld / 32) : 0) - k, k, K, v);  // uniform
-    else load8<T, VEC>(x + (size_t)r * a.ld, k, K, v);
+    load8<T, VEC>(x + (size_t)r * a.ld, k, K, v);
   };
   constexpr int NH = CH > 0 ? CH : 1;
   const int runs = CH > 0 ? CH : (kc * 8 + 64 * WPR - 1) / (64 * WPR);
@@ -192,6 +191,116 @@ __global__ __launch_bounds__(256 * WPR) void q_rows_kernel(QRowsArgs a) {
   if (!q_plain(s)) write([&](float v) { return (uint32_t)q_value(v, s); });
   else if (sizeof(T) == 2 && !ln) write([&](float v) { return q_byte<true>(v, s, inv); });
   else write([&](float v) { return q_byte<false>(v, s, inv); });
+}
+
+
+// Rows in operand order (the encoder's H: 16 rows x 32 columns to a kilobyte of
+// bf16, frag_off): a tile of 16 rows to a workgroup of NW waves.  Lane 16 g + n
+// works on row n as the product will hold it, values 64 c + 16 g .. + 15 of the
+// CI chunks c = w, w + NW, ... (K <= 64 NW CI), so a wave reads and writes whole
+// runs of 256 bytes; a wave per row, as above, would use 16 bytes of every line
+// that it touches (8192 rows of 1024: 33 us against T_FRAG).
+template <class T, int NW, int CI>
+__global__ __launch_bounds__(64 * NW) void q_tile_kernel(QRowsArgs a) {
+  __shared__ uint32_t s_row[3][16][NW];
+  const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long rows = a.meta ? a.meta->m : a.rows, r = (long)blockIdx.x * 16 + n;
+  if ((long)blockIdx.x * 16 >= rows) return;  // uniform
+  const bool live = r < rows;
+  const int K = a.K, kc = (K + 63) / 64;
+  float held[CI][16];
+#pragma unroll
+  for (int i = 0; i < CI; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {  // K % 32 == 0: a run of 8 is inside or outside as a whole
+      const int k = live ? 64 * (w + NW * i) + 16 * g + 8 * h : K;
+      const T* x = static_cast<const T*>(a.x);
+      load8<T, true>(x + (k < K ? frag_off((int)r, k, (int)a.ld / 32) : 0) - k, k, K, held[i] + 8 * h);
+    }
+  // f(chunk, first k, the 16 values) for every chunk of the wave
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < CI; ++i) f(w + NW * i, 64 * (w + NW * i) + 16 * g, held[i]);
+  };
+  // op over the values that the lanes of row n hold, in every wave, in a fixed order
+  auto over_row = [&](uint32_t v, int slot, auto op) {
+    const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = op(p[0], p[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = op(q[0], q[1]);
+    if (g == 0) s_row[slot][n][w] = v;
+    __syncthreads();
+    v = s_row[slot][n][0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) v = op(v, s_row[slot][n][i]);
+    return v;
+  };
+  auto add = [](uint32_t x, uint32_t y) { return __float_as_uint(__uint_as_float(x) + __uint_as_float(y)); };
+  float mean = 0.0f, rstd = 1.0f;
+  const bool ln = a.gamma != nullptr;
+  if (ln) {  // uniform
+    float s = 0.0f, q = 0.0f;
+    each([&](int, int, float* v) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s += v[j];  // zeros past K
+    });
+    mean = __uint_as_float(over_row(__float_as_uint(s), 0, add)) / (float)K;
+    each([&](int, int k, float* v) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float d = v[j] - mean;
+        q += k + j < K ? d * d : 0.0f;
+      }
+    });
+    rstd = 1.0f / sqrtf(__uint_as_float(over_row(__float_as_uint(q), 1, add)) / (float)K + a.eps);
+  }
+  auto param = [&](const void* p, int k) {
+    return a.param_f32 ? static_cast<const float*>(p)[k] : Elem<T>::f(static_cast<const T*>(p)[k]);
+  };
+  auto normed = [&](int k, float* v) {
+    if (!ln) return;
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      v[j] = k + j < K ? fmaf((v[j] - mean) * rstd, param(a.gamma, k + j), a.beta ? param(a.beta, k + j) : 0.0f) : 0.0f;
+  };
+  uint32_t top = 0;
+  each([&](int, int k, float* v) {
+    normed(k, v);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) top = max(top, mag(v[j]));
+  });
+  top = over_row(top, 2, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+  const float s = q_scale(top), inv = __fdiv_rn(1.0f, s);
+  if (live && threadIdx.x < 16) a.scale[r] = s;
+  const bool plain = __all(q_plain(s) || !live);
+  auto write = [&](auto byte) {
+    each([&](int c, int, float* v) {
+      if (c >= kc) return;  // uniform
+      uint32_t b[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) b[j] = byte(v[j]);
+      uint4 o;
+      o.x = low_bytes(b[0], b[1], b[2], b[3]);
+      o.y = low_bytes(b[4], b[5], b[6], b[7]);
+      o.z = low_bytes(b[8], b[9], b[10], b[11]);
+      o.w = low_bytes(b[12], b[13], b[14], b[15]);
+      if (live) reinterpret_cast<uint4*>(a.dst)[((size_t)blockIdx.x * kc + c) * 64 + lane] = o;
+    });
+  };
+  // uniform per wave
+  if (!plain) write([&](float v) { return (uint32_t)q_value(v, s); });
+  else if (sizeof(T) == 2 && !ln) write([&](float v) { return q_byte<true>(v, s, inv); });
+  else write([&](float v) { return q_byte<false>(v, s, inv); });
+}
+
+template <class T>
+hipError_t launch_tile_t(const QRowsArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.rows + 15) / 16));
+  if (a.K <= 512) return launch_k(q_tile_kernel<T, 8, 1>, grid, dim3(512), 0, s, a);
+  if (a.K <= 1024) return launch_k(q_tile_kernel<T, 16, 1>, grid, dim3(1024), 0, s, a);
+  if (a.K <= 2048) return launch_k(q_tile_kernel<T, 16, 2>, grid, dim3(1024), 0, s, a);
+  return hipErrorInvalidValue;  // the widest model (kMaxDim)
 }
 
 template <class T, bool VEC>
@@ -329,8 +438,9 @@ __global__ __launch_bounds__(kQWaves * 64) void q_gemm_kernel(GemmArgs a) {
       for (int i = 1; i < kQWaves; ++i) sum += part[i][w][lane];
       const float4 cs = *reinterpret_cast<const float4*>(a.col_scale + col), bi = *reinterpret_cast<const float4*>(a.bias + col);
       ResRun<T, 4> res;
-      if (q8_wide<EPI>() && a.resid) res.load(static_cast<const T*>(a.resid) + (size_t)row * a.res_ld + col);
-      q8_store<T, 4, q8_wide<EPI>()>(a, row, col, true, &sum, a.row_scale[row], &cs, &bi, res);
+      if (q8_wide<EPI>() && a.resid) res.load(q8_res<T, 4>(a, q8_down<EPI>(), row, col));
+      if constexpr (q8_down<EPI>()) q8_down_store<T, 4>(a, row, col, true, &sum, a.row_scale[row], &cs, &bi, res, a.rows[row]);
+      else q8_store<T, 4, q8_wide<EPI>()>(a, row, col, true, &sum, a.row_scale[row], &cs, &bi, res);
     }
     __syncthreads();  // `part` is written again
   }
@@ -375,7 +485,8 @@ hipError_t launch_gemm_e(const GemmArgs& a, int expected, int rows, hipStream_t 
 }  // namespace
 
 hipError_t launch_q_rows(const QRowsArgs& a, hipStream_t s) {
-  const bool vec = a.frag || (a.K % 8 == 0 && a.ld % 8 == 0 && (uintptr_t)a.x % 16 == 0);
+  if (a.frag) return a.dtype ? launch_tile_t<uint16_t>(a, s) : launch_tile_t<float>(a, s);
+  const bool vec = a.K % 8 == 0 && (uintptr_t)a.ld * (a.dtype ? 2 : 4) % 16 == 0 && (uintptr_t)a.x % 16 == 0;
   if (a.dtype) return vec ? launch_rows_t<uint16_t, true>(a, s) : launch_rows_t<uint16_t, false>(a, s);
   return vec ? launch_rows_t<float, true>(a, s) : launch_rows_t<float, false>(a, s);
 }
@@ -383,6 +494,10 @@ hipError_t launch_q_rows(const QRowsArgs& a, hipStream_t s) {
 hipError_t launch_q_pack(const QPackArgs& a, hipStream_t s) {
   if (a.dtype == 2) return launch_pack_t<int8_t>(a, s);
   return a.dtype ? launch_pack_t<uint16_t>(a, s) : launch_pack_t<float>(a, s);
+}
+
+hipError_t launch_q_down(const GemmArgs& a, int out_f32, int expected, int rows, hipStream_t s) {
+  return out_f32 ? launch_gemm_e<EPI_QDOWN_F32>(a, expected, rows, s) : launch_gemm_e<EPI_QDOWN_BF>(a, expected, rows, s);
 }
 
 hipError_t launch_q_gemm(const GemmArgs& a, int out_f32, int expected, int rows, hipStream_t s) {

@@ -142,6 +142,9 @@ hipError_t launch_q_pack(const QPackArgs& a, hipStream_t s);
 hipError_t launch_q_rows(const QRowsArgs& a, hipStream_t s);
 // out = act(rows x weights) (+ resid): `expected` rows to tune for, at most `rows`
 hipError_t launch_q_gemm(const GemmArgs& a, int out_f32, int expected, int rows, hipStream_t s);
+// the encoder's down projection: out = S(resid + S(rows x weights + bias)), both in
+// operand order, also written to the cache's X^{layer + 1}
+hipError_t launch_q_down(const GemmArgs& a, int out_f32, int expected, int rows, hipStream_t s);
 
 hipError_t launch_qk(const QkArgs& a, hipStream_t s);
 hipError_t launch_qk_layer(const QkLayerArgs& a, int rows, hipStream_t s);
