@@ -644,7 +644,6 @@ incvit_status run_layers(incvit_handle* h, const Views& views, int B, const WsLa
       if (up) {
         qa.gamma = fptr(h, P.ln2_g);
         qa.beta = fptr(h, P.ln2_b);
-        qa.param_f32 = 1;
         qa.eps = sh.eps;
       }
       qa.dst = ws + wl.q8;

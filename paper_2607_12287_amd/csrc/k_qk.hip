@@ -22,54 +22,51 @@ namespace incvit {
 
 namespace {
 
-// V consecutive values as floats
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+// V consecutive values as floats (global memory: a cache's address comes from
+// memory, and would be taken for any address space)
 template <class T, int V> struct Run;
-template <> struct Run<uint16_t, 8> {
-  uint4 v;
-  __device__ void load(const uint16_t* p) { v = *reinterpret_cast<const uint4*>(p); }
-  __device__ float get(int i) const {
-    const uint32_t w = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
-    return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+template <int V> struct Run<uint16_t, V> {
+  uint32_t w[V / 2];
+  __device__ void load(const uint16_t* p) {
+    if constexpr (V == 8) *reinterpret_cast<u32x4_t*>(w) = *(const INCVIT_GLOBAL u32x4_t*)p;
+    else if constexpr (V == 4) *reinterpret_cast<u32x2_t*>(w) = *(const INCVIT_GLOBAL u32x2_t*)p;
+    else w[0] = *(const INCVIT_GLOBAL uint32_t*)p;
   }
+  __device__ float get(int i) const { return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); }
   __device__ static void store(uint16_t* p, const float* f) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(f2bf2(f[0], f[1]), f2bf2(f[2], f[3]), f2bf2(f[4], f[5]), f2bf2(f[6], f[7]));
+    if constexpr (V == 8) *(INCVIT_GLOBAL u32x4_t*)p = u32x4_t{f2bf2(f[0], f[1]), f2bf2(f[2], f[3]), f2bf2(f[4], f[5]), f2bf2(f[6], f[7])};
+    else if constexpr (V == 4) *(INCVIT_GLOBAL u32x2_t*)p = u32x2_t{f2bf2(f[0], f[1]), f2bf2(f[2], f[3])};
+    else *(INCVIT_GLOBAL uint32_t*)p = f2bf2(f[0], f[1]);
   }
 };
-template <> struct Run<uint16_t, 4> {
-  uint2 v;
-  __device__ void load(const uint16_t* p) { v = *reinterpret_cast<const uint2*>(p); }
-  __device__ float get(int i) const {
-    const uint32_t w = i < 2 ? v.x : v.y;
-    return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+template <int V> struct Run<float, V> {
+  float v[V];
+  __device__ void load(const float* p) {
+    if constexpr (V == 8) {
+      *reinterpret_cast<f32x4_t*>(v) = ((const INCVIT_GLOBAL f32x4_t*)p)[0];
+      *reinterpret_cast<f32x4_t*>(v + 4) = ((const INCVIT_GLOBAL f32x4_t*)p)[1];
+    } else if constexpr (V == 4) {
+      *reinterpret_cast<f32x4_t*>(v) = *(const INCVIT_GLOBAL f32x4_t*)p;
+    } else {
+      *reinterpret_cast<f32x2_t*>(v) = *(const INCVIT_GLOBAL f32x2_t*)p;
+    }
   }
-  __device__ static void store(uint16_t* p, const float* f) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(f2bf2(f[0], f[1]), f2bf2(f[2], f[3]));
+  __device__ float get(int i) const { return v[i]; }
+  __device__ static void store(float* p, const float* f) {
+    if constexpr (V == 4) *(INCVIT_GLOBAL f32x4_t*)p = f32x4_t{f[0], f[1], f[2], f[3]};
+    else *(INCVIT_GLOBAL f32x2_t*)p = f32x2_t{f[0], f[1]};
   }
 };
-template <> struct Run<float, 4> {
-  float4 v;
-  __device__ void load(const float* p) { v = *reinterpret_cast<const float4*>(p); }
-  __device__ float get(int i) const { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-  __device__ static void store(float* p, const float* f) { *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]); }
-};
-template <> struct Run<uint16_t, 2> {
-  uint32_t v;
-  __device__ void load(const uint16_t* p) { v = *reinterpret_cast<const uint32_t*>(p); }
-  __device__ float get(int i) const { return __uint_as_float(i ? v & 0xffff0000u : v << 16); }
-  __device__ static void store(uint16_t* p, const float* f) { *reinterpret_cast<uint32_t*>(p) = f2bf2(f[0], f[1]); }
-};
-template <> struct Run<float, 2> {
-  float2 v;
-  __device__ void load(const float* p) { v = *reinterpret_cast<const float2*>(p); }
-  __device__ float get(int i) const { return i ? v.y : v.x; }
-  __device__ static void store(float* p, const float* f) { *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]); }
-};
-template <class T> struct Run<T, 1> {
+template <class T> struct Run1 {
   T v;
-  __device__ void load(const T* p) { v = *p; }
+  __device__ void load(const T* p) { v = *gbl(p); }
   __device__ float get(int) const { return Elem<T>::f(v); }
-  __device__ static void store(T* p, const float* f) { *p = Elem<T>::cv(f[0]); }
+  __device__ static void store(T* p, const float* f) { *gbl(p) = Elem<T>::cv(f[0]); }
 };
+template <> struct Run<uint16_t, 1> : Run1<uint16_t> {};
+template <> struct Run<float, 1> : Run1<float> {};
 // V pairs of (cos, sin): 2 V floats
 template <int V>
 struct Turns {
@@ -234,11 +231,11 @@ Units units_of(int hq, int hk, int hp) {
   return u;
 }
 template <int GL>
-__device__ __forceinline__ bool unit_of(const Units& u, uint32_t& row, int& unit) {
+__device__ __forceinline__ bool unit_of(const Units& u, int bx, int by, uint32_t& row, int& unit) {
   const int g = threadIdx.x / GL;
   const int rl = (int)(((float)g + 0.5f) * __builtin_amdgcn_rcpf((float)u.upb));  // g / upb: both below 256
-  row = blockIdx.x * (uint32_t)u.rpb + rl;
-  unit = blockIdx.y * u.upb + g - rl * u.upb;
+  row = bx * (uint32_t)u.rpb + rl;
+  unit = by * u.upb + g - rl * u.upb;
   return rl < u.rpb && unit < u.per_row;
 }
 
@@ -252,7 +249,7 @@ __global__ __launch_bounds__(256) void qk_kernel(QkLaunch l) {
   const QkArgs& a = l.a;
   uint32_t r;
   int unit;
-  if (!unit_of<GL>(l.u, r, unit) || r >= a.rows) return;  // whole groups of lanes
+  if (!unit_of<GL>(l.u, blockIdx.x, blockIdx.y, r, unit) || r >= a.rows) return;  // whole groups of lanes
   const bool isk = unit >= l.u.uq;
   const QkSide s = isk ? a.k : a.q;
   const int h0 = (isk ? unit - l.u.uq : unit) * HP;
@@ -275,30 +272,44 @@ __global__ __launch_bounds__(256) void qk_kernel(QkLaunch l) {
                                  [&](int i, int d) { return out + i * s.out_head + d; });
 }
 
+// The encoder's rows: queries in the compact buffer, keys where the QKV
+// projection left them in the cache.  A chunk's V values (4 or 8) lie inside one
+// run of 8 of the cache's operand order (k_elem), so they are consecutive there
+// too.  The first `qblocks` workgroups take the queries, rows of heads after one
+// another; the others the keys, 16 rows of a few heads, since the same run of 4
+// tokens is 64 consecutive bytes there (8192 rows of 16 heads of 64: 28 -> 17.6 us).
 struct QkLayerLaunch {
   QkLayerArgs a;
-  Units u;
+  Units u;       // of the queries
+  int qblocks;
 };
 
-// The encoder's rows: queries in the compact buffer, keys where the QKV
-// projection left them in the cache.  A chunk's 4 values lie inside one run of 8
-// of the cache's operand order (k_elem), so they are consecutive there too.
-template <class T, int GL, int HP>
+template <class T, int V, int GL, int HP>
 __global__ __launch_bounds__(256) void qk_layer_kernel(QkLayerLaunch l) {
   const QkLayerArgs& a = l.a;
-  uint32_t r;
-  int unit;
-  if (!unit_of<GL>(l.u, r, unit) || r >= (uint32_t)a.meta->m) return;
-  const RowInfo ri = a.rows[r];
-  const int dh = a.sh.dh;
-  const bool isk = unit >= l.u.uq;
-  const int h0 = (isk ? unit - l.u.uq : unit) * HP;
-  T* q = static_cast<T*>(a.q) + (size_t)r * a.sh.D + h0 * dh;
-  T* k = reinterpret_cast<T*>(ri.cache + a.cl.k + (size_t)a.layer * a.cl.kv_layer);
+  const int dh = a.sh.dh, H = a.sh.H;
+  const uint32_t m = (uint32_t)a.meta->m;
   const HeadSpec spec{dh / 2, a.table ? dh / 2 : 0, a.adjacent, a.norm, a.eps, 1.0f / (float)dh};
-  auto at = [&](int i, int d) { return isk ? k + k_elem(a.sh, h0 + i, ri.tok, d) : q + i * dh + d; };
-  some_heads<T, float, 4, GL, 1, HP>(spec, threadIdx.x % GL, a.sh.H - h0, isk ? a.k_gamma : a.q_gamma,
-                                     isk ? a.k_beta : a.q_beta, a.table + (size_t)ri.tok * dh, at, at);
+  const int lane = threadIdx.x % GL;
+  if ((int)blockIdx.x < l.qblocks) {  // uniform
+    uint32_t r;
+    int unit;
+    const int ny = (l.u.per_row + l.u.upb - 1) / l.u.upb;
+    if (!unit_of<GL>(l.u, (int)blockIdx.x / ny, (int)blockIdx.x % ny, r, unit) || r >= m) return;
+    T* q = static_cast<T*>(a.q) + (size_t)r * a.sh.D + unit * HP * dh;
+    auto at = [&](int i, int d) { return q + i * dh + d; };
+    some_heads<T, float, V, GL, 1, HP>(spec, lane, H - unit * HP, a.q_gamma, a.q_beta, a.table + (size_t)a.rows[r].tok * dh, at, at);
+    return;
+  }
+  constexpr int G = 256 / GL, HB = (G + 15) / 16;  // heads per workgroup
+  const int kb = blockIdx.x - l.qblocks, hb = (H + HB - 1) / HB, g = threadIdx.x / GL;
+  const uint32_t r = (uint32_t)(kb / hb) * 16 + g % 16;
+  const int h = kb % hb * HB + g / 16;
+  if (r >= m || h >= H) return;
+  const RowInfo ri = a.rows[r];
+  T* k = reinterpret_cast<T*>(ri.cache + a.cl.k + (size_t)a.layer * a.cl.kv_layer);
+  auto at = [&](int, int d) { return k + k_elem(a.sh, h, ri.tok, d); };
+  some_heads<T, float, V, GL, 1, 1>(spec, lane, 1, a.k_gamma, a.k_beta, a.table + (size_t)ri.tok * dh, at, at);
 }
 
 // Two heads of a row to a group of lanes where that still leaves every SIMD two
@@ -359,24 +370,28 @@ hipError_t launch_qk(const QkArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_qk_layer(const QkLayerArgs& a, int rows, hipStream_t s) {
-  const int H = a.sh.H, chunks = a.sh.dh / 8;
-  auto go = [&](auto t, auto gl, auto hp) {
+  const int H = a.sh.H;
+  auto go = [&](auto t, auto v, auto gl, auto hp) {
     using T = decltype(t);
-    constexpr int GL = decltype(gl)::value, HP = decltype(hp)::value;
-    QkLayerLaunch l{a, units_of<GL>(H, H, HP)};
-    const dim3 grid((unsigned)((rows + l.u.rpb - 1) / l.u.rpb), (l.u.per_row + l.u.upb - 1) / l.u.upb);
-    return launch_k(qk_layer_kernel<T, GL, HP>, grid, dim3(256), 0, s, l);
+    constexpr int V = decltype(v)::value, GL = decltype(gl)::value, HP = decltype(hp)::value, HB = (256 / GL + 15) / 16;
+    QkLayerLaunch l{a, units_of<GL>(H, 0, HP), 0};
+    l.qblocks = (rows + l.u.rpb - 1) / l.u.rpb * ((l.u.per_row + l.u.upb - 1) / l.u.upb);
+    const unsigned kblocks = (unsigned)(rows + 15) / 16 * ((H + HB - 1) / HB);
+    return launch_k(qk_layer_kernel<T, V, GL, HP>, dim3(l.qblocks + kblocks), dim3(256), 0, s, l);
   };
-  auto heads = [&](auto t, auto gl) {
-    if (many_heads(rows, H, H, decltype(gl)::value)) return go(t, gl, std::integral_constant<int, 2>{});
-    return go(t, gl, std::integral_constant<int, 1>{});
+  auto heads = [&](auto t, auto v, auto gl) {
+    if (many_heads(rows, H, H, decltype(gl)::value)) return go(t, v, gl, std::integral_constant<int, 2>{});
+    return go(t, v, gl, std::integral_constant<int, 1>{});
   };
-  auto lanes = [&](auto t) {
-    if (chunks <= 4) return heads(t, std::integral_constant<int, 4>{});
-    if (chunks <= 8) return heads(t, std::integral_constant<int, 8>{});
-    return heads(t, std::integral_constant<int, 16>{});
+  auto lanes = [&](auto t, auto v) {
+    const int chunks = a.sh.dh / 2 / decltype(v)::value;
+    if (chunks <= 4) return heads(t, v, std::integral_constant<int, 4>{});
+    if (chunks <= 8) return heads(t, v, std::integral_constant<int, 8>{});
+    return heads(t, v, std::integral_constant<int, 16>{});
   };
-  return a.sh.dtype ? lanes(uint16_t{}) : lanes(float{});
+  if (!a.sh.dtype) return lanes(float{}, std::integral_constant<int, 4>{});
+  if (a.sh.dh % 16 == 0) return lanes(uint16_t{}, std::integral_constant<int, 8>{});
+  return lanes(uint16_t{}, std::integral_constant<int, 4>{});
 }
 
 }  // namespace incvit

@@ -55,30 +55,38 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
 }
 __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// 8 values of a row from k on (fewer where the row ends: zeros)
-template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, int k, int K, float* v) {
-  if constexpr (VEC) {  // K % 8 == 0, 16-byte aligned
-    if (k < K) {
-      if constexpr (std::is_same<T, float>::value) {
-        const float4 a = *reinterpret_cast<const float4*>(p + k), b = *reinterpret_cast<const float4*>(p + k + 4);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-      } else {
-        const uint4 u = *reinterpret_cast<const uint4*>(p + k);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// 8 values from p on, or zeros: the load runs either way (p is readable), so that
+// a lane's loads go out together.
+template <class T>
+__device__ __forceinline__ void load8(const T* p, bool any, float* v) {
+  if constexpr (std::is_same<T, float>::value) {
+    const f32x4_t a = *(const INCVIT_GLOBAL f32x4_t*)p, b = *(const INCVIT_GLOBAL f32x4_t*)(p + 4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[2 * i] = __uint_as_float(w[i] << 16);
-          v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-      }
-      return;
+    for (int i = 0; i < 4; ++i) {
+      v[i] = any ? a[i] : 0.0f;
+      v[4 + i] = any ? b[i] : 0.0f;
     }
+  } else {
+    const u32x4_t u = *(const INCVIT_GLOBAL u32x4_t*)p;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = any ? u[i] : 0u;
+      v[2 * i] = __uint_as_float(w << 16);
+      v[2 * i + 1] = __uint_as_float(w & 0xffff0000u);
+    }
+  }
+}
+// 8 values of a row of K from k on, zeros past K.  VEC: K % 8 == 0, 16-byte aligned.
+template <class T, bool VEC>
+__device__ __forceinline__ void row8(const T* row, int k, int K, float* v) {
+  if constexpr (VEC) {
+    load8<T>(row + min(k, K - 8), k < K, v);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = k + i < K ? Elem<T>::f(p[k + i]) : 0.0f;
+    for (int i = 0; i < 8; ++i) {
+      const T x = *gbl(row + min(k + i, K - 1));
+      v[i] = k + i < K ? Elem<T>::f(x) : 0.0f;
+    }
   }
 }
 
@@ -98,10 +106,8 @@ __global__ __launch_bounds__(256 * WPR) void q_rows_kernel(QRowsArgs a) {
   const bool live = r < rows;                // uniform per wave
   const int K = a.K, kc = (K + 63) / 64;
   const T* x = static_cast<const T*>(a.x);
-  auto fetch = [&](int i, float* v) {  // the lane's i-th run of 8
-    const int k = live ? 8 * (lane + 64 * (wk + WPR * i)) : K;
-    load8<T, VEC>(x + (size_t)r * a.ld, k, K, v);
-  };
+  const T* row = x + (size_t)min(r, rows - 1) * a.ld;
+  auto fetch = [&](int i, float* v) { row8<T, VEC>(row, 8 * (lane + 64 * (wk + WPR * i)), K, v); };  // the lane's i-th run of 8
   constexpr int NH = CH > 0 ? CH : 1;
   const int runs = CH > 0 ? CH : (kc * 8 + 64 * WPR - 1) / (64 * WPR);
   float held[NH][8];
@@ -151,14 +157,15 @@ __global__ __launch_bounds__(256 * WPR) void q_rows_kernel(QRowsArgs a) {
     });
     rstd = 1.0f / sqrtf(row_sum(q, s_sq) / (float)K + a.eps);
   }
-  auto param = [&](const void* p, int k) {
-    return a.param_f32 ? static_cast<const float*>(p)[k] : Elem<T>::f(static_cast<const T*>(p)[k]);
-  };
   auto normed = [&](int k, float* v) {
     if (!ln) return;
+    float gm[8], bt[8];
+    row8<T, VEC>(static_cast<const T*>(a.gamma), k, K, gm);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      v[j] = k + j < K ? fmaf((v[j] - mean) * rstd, param(a.gamma, k + j), a.beta ? param(a.beta, k + j) : 0.0f) : 0.0f;
+    for (int j = 0; j < 8; ++j) bt[j] = 0.0f;
+    if (a.beta) row8<T, VEC>(static_cast<const T*>(a.beta), k, K, bt);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = k + j < K ? fmaf((v[j] - mean) * rstd, gm[j], bt[j]) : 0.0f;
   };
   uint32_t top = 0;
   each([&](int k, float* v) {
@@ -195,33 +202,43 @@ __global__ __launch_bounds__(256 * WPR) void q_rows_kernel(QRowsArgs a) {
 
 
 // Rows in operand order (the encoder's H: 16 rows x 32 columns to a kilobyte of
-// bf16, frag_off): a tile of 16 rows to a workgroup of NW waves.  Lane 16 g + n
+// bf16, frag_off) behind their LayerNorm: a tile of 16 rows to a workgroup of NW waves.  Lane 16 g + n
 // works on row n as the product will hold it, values 64 c + 16 g .. + 15 of the
 // CI chunks c = w, w + NW, ... (K <= 64 NW CI), so a wave reads and writes whole
 // runs of 256 bytes; a wave per row, as above, would use 16 bytes of every line
-// that it touches (8192 rows of 1024: 33 us against T_FRAG).
+// that it touches (8192 rows of 1024: 33 us against 10).
 template <class T, int NW, int CI>
 __global__ __launch_bounds__(64 * NW) void q_tile_kernel(QRowsArgs a) {
   __shared__ uint32_t s_row[3][16][NW];
+  __shared__ float4 s_gain[kMaxDim / 4], s_shift[kMaxDim / 4];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long rows = a.meta ? a.meta->m : a.rows, r = (long)blockIdx.x * 16 + n;
-  if ((long)blockIdx.x * 16 >= rows) return;  // uniform
-  const bool live = r < rows;
   const int K = a.K, kc = (K + 63) / 64;
+  const long r = (long)blockIdx.x * 16 + n;
+  // the first rows, the likely ones, load before the row count is read (the
+  // compact rows are padded past every launched one); the LayerNorm's gains and
+  // shifts (fp32) go to LDS beside them
+  const bool ahead = blockIdx.x < 8;  // uniform
+  if (!ahead && (long)blockIdx.x * 16 >= a.meta->m) return;
   float held[CI][16];
 #pragma unroll
   for (int i = 0; i < CI; ++i)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {  // K % 32 == 0: a run of 8 is inside or outside as a whole
-      const int k = live ? 64 * (w + NW * i) + 16 * g + 8 * h : K;
-      const T* x = static_cast<const T*>(a.x);
-      load8<T, true>(x + (k < K ? frag_off((int)r, k, (int)a.ld / 32) : 0) - k, k, K, held[i] + 8 * h);
+      const int k = 64 * (w + NW * i) + 16 * g + 8 * h;
+      load8<T>(static_cast<const T*>(a.x) + frag_off((int)r, min(k, K - 8), (int)a.ld / 32), k < K, held[i] + 8 * h);
     }
-  // f(chunk, first k, the 16 values) for every chunk of the wave
+  if ((int)threadIdx.x < K / 4) {
+    s_gain[threadIdx.x] = static_cast<const float4*>(a.gamma)[threadIdx.x];
+    s_shift[threadIdx.x] = static_cast<const float4*>(a.beta)[threadIdx.x];
+  }
+  const long rows = a.meta->m;
+  if ((long)blockIdx.x * 16 >= rows) return;  // uniform
+  const bool live = r < rows;
+  // f(i, first k, the 16 values) for every chunk w + NW i of the wave
   auto each = [&](auto f) {
 #pragma unroll
-    for (int i = 0; i < CI; ++i) f(w + NW * i, 64 * (w + NW * i) + 16 * g, held[i]);
+    for (int i = 0; i < CI; ++i) f(i, 64 * (w + NW * i) + 16 * g, held[i]);
   };
   // op over the values that the lanes of row n hold, in every wave, in a fixed order
   auto over_row = [&](uint32_t v, int slot, auto op) {
@@ -237,45 +254,40 @@ __global__ __launch_bounds__(64 * NW) void q_tile_kernel(QRowsArgs a) {
     return v;
   };
   auto add = [](uint32_t x, uint32_t y) { return __float_as_uint(__uint_as_float(x) + __uint_as_float(y)); };
-  float mean = 0.0f, rstd = 1.0f;
-  const bool ln = a.gamma != nullptr;
-  if (ln) {  // uniform
-    float s = 0.0f, q = 0.0f;
-    each([&](int, int, float* v) {
+  float s = 0.0f, q = 0.0f;
+  each([&](int, int, float* v) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) s += v[j];  // zeros past K
-    });
-    mean = __uint_as_float(over_row(__float_as_uint(s), 0, add)) / (float)K;
-    each([&](int, int k, float* v) {
+    for (int j = 0; j < 16; ++j) s += v[j];  // zeros past K
+  });
+  const float mean = __uint_as_float(over_row(__float_as_uint(s), 0, add)) / (float)K;
+  each([&](int, int k, float* v) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float d = v[j] - mean;
-        q += k + j < K ? d * d : 0.0f;
-      }
-    });
-    rstd = 1.0f / sqrtf(__uint_as_float(over_row(__float_as_uint(q), 1, add)) / (float)K + a.eps);
-  }
-  auto param = [&](const void* p, int k) {
-    return a.param_f32 ? static_cast<const float*>(p)[k] : Elem<T>::f(static_cast<const T*>(p)[k]);
-  };
-  auto normed = [&](int k, float* v) {
-    if (!ln) return;
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-      v[j] = k + j < K ? fmaf((v[j] - mean) * rstd, param(a.gamma, k + j), a.beta ? param(a.beta, k + j) : 0.0f) : 0.0f;
-  };
+    for (int j = 0; j < 16; ++j) {
+      const float d = v[j] - mean;
+      q += k < K ? d * d : 0.0f;  // K % 32 == 0
+    }
+  });
+  const float rstd = 1.0f / sqrtf(__uint_as_float(over_row(__float_as_uint(q), 1, add)) / (float)K + a.eps);
   uint32_t top = 0;
   each([&](int, int k, float* v) {
-    normed(k, v);
+    if (k >= K) return;  // zeros
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const float4 gm = s_gain[k / 4 + m], bm = s_shift[k / 4 + m];
+      const float gv[4] = {gm.x, gm.y, gm.z, gm.w}, bv[4] = {bm.x, bm.y, bm.z, bm.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[4 * m + j] = fmaf((v[4 * m + j] - mean) * rstd, gv[j], bv[j]);
+    }
 #pragma unroll
     for (int j = 0; j < 16; ++j) top = max(top, mag(v[j]));
   });
   top = over_row(top, 2, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-  const float s = q_scale(top), inv = __fdiv_rn(1.0f, s);
-  if (live && threadIdx.x < 16) a.scale[r] = s;
-  const bool plain = __all(q_plain(s) || !live);
+  const float sc = q_scale(top), inv = __fdiv_rn(1.0f, sc);
+  if (live && threadIdx.x < 16) a.scale[r] = sc;
+  const bool plain = __all(q_plain(sc) || !live);
   auto write = [&](auto byte) {
-    each([&](int c, int, float* v) {
+    each([&](int i, int, float* v) {
+      const int c = w + NW * i;
       if (c >= kc) return;  // uniform
       uint32_t b[16];
 #pragma unroll
@@ -289,9 +301,8 @@ __global__ __launch_bounds__(64 * NW) void q_tile_kernel(QRowsArgs a) {
     });
   };
   // uniform per wave
-  if (!plain) write([&](float v) { return (uint32_t)q_value(v, s); });
-  else if (sizeof(T) == 2 && !ln) write([&](float v) { return q_byte<true>(v, s, inv); });
-  else write([&](float v) { return q_byte<false>(v, s, inv); });
+  if (!plain) write([&](float v) { return (uint32_t)q_value(v, sc); });
+  else write([&](float v) { return q_byte<false>(v, sc, inv); });
 }
 
 template <class T>
@@ -486,7 +497,7 @@ hipError_t launch_gemm_e(const GemmArgs& a, int expected, int rows, hipStream_t 
 
 hipError_t launch_q_rows(const QRowsArgs& a, hipStream_t s) {
   if (a.frag) return a.dtype ? launch_tile_t<uint16_t>(a, s) : launch_tile_t<float>(a, s);
-  const bool vec = a.K % 8 == 0 && (uintptr_t)a.ld * (a.dtype ? 2 : 4) % 16 == 0 && (uintptr_t)a.x % 16 == 0;
+  const bool vec = a.K % 8 == 0 && ((uintptr_t)a.ld * (a.dtype ? 2 : 4) | (uintptr_t)a.x | (uintptr_t)a.gamma | (uintptr_t)a.beta) % 16 == 0;
   if (a.dtype) return vec ? launch_rows_t<uint16_t, true>(a, s) : launch_rows_t<uint16_t, false>(a, s);
   return vec ? launch_rows_t<float, true>(a, s) : launch_rows_t<float, false>(a, s);
 }

@@ -128,14 +128,14 @@ struct QPackArgs {
 struct QRowsArgs {
   const void* x;        // [rows][ld], or with `frag` 16 x 32 operand order (frag_off) of `ld` columns
   long ld;
-  const void* gamma;    // LayerNorm before the quantisation, or null
-  const void* beta;     // (fp32 where param_f32, else the rows' type)
+  const void* gamma;    // LayerNorm before the quantisation: of the rows' type, or null;
+  const void* beta;     // with `frag` fp32, 16-byte aligned and both there
   float eps;
   char* dst;            // QRowsLayout's kilobytes
   float* scale;
   const Meta* meta;     // rows on the device, or null
   long rows;
-  int K, dtype, frag, param_f32;
+  int K, dtype, frag;
 };
 
 hipError_t launch_q_pack(const QPackArgs& a, hipStream_t s);
