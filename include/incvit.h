@@ -434,9 +434,9 @@ incvit_status incvit_qlinear_quantize_rows(int32_t dtype, int64_t rows, int32_t 
 
 /* The product of quantised rows with packed weights.  out: rows of N values of
  * `dtype`, out_stride >= N elements apart; residual: likewise, added after act,
- * or NULL; it may be `out` with the same stride.  gelu: 0 or 1.  Any strides and
- * alignment of whole elements; multiples of four (and 16-byte aligned rows)
- * take the fast path. */
+ * or NULL; it may be `out` with the same stride; out overlaps nothing else.
+ * gelu: 0 or 1.  Any strides and alignment of whole elements; N a multiple of 8
+ * (fp32: 4) and 16-byte aligned rows take the fast path. */
 incvit_status incvit_qlinear_multiply(int32_t dtype, int64_t rows, int32_t K, int32_t N,
                                       const void* qrows, const void* weights, int32_t gelu,
                                       const void* residual, int64_t res_stride, void* out,
@@ -444,7 +444,8 @@ incvit_status incvit_qlinear_multiply(int32_t dtype, int64_t rows, int32_t K, in
 
 /* Both in one call: rows of `dtype` quantised into workspace
  * (incvit_qlinear_rows_bytes(rows, K) bytes, 256-byte aligned, the call's own
- * until it has run on `stream`), then multiplied. */
+ * until it has run on `stream`), then multiplied; a few tokens (up to 8 rows) in
+ * one launch, with the same bits. */
 incvit_status incvit_qlinear(int32_t dtype, int64_t rows, int32_t K, int32_t N, const void* x,
                              int64_t x_stride, const void* weights, int32_t gelu,
                              const void* residual, int64_t res_stride, void* out,

@@ -203,6 +203,8 @@ struct GemmArgs {
   int m_host;              // rows, where meta is null
   int n;                   // output columns (Nout: rounded up to 16)
   int gelu;
+  long x_ld;               // rows that are quantised by the product itself (A): their stride,
+  int k;                   // and K
 };
 
 // Row kernel that finishes the split-K MLP down projection, one workgroup per

@@ -100,11 +100,9 @@ incvit_status q_rows(int32_t dtype, int64_t rows, int32_t K, const void* x, int6
   return launched(launch_q_rows(a, s), "qlinear_quantize_rows");
 }
 
-incvit_status q_multiply(int32_t dtype, int64_t rows, int32_t K, int32_t N, const void* qrows, const void* weights, int32_t gelu,
-                         const void* residual, int64_t res_stride, void* out, int64_t out_stride, hipStream_t s) {
-  const QRowsLayout rl(rows, K);
+// What a product has but its rows and outputs.
+GemmArgs q_args(int32_t K, int32_t N, const void* weights, int32_t gelu, int64_t res_stride, int64_t out_stride) {
   const QWeightsLayout wl(K, N);
-  const size_t eb = dtype == INCVIT_BF16 ? 2 : 4;
   const char* w = static_cast<const char*>(weights);
   GemmArgs a = {};
   a.W = w;
@@ -118,10 +116,18 @@ incvit_status q_multiply(int32_t dtype, int64_t rows, int32_t K, int32_t N, cons
   a.gelu = gelu;
   a.out_ld = (long)out_stride;
   a.res_ld = (long)res_stride;
+  return a;
+}
+
+incvit_status q_multiply(int32_t dtype, int64_t rows, int32_t K, int32_t N, const void* qrows, const void* weights, int32_t gelu,
+                         const void* residual, int64_t res_stride, void* out, int64_t out_stride, hipStream_t s) {
+  const QRowsLayout rl(rows, K);
+  const size_t eb = dtype == INCVIT_BF16 ? 2 : 4;
+  GemmArgs a = q_args(K, N, weights, gelu, res_stride, out_stride);
   const int64_t slab = q_slab(K);
   for (int64_t r = 0; r < rows; r += slab) {
     const int m = (int)(rows - r < slab ? rows - r : slab);
-    a.A = static_cast<const char*>(qrows) + (size_t)(r / 16) * wl.kc * 1024;
+    a.A = static_cast<const char*>(qrows) + (size_t)(r / 16) * a.kchunks * 1024;
     a.row_scale = reinterpret_cast<const float*>(static_cast<const char*>(qrows) + rl.scale) + r;
     a.out = static_cast<char*>(out) + (size_t)r * out_stride * eb;
     a.resid = residual ? static_cast<const char*>(residual) + (size_t)r * res_stride * eb : nullptr;
@@ -291,6 +297,16 @@ incvit_status incvit_qlinear(int32_t dtype, int64_t rows, int32_t K, int32_t N, 
   if ((st = check_x(dtype, x, x_stride, workspace)) != INCVIT_OK) return st;
   if ((st = check_out(dtype, rows, N, weights, gelu, residual, res_stride, out, out_stride)) != INCVIT_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (q_token_fits(rows, K)) {
+    GemmArgs a = q_args(K, N, weights, gelu, res_stride, out_stride);
+    a.A = x;
+    a.x_ld = (long)x_stride;
+    a.k = K;
+    a.out = out;
+    a.resid = residual;
+    a.m_host = (int)rows;
+    return launched(launch_q_token(a, dtype == INCVIT_F32, s), "qlinear");
+  }
   if ((st = q_rows(dtype, rows, K, x, x_stride, nullptr, nullptr, 0.0f, workspace, s)) != INCVIT_OK) return st;
   return q_multiply(dtype, rows, K, N, workspace, weights, gelu, residual, res_stride, out, out_stride, s);
 }

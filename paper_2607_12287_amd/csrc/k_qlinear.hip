@@ -457,6 +457,89 @@ __global__ __launch_bounds__(kQWaves * 64) void q_gemm_kernel(GemmArgs a) {
   }
 }
 
+// Up to 8 rows quantised by every workgroup for itself, a wave per row: one launch
+// for a few tokens.  A = x, rows on the host; the integers take rows * (64 kc +
+// 16) bytes of LDS (the 16 keep a fragment's rows on different banks).  The first
+// weights are on their way meanwhile.  HELD: a wave's row stays in registers
+// (bf16, 16-byte runs, K <= 2048), else it is read twice.
+template <int EPI, bool VEC, bool HELD>
+__global__ __launch_bounds__(kQWaves * 64) void q_token_kernel(GemmArgs a) {
+  using T = q8_out<EPI>;
+  constexpr int U = 3;
+  __shared__ i32x4_t part[kQWaves][64];
+  __shared__ float s_scale[kQWaves];
+  extern __shared__ __align__(16) char s_q[];
+  const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int M = a.m_host, K = a.k, kc = a.kchunks, cblk = blockIdx.x, pitch = 64 * kc + 16;
+  const u32x4_t* W = reinterpret_cast<const u32x4_t*>(a.W) + (size_t)cblk * kc * 64 + lane;
+  u32x4_t wf[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) wf[u] = W[(size_t)min(w + kQWaves * u, kc - 1) * 64];
+  if (w < M) {  // uniform
+    const T* row = static_cast<const T*>(a.A) + (size_t)w * a.x_ld;
+    auto write = [&](int k, const float* v, float s, float inv, bool plain) {
+      uint32_t b[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) b[j] = plain ? q_byte<sizeof(T) == 2>(v[j], s, inv) : (uint32_t)q_value(v[j], s);
+      *reinterpret_cast<uint2*>(s_q + w * pitch + k) = make_uint2(low_bytes(b[0], b[1], b[2], b[3]), low_bytes(b[4], b[5], b[6], b[7]));
+    };
+    uint32_t top = 0;
+    constexpr int RUNS = HELD ? 4 : 1;
+    float held[RUNS][8];
+    if constexpr (HELD) {
+#pragma unroll
+      for (int j = 0; j < RUNS; ++j) row8<T, VEC>(row, 8 * lane + 512 * j, K, held[j]);
+#pragma unroll
+      for (int j = 0; j < RUNS; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, mag(held[j][e]));
+    } else {
+      for (int k = 8 * lane; k < K; k += 512) {
+        row8<T, VEC>(row, k, K, held[0]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, mag(held[0][e]));
+      }
+    }
+    const float s = q_scale(lanes_max<64>(top)), inv = __fdiv_rn(1.0f, s);
+    if (lane == 0) s_scale[w] = s;
+    const bool plain = q_plain(s);  // uniform
+    if constexpr (HELD) {
+#pragma unroll
+      for (int j = 0; j < RUNS; ++j)
+        if (8 * lane + 512 * j < 64 * kc) write(8 * lane + 512 * j, held[j], s, inv, plain);
+    } else {
+      for (int k = 8 * lane; k < 64 * kc; k += 512) {
+        row8<T, VEC>(row, k, K, held[0]);  // from the L1
+        write(k, held[0], s, inv, plain);
+      }
+    }
+  }
+  __syncthreads();
+  i32x4_t acc = i32x4_t{0, 0, 0, 0};
+  const char* Ar = s_q + min(n, M - 1) * pitch + 16 * g;
+  for (int c0 = w; c0 < kc; c0 += kQWaves * U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (c0 + kQWaves * u < kc) mma_q8(acc, wf[u], *reinterpret_cast<const u32x4_t*>(Ar + 64 * (c0 + kQWaves * u)));  // uniform
+    if (c0 + kQWaves * U < kc) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) wf[u] = W[(size_t)min(c0 + kQWaves * (U + u), kc - 1) * 64];
+    }
+  }
+  part[w][lane] = acc;
+  __syncthreads();
+  const int col = cblk * 16 + 4 * g;
+  if (w > 0 || n >= M || col >= a.n) return;
+  i32x4_t sum = part[0][lane];
+#pragma unroll
+  for (int i = 1; i < kQWaves; ++i) sum += part[i][lane];
+  const float4 cs = *reinterpret_cast<const float4*>(a.col_scale + col), bi = *reinterpret_cast<const float4*>(a.bias + col);
+  ResRun<T, 4> res;
+  if (q8_wide<EPI>() && a.resid) res.load(q8_res<T, 4>(a, false, n, col));
+  q8_store<T, 4, q8_wide<EPI>()>(a, n, col, true, &sum, s_scale[n], &cs, &bi, res);
+}
+
 template <int EPI, int RT, int U>
 hipError_t launch_few(const GemmArgs& a0, int expected, hipStream_t s) {
   GemmArgs a = a0;
@@ -493,7 +576,38 @@ hipError_t launch_gemm_e(const GemmArgs& a, int expected, int rows, hipStream_t 
   return rt == 2 ? launch_few<EPI, 2, 4>(a, expected, s) : launch_few<EPI, 1, 4>(a, expected, s);
 }
 
+template <int EPI>
+hipError_t launch_token_e(const GemmArgs& a, hipStream_t s) {
+  constexpr bool F32 = std::is_same<q8_out<EPI>, float>::value;
+  const size_t lds = (size_t)a.m_host * (64 * a.kchunks + 16);
+  const dim3 grid(a.Nout / 16), block(kQWaves * 64);
+  const bool vec = a.k % 8 == 0 && ((uintptr_t)a.x_ld * (F32 ? 4 : 2) | (uintptr_t)a.A) % 16 == 0;
+  if constexpr (!F32) {
+    if (vec && a.k <= 2048) return launch_k(q_token_kernel<EPI, true, true>, grid, block, lds, s, a);
+  }
+  if (vec) return launch_k(q_token_kernel<EPI, true, false>, grid, block, lds, s, a);
+  return launch_k(q_token_kernel<EPI, false, false>, grid, block, lds, s, a);
+}
+
+// whether out (and the residual) take 16 bytes at once
+bool q_wide(const GemmArgs& a, int out_f32) {
+  const uintptr_t eb = out_f32 ? 4 : 2;
+  uintptr_t bits = (uintptr_t)a.out | (uintptr_t)a.resid | (uintptr_t)a.n * eb | (uintptr_t)a.out_ld * eb;
+  if (a.resid) bits |= (uintptr_t)a.res_ld * eb;
+  return bits % 16 == 0;
+}
+
 }  // namespace
+
+// Us per call, one launch against two: 1 x 1152 -> 4304 3.7 against 5.2, 8 rows 4.7
+// against 5.7 (16 rows, two to a wave: 6.5 against 5.8); 1 x 4304 -> 1152 6.8
+// against 7.1; and a launch of 3.5 us of the host's less.
+bool q_token_fits(int64_t rows, int K) { return rows <= 8 && rows * ((K + 63) / 64 * 64 + 16) <= 49152; }
+
+hipError_t launch_q_token(const GemmArgs& a, int f32, hipStream_t s) {
+  if (q_wide(a, f32)) return f32 ? launch_token_e<EPI_QF32>(a, s) : launch_token_e<EPI_QBF>(a, s);
+  return f32 ? launch_token_e<EPI_QF32_ANY>(a, s) : launch_token_e<EPI_QBF_ANY>(a, s);
+}
 
 hipError_t launch_q_rows(const QRowsArgs& a, hipStream_t s) {
   if (a.frag) return a.dtype ? launch_tile_t<uint16_t>(a, s) : launch_tile_t<float>(a, s);
@@ -512,11 +626,7 @@ hipError_t launch_q_down(const GemmArgs& a, int out_f32, int expected, int rows,
 }
 
 hipError_t launch_q_gemm(const GemmArgs& a, int out_f32, int expected, int rows, hipStream_t s) {
-  const uintptr_t eb = out_f32 ? 4 : 2;
-  uintptr_t bits = (uintptr_t)a.out | (uintptr_t)a.resid | (uintptr_t)a.n * eb | (uintptr_t)a.out_ld * eb;
-  if (a.resid) bits |= (uintptr_t)a.res_ld * eb;
-  if (bits % 16 == 0)
-    return out_f32 ? launch_gemm_e<EPI_QF32>(a, expected, rows, s) : launch_gemm_e<EPI_QBF>(a, expected, rows, s);
+  if (q_wide(a, out_f32)) return out_f32 ? launch_gemm_e<EPI_QF32>(a, expected, rows, s) : launch_gemm_e<EPI_QBF>(a, expected, rows, s);
   return out_f32 ? launch_gemm_e<EPI_QF32_ANY>(a, expected, rows, s) : launch_gemm_e<EPI_QBF_ANY>(a, expected, rows, s);
 }
 

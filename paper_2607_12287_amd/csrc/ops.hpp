@@ -142,6 +142,10 @@ hipError_t launch_q_pack(const QPackArgs& a, hipStream_t s);
 hipError_t launch_q_rows(const QRowsArgs& a, hipStream_t s);
 // out = act(rows x weights) (+ resid): `expected` rows to tune for, at most `rows`
 hipError_t launch_q_gemm(const GemmArgs& a, int out_f32, int expected, int rows, hipStream_t s);
+// A few rows quantised and multiplied in one launch (a.A = the rows): for which
+// sizes, and the launch.
+bool q_token_fits(int64_t rows, int K);
+hipError_t launch_q_token(const GemmArgs& a, int f32, hipStream_t s);
 // the encoder's down projection: out = S(resid + S(rows x weights + bias)), both in
 // operand order, also written to the cache's X^{layer + 1}
 hipError_t launch_q_down(const GemmArgs& a, int out_f32, int expected, int rows, hipStream_t s);

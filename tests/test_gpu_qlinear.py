@@ -203,6 +203,26 @@ def test_rows_behind_a_layernorm(rows, dtype, K):
     assert np.all(d <= bound * 1.01), (d / bound).max()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K,N", [(1152, 176), (2048, 40), (2056, 48), (5000, 33), (6144, 24), (1001, 50), (63, 8)])
+def test_a_few_tokens_in_one_launch(dtype, K, N):
+    """Up to 8 rows are quantised by the product itself: the same bits as in two steps, and as 9 rows that are not."""
+    x, w, b, r = make(9, K, N, dtype)
+    x[4] = 0.0
+    x[6, K - 1] = float("inf")
+    lin = incvit.QLinear(w, b)
+    nine = lin(x, residual=r)
+    for rows in (1, 2, 5, 7, 8):
+        got = lin(x[:rows], residual=r[:rows])
+        assert torch.equal(got.nan_to_num(7.0), nine[:rows].nan_to_num(7.0))
+        two = lin(incvit.quantize_rows(x[:rows]), residual=r[:rows])
+        assert torch.equal(got.nan_to_num(7.0), two.nan_to_num(7.0))
+    keep = x[:3].clone()
+    wide = torch.full((3, K + 5), float("nan"), dtype=x.dtype, device="cuda")  # what follows a row is not read into it
+    wide[:, :K] = keep
+    assert torch.equal(lin(wide[:, :K]), lin(keep))
+
+
 def test_quantised_rows_serve_products_of_other_widths():
     x, w, b, _ = make(50, 320, 96, "bf16")
     a, c = incvit.QLinear(w, b), incvit.QLinear(w[:, :40].contiguous())
