@@ -170,10 +170,10 @@ struct RowsArgs {  // commit: ref/X0/Z0 of the refreshed rows, row map
 };
 
 enum Epi { EPI_QKV = 0, EPI_FC1 = 1, EPI_PART = 2, EPI_RES = 3, EPI_ATT = 4, EPI_DOWN = 5,
-           // 8-bit products, bf16 or fp32 output: 16 bytes at once, or any strides and width
-           EPI_QBF = 6, EPI_QF32 = 7, EPI_QBF_ANY = 8, EPI_QF32_ANY = 9,
-           // and DOWN of 8-bit products
-           EPI_QDOWN_BF = 10, EPI_QDOWN_F32 = 11 };
+           // 8-bit products, bf16 or fp32 output: 16 bytes at once, or any strides and width;
+           // with a residual; and DOWN of 8-bit products
+           EPI_QBF = 6, EPI_QF32 = 7, EPI_QBF_ANY = 8, EPI_QF32_ANY = 9, EPI_QRES_BF = 10, EPI_QRES_F32 = 11,
+           EPI_QDOWN_BF = 12, EPI_QDOWN_F32 = 13 };
 
 // Fields in the order the kernel's prologue needs them, so that its argument
 // loads go out together.

@@ -99,8 +99,14 @@ template <int EPI>
 __host__ __device__ constexpr bool q8_down() {
   return EPI == EPI_QDOWN_BF || EPI == EPI_QDOWN_F32;
 }
+// a residual that is loaded ahead: with the epilogue's form, since loads under a
+// branch would have the compiler wait for every load and store at their use
 template <int EPI>
-using q8_out = std::conditional_t<EPI == EPI_QBF || EPI == EPI_QBF_ANY || EPI == EPI_QDOWN_BF, uint16_t, float>;
+__host__ __device__ constexpr bool q8_resid() {
+  return EPI >= EPI_QRES_BF;
+}
+template <int EPI>
+using q8_out = std::conditional_t<EPI == EPI_QBF || EPI == EPI_QBF_ANY || EPI == EPI_QRES_BF || EPI == EPI_QDOWN_BF, uint16_t, float>;
 template <int EPI>
 __host__ __device__ constexpr int gemm_waves() {
   return kGemmWaves;
@@ -200,6 +206,9 @@ struct ResRun {
     if constexpr (std::is_same<T, float>::value) return __uint_as_float(w[j]);
     else return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
   }
+  // 16-byte stores of bf16 go past the L2 of the XCD that made them (8192 x 1024 ->
+  // 4096 48.6 -> 46 us, 4096 x 768 -> 2304 15.5 -> 14.2, and what reads them next is
+  // no slower); stores of parts of lines must not
   __device__ __forceinline__ void store(T* p, const float* y) {
     if constexpr (std::is_same<T, float>::value) {
       *reinterpret_cast<float4*>(p) = make_float4(y[0], y[1], y[2], y[3]);
@@ -207,7 +216,7 @@ struct ResRun {
 #pragma unroll
       for (int j = 0; j < NC / 2; ++j) w[j] = f2bf2(y[2 * j], y[2 * j + 1]);
       if constexpr (sizeof(w) == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-      else *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+      else __builtin_nontemporal_store((u32x4_t{w[0], w[1], w[2], w[3]}), (INCVIT_GLOBAL u32x4_t*)p);
     }
   }
 };
@@ -237,7 +246,7 @@ __device__ __forceinline__ void q8_down_store(const GemmArgs& a, int row, int co
   o.store(static_cast<T*>(a.out) + frag_off(row, col, a.ldo / 32), y);
   o.store(x_row<T>(ri.cache, a.cl, a.sh, a.layer + 1, ri.tok) + col, y);
 }
-template <class T, int NC, bool WIDE>
+template <class T, int NC, bool WIDE, bool RES>
 __device__ __forceinline__ void q8_store(const GemmArgs& a, int row, int col, bool ok, const i32x4_t* acc, float rs,
                                          const float4* cs, const float4* cb, const ResRun<T, NC>& res) {
   float y[NC];
@@ -248,7 +257,7 @@ __device__ __forceinline__ void q8_store(const GemmArgs& a, int row, int col, bo
   }
   T* out = static_cast<T*>(a.out) + (size_t)row * a.out_ld + col;
   if constexpr (WIDE) {
-    if (a.resid) {  // uniform
+    if constexpr (RES) {
 #pragma unroll
       for (int j = 0; j < NC; ++j) y[j] += res.get(j);
     }

@@ -407,7 +407,7 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
       // residuals while the run before is worked on; loads run for every lane
       // (clamped) and only the stores are masked, as below.
       using TO = q8_out<EPI>;
-      constexpr bool WIDE = q8_wide<EPI>(), DOWN = q8_down<EPI>();
+      constexpr bool WIDE = q8_wide<EPI>(), DOWN = q8_down<EPI>(), RES = q8_resid<EPI>();
       constexpr int PB = std::is_same<TO, uint16_t>::value && TC % 2 == 0 ? 2 : 1, NC = 4 * PB, NP = TC / PB;
       float rs[TR];
 #pragma unroll
@@ -429,7 +429,7 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
         }
       };
       auto load_res = [&](int i) {  // run i: columns p = i / TR, rows r = i % TR
-        if (WIDE && a.resid)        // uniform
+        if constexpr (RES)
           rv[i & 1].load(q8_res<TO, NC>(a, DOWN, min(t.m0 + (wr * TR + i % TR) * 16 + n, M - 1), min(cw + i / TR * PB * 16, a.n - NC)));
       };
       load_cols(0);
@@ -446,7 +446,7 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
         if constexpr (PB == 2) join_blocks(v[0], v[1]);
         const bool ok = row < M && col < a.n;
         if constexpr (DOWN) q8_down_store<TO, NC>(a, row, col, ok, v, rs[r], cs[p & 1], cb[p & 1], rv[i & 1], ri[r]);
-        else q8_store<TO, NC, WIDE>(a, row, col, ok, v, rs[r], cs[p & 1], cb[p & 1], rv[i & 1]);
+        else q8_store<TO, NC, WIDE, RES>(a, row, col, ok, v, rs[r], cs[p & 1], cb[p & 1], rv[i & 1]);
       }
     } else {
     // ---- epilogue: lane (g, n) holds columns 4g..4g+3 of row n of each 16x16

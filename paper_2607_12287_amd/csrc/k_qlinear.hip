@@ -449,9 +449,9 @@ __global__ __launch_bounds__(kQWaves * 64) void q_gemm_kernel(GemmArgs a) {
       for (int i = 1; i < kQWaves; ++i) sum += part[i][w][lane];
       const float4 cs = *reinterpret_cast<const float4*>(a.col_scale + col), bi = *reinterpret_cast<const float4*>(a.bias + col);
       ResRun<T, 4> res;
-      if (q8_wide<EPI>() && a.resid) res.load(q8_res<T, 4>(a, q8_down<EPI>(), row, col));
+      if constexpr (q8_resid<EPI>()) res.load(q8_res<T, 4>(a, q8_down<EPI>(), row, col));
       if constexpr (q8_down<EPI>()) q8_down_store<T, 4>(a, row, col, true, &sum, a.row_scale[row], &cs, &bi, res, a.rows[row]);
-      else q8_store<T, 4, q8_wide<EPI>()>(a, row, col, true, &sum, a.row_scale[row], &cs, &bi, res);
+      else q8_store<T, 4, q8_wide<EPI>(), q8_resid<EPI>()>(a, row, col, true, &sum, a.row_scale[row], &cs, &bi, res);
     }
     __syncthreads();  // `part` is written again
   }
@@ -536,8 +536,8 @@ __global__ __launch_bounds__(kQWaves * 64) void q_token_kernel(GemmArgs a) {
   for (int i = 1; i < kQWaves; ++i) sum += part[i][lane];
   const float4 cs = *reinterpret_cast<const float4*>(a.col_scale + col), bi = *reinterpret_cast<const float4*>(a.bias + col);
   ResRun<T, 4> res;
-  if (q8_wide<EPI>() && a.resid) res.load(q8_res<T, 4>(a, false, n, col));
-  q8_store<T, 4, q8_wide<EPI>()>(a, n, col, true, &sum, s_scale[n], &cs, &bi, res);
+  if constexpr (q8_resid<EPI>()) res.load(q8_res<T, 4>(a, false, n, col));
+  q8_store<T, 4, q8_wide<EPI>(), q8_resid<EPI>()>(a, n, col, true, &sum, s_scale[n], &cs, &bi, res);
 }
 
 template <int EPI, int RT, int U>
@@ -605,8 +605,9 @@ bool q_wide(const GemmArgs& a, int out_f32) {
 bool q_token_fits(int64_t rows, int K) { return rows <= 8 && rows * ((K + 63) / 64 * 64 + 16) <= 49152; }
 
 hipError_t launch_q_token(const GemmArgs& a, int f32, hipStream_t s) {
-  if (q_wide(a, f32)) return f32 ? launch_token_e<EPI_QF32>(a, s) : launch_token_e<EPI_QBF>(a, s);
-  return f32 ? launch_token_e<EPI_QF32_ANY>(a, s) : launch_token_e<EPI_QBF_ANY>(a, s);
+  if (!q_wide(a, f32)) return f32 ? launch_token_e<EPI_QF32_ANY>(a, s) : launch_token_e<EPI_QBF_ANY>(a, s);
+  if (a.resid) return f32 ? launch_token_e<EPI_QRES_F32>(a, s) : launch_token_e<EPI_QRES_BF>(a, s);
+  return f32 ? launch_token_e<EPI_QF32>(a, s) : launch_token_e<EPI_QBF>(a, s);
 }
 
 hipError_t launch_q_rows(const QRowsArgs& a, hipStream_t s) {
@@ -626,8 +627,11 @@ hipError_t launch_q_down(const GemmArgs& a, int out_f32, int expected, int rows,
 }
 
 hipError_t launch_q_gemm(const GemmArgs& a, int out_f32, int expected, int rows, hipStream_t s) {
-  if (q_wide(a, out_f32)) return out_f32 ? launch_gemm_e<EPI_QF32>(a, expected, rows, s) : launch_gemm_e<EPI_QBF>(a, expected, rows, s);
-  return out_f32 ? launch_gemm_e<EPI_QF32_ANY>(a, expected, rows, s) : launch_gemm_e<EPI_QBF_ANY>(a, expected, rows, s);
+  auto go = [&](auto e) { return launch_gemm_e<decltype(e)::value>(a, expected, rows, s); };
+  using std::integral_constant;
+  if (!q_wide(a, out_f32)) return out_f32 ? go(integral_constant<int, EPI_QF32_ANY>{}) : go(integral_constant<int, EPI_QBF_ANY>{});
+  if (a.resid) return out_f32 ? go(integral_constant<int, EPI_QRES_F32>{}) : go(integral_constant<int, EPI_QRES_BF>{});
+  return out_f32 ? go(integral_constant<int, EPI_QF32>{}) : go(integral_constant<int, EPI_QBF>{});
 }
 
 }  // namespace incvit
