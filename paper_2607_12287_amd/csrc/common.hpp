@@ -12,6 +12,7 @@
 namespace incvit {
 
 constexpr int kMaxViews = 64;
+constexpr int kMaxDevices = 64;
 constexpr int kMaxTokens = 4096;
 constexpr int kMaxDim = 2048;
 constexpr int kMaxHeadDim = 128;

@@ -51,6 +51,8 @@
 // depend on the tile shape beyond the fp32 order of the MFMA accumulation,
 // which is fixed (k ascending); no atomics.
 #pragma once
+#include <atomic>
+
 #include "gemm.hpp"
 
 namespace incvit {
@@ -558,13 +560,23 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // no load into this workgroup's LDS outlives it
 }
 
+// More than 64 KB of dynamic LDS for a kernel on the current device, once for each.
+inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<bool> (&done)[kMaxDevices]) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess || (dev >= 0 && dev < kMaxDevices && done[dev])) return e;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess && dev >= 0 && dev < kMaxDevices) done[dev] = true;
+  return e;
+}
+
 template <int EPI, int BM, int BN, int WR, int KD, int NS>
 hipError_t launch_tiled_cfg(const GemmArgs& a, int rows, hipStream_t s) {
   constexpr int lds = tiled_lds_bytes<EPI, BM, BN, KD, NS>();
   if constexpr (lds > 65536) {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_tiled_kernel<EPI, BM, BN, WR, KD, NS>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (attr != hipSuccess) return attr;
+    static std::atomic<bool> done[kMaxDevices] = {};  // a function's attributes are each device's own
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&gemm_tiled_kernel<EPI, BM, BN, WR, KD, NS>), lds, done);
+    if (e != hipSuccess) return e;
   }
   constexpr int slots = 256 * tiled_per_cu<EPI, BM, BN, KD, NS>();  // workgroups the chip holds
   const int mt = (rows + BM - 1) / BM, nt = (a.Nout + BN - 1) / BN;

@@ -1091,7 +1091,6 @@ incvit_status incvit_encode_frame(incvit_handle* h, int32_t B, const float* patc
 static __device__ __align__(256) char scratch[INCVIT_NOALLOC_SCRATCH_BYTES];
 
 namespace {
-constexpr int kMaxDevices = 64;
 std::mutex g_scratch_mu;
 void* g_scratch[kMaxDevices] = {};
 
