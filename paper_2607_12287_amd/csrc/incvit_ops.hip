@@ -1,4 +1,5 @@
 // C ABI of the stand-alone operators: argument checks and launches.
+#include <algorithm>
 #include <cmath>
 
 #include "ops.hpp"
@@ -80,24 +81,31 @@ incvit_status check_out(int32_t dtype, int64_t rows, int32_t N, const void* weig
   return INCVIT_OK;
 }
 
-// Rows per launch: the large-row GEMM addresses its rows' integers with 32 bits.
-int64_t q_slab(int32_t K) { return (((int64_t)1 << 31) / ((K + 63) / 64 * 64)) / 256 * 256; }
+// Rows per launch: the large-row GEMM addresses its rows' integers with 32 bits,
+// and a launch counts its threads in as many.
+int64_t q_slab(int32_t K) { return std::min((((int64_t)1 << 31) / ((K + 63) / 64 * 64)) / 256 * 256, (int64_t)1 << 21); }
 
 incvit_status q_rows(int32_t dtype, int64_t rows, int32_t K, const void* x, int64_t x_stride, const void* gamma, const void* beta,
                      float eps, void* qrows, hipStream_t s) {
   const QRowsLayout l(rows, K);
+  const size_t eb = dtype == INCVIT_BF16 ? 2 : 4;
   QRowsArgs a = {};
-  a.x = x;
   a.ld = (long)x_stride;
   a.gamma = gamma;
   a.beta = beta;
   a.eps = eps;
-  a.dst = static_cast<char*>(qrows);
-  a.scale = reinterpret_cast<float*>(a.dst + l.scale);
-  a.rows = (long)rows;
   a.K = K;
   a.dtype = dtype;
-  return launched(launch_q_rows(a, s), "qlinear_quantize_rows");
+  const int64_t slab = q_slab(K);
+  for (int64_t r = 0; r < rows; r += slab) {
+    a.x = static_cast<const char*>(x) + (size_t)r * x_stride * eb;
+    a.dst = static_cast<char*>(qrows) + (size_t)(r / 16) * l.kc * 1024;
+    a.scale = reinterpret_cast<float*>(static_cast<char*>(qrows) + l.scale) + r;
+    a.rows = (long)(rows - r < slab ? rows - r : slab);
+    const incvit_status st = launched(launch_q_rows(a, s), "qlinear_quantize_rows");
+    if (st != INCVIT_OK) return st;
+  }
+  return INCVIT_OK;
 }
 
 // What a product has but its rows and outputs.

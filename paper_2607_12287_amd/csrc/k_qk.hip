@@ -178,7 +178,7 @@ __device__ __forceinline__ void some_heads(const HeadSpec& h, int lane, int head
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       // pair v is (a_v, b_v), or values 2 v and 2 v + 1 of the 2 V in a row; the
-      // values past the rotated ones turn by (1, 0)
+      // values past the rotated ones stay
       if (rot[c]) {
         if (!h.adjacent) {
 #pragma unroll
@@ -249,7 +249,9 @@ __global__ __launch_bounds__(256) void qk_kernel(QkLaunch l) {
   const QkArgs& a = l.a;
   uint32_t r;
   int unit;
-  if (!unit_of<GL>(l.u, blockIdx.x, blockIdx.y, r, unit) || r >= a.rows) return;  // whole groups of lanes
+  const bool mine = unit_of<GL>(l.u, blockIdx.x, blockIdx.y, r, unit);
+  r += (uint32_t)a.row0;
+  if (!mine || r >= a.rows) return;  // whole groups of lanes
   const bool isk = unit >= l.u.uq;
   const QkSide s = isk ? a.k : a.q;
   const int h0 = (isk ? unit - l.u.uq : unit) * HP;
@@ -320,8 +322,14 @@ inline bool many_heads(long rows, int hq, int hk, int gl) { return hq % 2 == 0 &
 template <class T, int V, int GL, int C, int HP>
 hipError_t launch_h(const QkArgs& a, hipStream_t s) {
   QkLaunch l{a, units_of<GL>(a.q.heads, a.k.heads, HP)};
-  const dim3 grid((unsigned)((a.rows + l.u.rpb - 1) / l.u.rpb), (l.u.per_row + l.u.upb - 1) / l.u.upb);
-  return launch_k(qk_kernel<T, V, GL, C, HP>, grid, dim3(256), 0, s, l);
+  constexpr long kBlocks = 1 << 22;  // of a launch: threads are counted in 32 bits
+  for (l.a.row0 = 0; l.a.row0 < a.rows; l.a.row0 += kBlocks * l.u.rpb) {
+    const long blocks = (a.rows - l.a.row0 + l.u.rpb - 1) / l.u.rpb;
+    const dim3 grid((unsigned)std::min(blocks, kBlocks), (l.u.per_row + l.u.upb - 1) / l.u.upb);
+    const hipError_t e = launch_k(qk_kernel<T, V, GL, C, HP>, grid, dim3(256), 0, s, l);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 template <class T, int V, int GL, int C>
 hipError_t launch_v(const QkArgs& a, hipStream_t s) {

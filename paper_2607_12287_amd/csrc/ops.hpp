@@ -56,7 +56,8 @@ struct QkArgs {
   QkSide q, k;
   int dtype, head_dim, rot_pairs, adjacent, norm;
   float eps;
-  long rows;
+  long rows;           // all of the call's
+  long row0;           // the launch's first
   const float* table;  // [table_rows][rot_pairs][2]
   long table_rows;
   const int* index;    // [rows] table row of a row, or null: r % table_rows

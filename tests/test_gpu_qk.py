@@ -222,3 +222,18 @@ def test_another_stream_and_captured_calls():
         torch.cuda.synchronize()
         want, wk = run(torch.zeros_like(q), ko.clone())
         assert torch.equal(out, want) and torch.equal(kout, wk)
+
+
+def test_more_rows_than_one_launch_counts():
+    """70 million rows of one head of two values: a launch of a thread each would pass 2^32."""
+    rows = 70_000_001
+    x = torch.randn(rows, 1, 2, device="cuda", generator=torch.Generator("cuda").manual_seed(5)).to(torch.bfloat16)
+    table = make_table(7, 1)
+    got, _ = incvit.qk_norm_rope(x, None, table, norm=None)
+    t = table[torch.arange(rows, device="cuda") % 7, 0].double()
+    for lo in range(0, rows, 1 << 24):
+        s = slice(lo, lo + (1 << 24))
+        a, b, c, n = x[s, 0, 0].double(), x[s, 0, 1].double(), t[s, 0], t[s, 1]
+        for i, y in ((0, a * c - b * n), (1, b * c + a * n)):
+            bound = 4 * U * (a.abs() + b.abs()) + 2.0 ** -8 * y.abs() + 1e-30
+            assert bool(((got[s, 0, i].double() - y).abs() <= bound).all())

@@ -283,3 +283,15 @@ def test_the_front_of_an_attention_layer():
     rest = torch.ones(N, dtype=torch.bool, device="cuda")
     rest[tok.long()] = False
     assert torch.equal(cache[rest], before[rest])
+
+
+def test_more_rows_than_one_launch_counts():
+    """70 million rows of one value: each is its own scale, so the integers are +-127 (or 0) and the product is known."""
+    rows = 70_000_003
+    x = torch.randn(rows, 1, device="cuda", generator=torch.Generator("cuda").manual_seed(6)).to(torch.bfloat16)
+    w = torch.tensor([[0.75]], device="cuda", dtype=torch.bfloat16)
+    got = incvit.QLinear(w)(x)
+    for lo in range(0, rows, 1 << 24):
+        y = x[lo:lo + (1 << 24)].double() * 0.75
+        # two scales rounded to fp32, their product and the sum's scaling: 5 u, then bf16
+        assert bool(((got[lo:lo + (1 << 24)].double() - y).abs() <= (5 * U + 2.0 ** -8) * y.abs() + 1e-38).all())
