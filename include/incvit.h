@@ -71,7 +71,8 @@ typedef enum { INCVIT_F32 = 0, INCVIT_BF16 = 1 } incvit_dtype;
 
 /* What the cosine of eq. 3 compares, per token (both in fp32, fixed order):
  *   INCVIT_SCORE_EMBED: T[i] = patch embedding + position (the layer-1 input);
- *   INCVIT_SCORE_KEY:   the first layer's key, LN1(S(T[i])) W_K + b_K with
+ *   INCVIT_SCORE_KEY:   the first layer's key (before qk_norm and rope),
+ *     LN1(S(T[i])) W_K + b_K with
  *     layer 0's LayerNorm and key columns, S = rounding to the storage type:
  *     mean and variance from 64 lane partials (lane j takes d = j, j+64, ...
  *     in increasing d; the sum with adds, the squares of x - mean with fma)
@@ -100,8 +101,9 @@ typedef struct {
   int32_t score;       /* incvit_score; part of the cache identity */
   int32_t mlp_all;     /* 0: exact reuse (default); 1: every row through the MLP
                           each frame (see above); part of the cache identity */
-  /* Encoders without the learned positions' monopoly (all zero: as above; each
-   * is part of the cache identity): */
+  /* Parts of other vision transformers (all zero: as above; each is part of
+   * the cache identity; learned positions are added as before, zeros where a
+   * model has none): */
   int32_t rope;        /* 0: none; 1, 2: queries and keys of every layer are rotated
                           by their token's row and column in the patch grid, pairs
                           as INCVIT_PAIR_HALVES (1) or INCVIT_PAIR_ADJACENT (2) of
@@ -166,7 +168,8 @@ size_t incvit_cache_bytes(const incvit_handle* h);
 
 /* Bytes of one stream's cache in the canonical (export) layout:
  * ref [N][D] fp32, then in the storage dtype X [L+1][N][D], K [L][N][D],
- * V [L][N][D], Y [N][D], and with mlp_all A [L][N][D]. */
+ * V [L][N][D], Y [N][D], and with mlp_all A [L][N][D].  K holds the keys that the
+ * attention reads: with qk_norm and rope normed and rotated. */
 size_t incvit_cache_canonical_bytes(const incvit_handle* h);
 
 /* Bytes of workspace a call with B streams needs (256-byte aligned base). */
@@ -320,8 +323,8 @@ incvit_status incvit_rope_table(const incvit_rope* r, int64_t tokens, const int3
  * axes a token is at (t0 + frame, y0 + row, x0 + column), with two at (y0 + row,
  * x0 + column), with one at t0 + its number within the grid counted frame by
  * frame and row by row (whatever merge is).  grids: HOST [n], read before the
- * call returns; sizes >= 1, h and w multiples of merge >= 1; n >= 0; tokens and
- * table as above. */
+ * call returns; sizes >= 1, h and w multiples of merge >= 1 (else
+ * INCVIT_ERR_SHAPE); n >= 0; tokens and table as above. */
 incvit_status incvit_rope_table_grids(const incvit_rope* r, int32_t n, const incvit_grid* grids,
                                       int32_t merge, float* table, void* stream);
 
@@ -337,7 +340,8 @@ incvit_status incvit_rope_table_grids(const incvit_rope* r, int32_t n, const inc
  *   (x_a cos - x_b sin, x_b cos + x_a sin)
  * with (cos, sin) of pair i in the row's table row; the values past rot_dim stay
  * as the norm left them.  2 <= head_dim <= 256, even; 0 <= rot_dim <= head_dim,
- * even (0: no rotation, no table); eps >= 0 and finite. */
+ * even (0: no rotation, no table); eps >= 0 and finite (with 0 a head of zeros
+ * becomes NaN). */
 typedef enum { INCVIT_NORM_NONE = 0, INCVIT_NORM_RMS = 1, INCVIT_NORM_LAYER = 2 } incvit_norm;
 typedef enum { INCVIT_PAIR_HALVES = 0, INCVIT_PAIR_ADJACENT = 1 } incvit_pairing;
 
@@ -370,6 +374,7 @@ typedef struct {
  *   table: fp32 [table_rows][rot_dim / 2][2] as incvit_rope_table writes it,
  *     8-byte aligned; row r is rotated by table row index[r] (device int32
  *     [rows]), or r % table_rows if index is NULL (frames that share a grid);
+ *     without rotation none of the three is looked at;
  *   k_rows: device int32 [rows]: the row of k->out that row r's keys go to, of
  *     k_out_rows rows (a cache); NULL: row r.  The rows must differ from each
  *     other; rows of k->out that are not named keep what they hold.
@@ -394,8 +399,9 @@ incvit_status incvit_qk_norm_rope(const incvit_qk* c, int64_t rows, const incvit
  *   y_mn = act((sum_k q_mk w_kn) * (s_m * s_n) + b_n) + residual_mn, the sum
  *   exact in int32, the rest in fp32 with one rounding at the end; act is the
  *   identity or the tanh GELU.
- * A row or column of zeros has scale 0 (and integers 0), one that holds an
- * infinity or a NaN has scale NaN and makes its outputs NaN.
+ * Integers are limited to [-127, 127], which only scales at the end of fp32's
+ * range ever need; a row or column whose scale is 0 (zeros) has integers 0, one
+ * that holds an infinity or a NaN has scale NaN and makes its outputs NaN.
  * 1 <= K <= 65536, 1 <= N <= 2^20, and K * N below 2^32 bytes as packed;
  * otherwise INCVIT_ERR_UNSUPPORTED. */
 
@@ -521,6 +527,8 @@ void incvit_graph_destroy(incvit_graph* g);
  * The cols and row_groups fields do not apply to its launches; its MLP down
  * projection follows fc2_mode (1: split over K with the row kernel, 2:
  * unsplit; 0: split while its 64 x 128 tiles number fewer than 128).
+ * With mlp_int8 the MLP's products choose their own form by rows and sizes: cols,
+ * fc2_mode and tiled say nothing of them, and row_groups the rows to expect.
  * A NULL pointer restores the defaults. */
 typedef struct {
   int32_t cols[4];

@@ -6,6 +6,7 @@
 #include <cstdio>
 #include <cstring>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -398,7 +399,11 @@ struct incvit_graph {
 };
 
 incvit_status incvit::op_fail(incvit_status st, const char* msg) {
-  g_error = msg;
+  try {
+    g_error = msg;
+  } catch (const std::bad_alloc&) {  // the status alone, then
+    g_error.clear();
+  }
   return st;
 }
 

@@ -48,12 +48,12 @@ def rope_table(rope: _c.incvit_rope, positions=None, grids=None, merge: int = 1,
             raise ValueError("positions: device int32 [axes][tokens]")
         tokens, device = positions.shape[1], positions.device
     else:
-        arr = (_c.incvit_grid * len(grids))(*grids)
+        arr = (_c.incvit_grid * len(grids))(*[tuple(g) for g in grids])
         tokens = 0
         for g in grids:
             tokens += g[0] * g[1] * g[2]
         if device is None:
-            device = out.device if out is not None else torch.device("cuda", _current())
+            device = out.device if out is not None else torch.device("cuda", torch.cuda.current_device())
         elif not isinstance(device, torch.device) or device.index is None:
             device = torch.empty(0, device=device).device
     if out is None:
