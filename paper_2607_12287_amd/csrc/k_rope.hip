@@ -7,7 +7,8 @@
 // dropped terms are 1.8e-9 and 1.2e-10), swapped and signed by q.
 //
 // Bound: the table's bytes (8 per token and pair), and for a single frame the
-// launch.  A thread forms two pairs of one token, 16 bytes, and finds the token's
+// launch: 256 tokens of 36 pairs 3.4 us; a 6.7 MB table of video grids 6.0.  A
+// thread forms two pairs of one token, 16 bytes, and finds the token's
 // place in its grid by products with reciprocals in fp64.
 #include <cmath>
 
