@@ -47,7 +47,8 @@
 // exact int32 sums): a fragment is 16 rows or columns by 64 values, again a
 // kilobyte, and the epilogue applies the rows' and columns' scales.  8192 x 1024
 // -> 4096 with GELU: 43 us, of which the K loop is 23 (14 at the matrix rate) and the
-// rest the epilogue's 67 MB, which one workgroup per CU does not overlap with it.
+// rest the epilogue, which one workgroup per CU does not overlap with it: 67 MB of
+// stores (a fill of as much takes 11) and the GELU (4 to 8).
 //
 // bf16 models only otherwise (fp32 models use the small-M kernel).  Results do not
 // depend on the tile shape beyond the fp32 order of the MFMA accumulation,

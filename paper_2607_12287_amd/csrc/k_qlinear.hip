@@ -8,7 +8,7 @@
 //     write the row's integers in the matrix instruction's operand order (with a
 //     LayerNorm before it, whose statistics are two passes over registers).
 //     Bound by memory: 8192 x 1024 8.2 us (3.1 TB/s), 8192 x 4096 25 (4.0 TB/s),
-//     32 x 1152 3.2 (latency);
+//     23 x 1152 3.2 (latency);
 //   * q_tile_kernel: the same for the encoder's rows in operand order;
 //   * q_gemm_kernel, few rows: weights stream past them once.  A workgroup owns
 //     16 columns; its waves take the K chunks in turn, so every wave has loads of
