@@ -622,8 +622,10 @@ hipError_t launch_tiled_cfg(const GemmArgs& a, int rows, hipStream_t s) {
 //     512 rows 14.9 (64 x 128: 19.3); with at most one per CU its ring takes
 //     the whole LDS, more ahead of weights that come from HBM: QKV of 1024
 //     rows within the 448x448 encode 20.1 -> 17.6; else two per CU.
-// 8-bit products follow the same rule (us, in graphs): 1024 x 4304 -> 1152 64 x
-//   128 13.8, 64 x 64 19.1, 128 x 128 20.4; 1024 x 1152 -> 4304 256 x 128 and
+// 8-bit products follow the same rule with 64 x 96 between the first two (K staged
+//   by 256; us, in graphs): 1024 x 4304 -> 1152 64 x 96 12.3, 64 x 128 13.7, 64 x
+//   64 19.1, 128 x 128 20.4; with a residual 13.8 and 14.6; 300 x 4304 -> 4304 12.8
+//   and 14.4, 1024 x 1152 -> 1152 7.3 and 7.2, 640 x 1024 -> 2048 6.4 and 6.7; 1024 x 1152 -> 4304 256 x 128 and
 //   128 x 128 14.6, 64 x 128 16.3; 4096 x 1024 -> 4096 256 x 256 22.8, 256 x 128
 //   27.0, 128 x 128 28.1; 8192 x 4096 -> 1024 256 x 128 33, 128 x 128 37.5.
 template <int EPI>
@@ -637,6 +639,9 @@ hipError_t launch_tiled_epi(const GemmArgs& a, int expected, int rows, hipStream
   if (tiles(64, 64) <= 256) return launch_tiled_cfg<EPI, 64, 64, 2, 2, 8>(a, rows, s);
   // outputs whose columns are stored one by one
   if constexpr (is_q8<EPI>() && !q8_wide<EPI>()) return launch_tiled_cfg<EPI, 128, 128, 2, 1, 4>(a, rows, s);
+  if constexpr (is_q8<EPI>()) {
+    if (tiles(64, 96) <= 256) return launch_tiled_cfg<EPI, 64, 96, 4, 4, 4>(a, rows, s);
+  }
   if (tiles(64, 128) <= 256) return launch_tiled_cfg<EPI, 64, 128, 2, 2, 6>(a, rows, s);
   // at least `quarters` quarters of the places in all rounds of t tiles
   auto full = [](int t, int quarters) { return 4 * t >= quarters * 256 * ((t + 255) / 256); };

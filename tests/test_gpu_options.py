@@ -141,3 +141,9 @@ def test_caches_of_other_options_are_not_read():
             assert (other.status(c[0]) == incvit.INCVIT_OK) == (i == j)
     for e in encs:
         e.close()
+
+
+def test_more_rows_than_expected():
+    """A step told to expect 256 rows refreshes 800: the MLP's workgroups take several of the tiles chosen for 256 (64 x 96)."""
+    m = synth.ModelShape(120, 120, 3, 6, 640, 1, 8, 4352, "bf16", mlp_int8=True)
+    run_steps(m, 41, views=2, frames=2, tau=2.0, row_groups=8)

@@ -295,3 +295,12 @@ def test_more_rows_than_one_launch_counts():
         y = x[lo:lo + (1 << 24)].double() * 0.75
         # two scales rounded to fp32, their product and the sum's scaling: 5 u, then bf16
         assert bool(((got[lo:lo + (1 << 24)].double() - y).abs() <= (5 * U + 2.0 ** -8) * y.abs() + 1e-38).all())
+
+
+@pytest.mark.parametrize("rows,K,N,dtype", [(1000, 1100, 1160, "bf16"), (1024, 260, 1280, "f32"), (1000, 4304, 1152, "bf16"),
+                                            (300, 1152, 4312, "bf16"), (1024, 2500, 1084, "f32"), (641, 1024, 2040, "bf16")])
+def test_tiles_of_96_columns(rows, K, N, dtype):
+    """More than 256 tiles of 64 x 64 and at most 256 of 64 x 96, with column blocks and chunks that do not fill the last."""
+    x, w, b, r = make(rows, K, N, dtype)
+    lin, _ = run(x, w, b, None, True)
+    run(x, w, b, r, False, lin)
