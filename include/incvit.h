@@ -451,7 +451,8 @@ incvit_status incvit_qlinear_multiply(int32_t dtype, int64_t rows, int32_t K, in
 /* Both in one call: rows of `dtype` quantised into workspace
  * (incvit_qlinear_rows_bytes(rows, K) bytes, 256-byte aligned, the call's own
  * until it has run on `stream`), then multiplied; a few tokens (up to 8 rows) in
- * one launch, with the same bits. */
+ * one launch, with the same bits.  out may also overlap x, which is read before
+ * anything is written. */
 incvit_status incvit_qlinear(int32_t dtype, int64_t rows, int32_t K, int32_t N, const void* x,
                              int64_t x_stride, const void* weights, int32_t gelu,
                              const void* residual, int64_t res_stride, void* out,

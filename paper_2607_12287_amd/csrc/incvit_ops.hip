@@ -108,6 +108,13 @@ incvit_status q_rows(int32_t dtype, int64_t rows, int32_t K, const void* x, int6
   return INCVIT_OK;
 }
 
+// Whether rows of n elements every `stride` from p on and the same from q on share
+// a span of memory.
+bool spans_meet(int64_t rows, size_t eb, const void* p, int64_t n, int64_t stride, const void* q, int64_t m, int64_t ostride) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  return a < b + ((rows - 1) * ostride + m) * eb && b < a + ((rows - 1) * stride + n) * eb;
+}
+
 // What a product has but its rows and outputs.
 GemmArgs q_args(int32_t K, int32_t N, const void* weights, int32_t gelu, int64_t res_stride, int64_t out_stride) {
   const QWeightsLayout wl(K, N);
@@ -305,7 +312,8 @@ incvit_status incvit_qlinear(int32_t dtype, int64_t rows, int32_t K, int32_t N, 
   if ((st = check_x(dtype, x, x_stride, workspace)) != INCVIT_OK) return st;
   if ((st = check_out(dtype, rows, N, weights, gelu, residual, res_stride, out, out_stride)) != INCVIT_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (q_token_fits(rows, K)) {
+  // in one launch only where no workgroup's output can be another's input
+  if (q_token_fits(rows, K) && !spans_meet(rows, dtype == INCVIT_BF16 ? 2 : 4, x, K, x_stride, out, N, out_stride)) {
     GemmArgs a = q_args(K, N, weights, gelu, res_stride, out_stride);
     a.A = x;
     a.x_ld = (long)x_stride;

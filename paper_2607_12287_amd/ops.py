@@ -1,7 +1,8 @@
 """The library's stand-alone operators on torch tensors (reached as attributes of
 :mod:`paper_2607_12287_amd.incvit`).  Argument checks and memory only: a call is
 one or two kernels of a few microseconds, so the checks build nothing that they do
-not need.  Work goes to the current stream of the tensors' device.
+not need.  Work goes to the current stream of the tensors' device; results carry
+no gradient.
 """
 from __future__ import annotations
 
@@ -200,7 +201,7 @@ class QLinear:
     def __call__(self, x, gelu: bool = False, residual=None, out=None):
         """act(x W + b) + residual for x [rows][K] (fp32 or bf16, the values of a row
         one after another) or QRows; residual and out [rows][N] of x's type (out may
-        be residual).  Returns out."""
+        be residual, or overlap x).  Returns out."""
         q = isinstance(x, QRows)
         if q:
             code, rows, K, dev = _CODES[x.dtype], x.rows, x.K, x.buf.device

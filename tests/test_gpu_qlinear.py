@@ -304,3 +304,24 @@ def test_tiles_of_96_columns(rows, K, N, dtype):
     x, w, b, r = make(rows, K, N, dtype)
     lin, _ = run(x, w, b, None, True)
     run(x, w, b, r, False, lin)
+
+
+@pytest.mark.parametrize("rows", [1, 8, 9, 300])
+def test_output_over_the_input(rows):
+    """The rows are read before any output is written: in place, shifted by a row's half, and beside each other in one buffer."""
+    K = 640
+    x, w, b, _ = make(rows, K, K, "bf16")
+    lin = incvit.QLinear(w, b)
+    want = lin(x)
+    y = x.clone()
+    lin(y, out=y)
+    assert torch.equal(y, want)
+    buf = torch.zeros(rows * K + K // 2, device="cuda", dtype=x.dtype)
+    src = buf[:rows * K].view(rows, K)
+    src.copy_(x)
+    out = buf[K // 2:].view(rows, K)
+    lin(src, out=out)
+    assert torch.equal(out, want)
+    pair = torch.cat([x, torch.zeros_like(x)], dim=1)
+    lin(pair[:, :K], out=pair[:, K:])
+    assert torch.equal(pair[:, K:], want) and torch.equal(pair[:, :K], x)
