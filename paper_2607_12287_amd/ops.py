@@ -6,6 +6,7 @@ no gradient.
 """
 from __future__ import annotations
 
+import struct
 from typing import Optional
 
 import torch
@@ -14,6 +15,9 @@ from . import incvit as _c
 
 _BF16, _F32 = torch.bfloat16, torch.float32
 _CODES = {_F32: _c.INCVIT_F32, _BF16: _c.INCVIT_BF16, torch.int8: _c.INCVIT_I8}
+# incvit_heads and incvit_qk as their bytes: 0.1 us each, a ctypes structure 0.4
+_HEADS, _QK = struct.Struct("4P4qi4x"), struct.Struct("5if")
+assert _HEADS.size == _c.ctypes.sizeof(_c.incvit_heads) and _QK.size == _c.ctypes.sizeof(_c.incvit_qk)
 _stream_of = torch._C._cuda_getCurrentRawStream
 _current = torch._C._cuda_getDevice
 
@@ -58,7 +62,7 @@ def rope_table(rope: _c.incvit_rope, positions=None, grids=None, merge: int = 1,
         elif not isinstance(device, torch.device) or device.index is None:
             device = torch.empty(0, device=device).device
     if out is None:
-        out = torch.empty((max(tokens, 0), n, 2), dtype=_F32, device=device)
+        out = torch.empty(max(tokens, 0), n, 2, dtype=_F32, device=device)
     elif not (out.device == device and out.is_cuda and out.dtype == _F32 and out.is_contiguous() and out.numel() == tokens * n * 2):
         raise ValueError("out: device fp32 [tokens][pairs][2]")
     if positions is not None:
@@ -72,7 +76,8 @@ def rope_table(rope: _c.incvit_rope, positions=None, grids=None, merge: int = 1,
 # ------------------------------------------- head norms with the rotation --
 
 
-def _heads(x, out, gamma, beta, who: str) -> _c.incvit_heads:
+def _heads(x, out, gamma, beta, who: str) -> bytes:
+    """The bytes of the incvit_heads of x and out."""
     for t in (gamma, beta):
         if t is not None and not (t.dtype == x.dtype and t.device == x.device and t.is_contiguous() and t.numel() == x.shape[2]):
             raise ValueError(f"{who}_gamma, {who}_beta: [head_dim] of the rows' type and device")
@@ -81,7 +86,8 @@ def _heads(x, out, gamma, beta, who: str) -> _c.incvit_heads:
         raise ValueError(f"{who}_out: rows of the same heads, type and device")
     if s[2] != 1 or o[2] != 1:
         raise ValueError(f"{who}, {who}_out: the values of a head lie one after another")
-    return _c.incvit_heads(x.data_ptr(), out.data_ptr(), _ptr(gamma), _ptr(beta), s[0], s[1], o[0], o[1], x.shape[1])
+    return _HEADS.pack(x.data_ptr(), out.data_ptr(), 0 if gamma is None else gamma.data_ptr(), 0 if beta is None else beta.data_ptr(),
+                       s[0], s[1], o[0], o[1], x.shape[1])
 
 
 def qk_norm_rope(q=None, k=None, table=None, pairing: str = "halves", norm: Optional[str] = "rms", q_gamma=None, k_gamma=None,
@@ -116,24 +122,24 @@ def qk_norm_rope(q=None, k=None, table=None, pairing: str = "halves", norm: Opti
     k_out_rows = 0
     if q is not None:
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+            q_out = torch.empty(rows, q.shape[1], d, dtype=dt, device=dev)
         elif q_out.shape[0] != rows:
             raise ValueError("q_out: as many rows as q")
-        hq = _c.ctypes.byref(_heads(q, q_out, q_gamma, q_beta, "q"))
+        hq = _heads(q, q_out, q_gamma, q_beta, "q")
     if k is not None:
         if k_rows is not None:
             if k_out is None:
                 raise ValueError("k_rows: rows of k_out, which has to be given")
             k_out_rows = k_out.shape[0]
         elif k_out is None:
-            k_out = torch.empty(k.shape, dtype=dt, device=dev)
+            k_out = torch.empty(rows, k.shape[1], d, dtype=dt, device=dev)
         elif k_out.shape[0] != rows:
             raise ValueError("k_out: as many rows as k")
-        hk = _c.ctypes.byref(_heads(k, k_out, k_gamma, k_beta, "k"))
+        hk = _heads(k, k_out, k_gamma, k_beta, "k")
     elif k_rows is not None:
         raise ValueError("k_rows: rows of k_out, without k")
-    c = _c.incvit_qk(_CODES[dt], d, rot, _c.PAIRINGS[pairing], _c.NORMS[norm], eps)
-    _call(_c.lib().incvit_qk_norm_rope, dev, _c.ctypes.byref(c), rows, hq, hk, _ptr(table), trows, _ptr(index), _ptr(k_rows),
+    c = _QK.pack(_CODES[dt], d, rot, _c.PAIRINGS[pairing], _c.NORMS[norm], eps)
+    _call(_c.lib().incvit_qk_norm_rope, dev, c, rows, hq, hk, _ptr(table), trows, _ptr(index), _ptr(k_rows),
           k_out_rows)
     return q_out, k_out
 
@@ -212,7 +218,7 @@ class QLinear:
             raise ValueError("x: rows of K values on the weights' device")
         N, dt = self.N, x.dtype
         if out is None:
-            out = torch.empty((rows, N), dtype=dt, device=dev)
+            out = torch.empty(rows, N, dtype=dt, device=dev)
         elif not (out.dtype == dt and out.device == dev and out.shape == (rows, N) and (out.stride(1) == 1 or N == 1)):
             raise ValueError("out: [rows][N] of x's type, the values of a row one after another")
         r = None
