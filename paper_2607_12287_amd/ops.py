@@ -97,7 +97,10 @@ def qk_norm_rope(q=None, k=None, table=None, pairing: str = "halves", norm: Opti
     table rows `index` (device int32 [rows]; without it row r % table rows) of
     `table` (rope_table's; None: no rotation).  k_rows (device int32 [rows]): the
     rows of k_out (a cache [..][k heads][d], then required) that the new keys go
-    to.  q_out, k_out may be q and k (in place).  Returns (q_out, k_out)."""
+    to.  q_out, k_out may be q and k (in place); made here they are new tensors.  A
+    row whose index is outside the table (padding: negative) gets no output: it
+    stays what it was in a given q_out or k_out and is zeros in a new one.  Returns
+    (q_out, k_out)."""
     x = q if q is not None else k
     if x is None:
         raise ValueError("q or k")
@@ -113,6 +116,7 @@ def qk_norm_rope(q=None, k=None, table=None, pairing: str = "halves", norm: Opti
         if not (table.device == dev and table.dtype == _F32 and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous()):
             raise ValueError("table: device fp32 [rows][pairs][2]")
         trows, rot = table.shape[0], 2 * table.shape[1]
+    new = torch.zeros if index is not None and rot else torch.empty  # rows that the kernel leaves out
     for t in (index, k_rows):
         if t is not None and not (t.dtype == torch.int32 and t.device == dev and t.is_contiguous() and t.numel() == rows):
             raise ValueError("index, k_rows: device int32 [rows]")
@@ -122,7 +126,7 @@ def qk_norm_rope(q=None, k=None, table=None, pairing: str = "halves", norm: Opti
     k_out_rows = 0
     if q is not None:
         if q_out is None:
-            q_out = torch.empty(rows, q.shape[1], d, dtype=dt, device=dev)
+            q_out = new(rows, q.shape[1], d, dtype=dt, device=dev)
         elif q_out.shape[0] != rows:
             raise ValueError("q_out: as many rows as q")
         hq = _heads(q, q_out, q_gamma, q_beta, "q")
@@ -132,7 +136,7 @@ def qk_norm_rope(q=None, k=None, table=None, pairing: str = "halves", norm: Opti
                 raise ValueError("k_rows: rows of k_out, which has to be given")
             k_out_rows = k_out.shape[0]
         elif k_out is None:
-            k_out = torch.empty(rows, k.shape[1], d, dtype=dt, device=dev)
+            k_out = new(rows, k.shape[1], d, dtype=dt, device=dev)
         elif k_out.shape[0] != rows:
             raise ValueError("k_out: as many rows as k")
         hk = _heads(k, k_out, k_gamma, k_beta, "k")
