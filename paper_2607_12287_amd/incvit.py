@@ -240,11 +240,23 @@ def incvit_rope_table(rope: incvit_rope, tokens: int, pos: int, axis_stride: int
     return lib().incvit_rope_table(ctypes.addressof(rope), tokens, pos, axis_stride, token_stride, table, stream)
 
 
+def grid_array(grids, merge: int):
+    """A ctypes array of incvit_grid (or itself) from (t, h, w[, t0[, y0[, x0]]]); ctypes would cut what is past 32 bits to
+    its low half."""
+    if not -0x80000000 <= merge <= 0x7fffffff:
+        raise ValueError("merge: a 32-bit integer")
+    if isinstance(grids, ctypes.Array):
+        return grids
+    for g in grids:
+        if max(g) > 0x7fffffff or min(g) < -0x80000000:
+            raise ValueError("grids: sizes and first positions are 32-bit integers")
+    return (incvit_grid * len(grids))(*[tuple(g) for g in grids])
+
+
 def incvit_rope_table_grids(rope: incvit_rope, grids, merge: int, table: int, stream: int = 0) -> int:
     """grids: a ctypes array of incvit_grid, or a sequence of (t, h, w[, t0[, y0[, x0]]])."""
-    if not isinstance(grids, ctypes.Array):
-        grids = (incvit_grid * len(grids))(*[tuple(g) for g in grids])
-    return lib().incvit_rope_table_grids(ctypes.addressof(rope), len(grids), grids, merge, table, stream)
+    arr = grid_array(grids, merge)
+    return lib().incvit_rope_table_grids(ctypes.addressof(rope), len(arr), arr, merge, table, stream)
 
 
 def incvit_qk_norm_rope(c: incvit_qk, rows: int, q: Optional[incvit_heads], k: Optional[incvit_heads], table: int,
@@ -260,8 +272,8 @@ def make_rope(head_dim: int, pairs: Sequence[int], theta: float = 10000.0, ladde
     or one): pairs[a] pairs of a head's dims turn with axis a.  2 * sum(pairs) <=
     head_dim dims are rotated."""
     n = len(pairs)
-    if not 1 <= n <= 3 or 2 * sum(pairs) > head_dim or (scale is not None and len(scale) != n):
-        raise ValueError("pairs names one to three axes with at most head_dim / 2 pairs together, scale a factor for each")
+    if not 1 <= n <= 3 or min(pairs) < 1 or 2 * sum(pairs) > head_dim or (scale is not None and len(scale) != n):
+        raise ValueError("pairs names one to three axes with a pair each and at most head_dim / 2 together, scale a factor for each")
     return incvit_rope(n, (ctypes.c_int32 * 3)(*pairs), LADDERS[ladder], LAYOUTS[layout], float(theta),
                        (ctypes.c_double * 3)(*(scale or (1.0,) * n)))
 

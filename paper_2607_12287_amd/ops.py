@@ -53,7 +53,7 @@ def rope_table(rope: _c.incvit_rope, positions=None, grids=None, merge: int = 1,
             raise ValueError("positions: device int32 [axes][tokens]")
         tokens, device = positions.shape[1], positions.device
     else:
-        arr = (_c.incvit_grid * len(grids))(*[tuple(g) for g in grids])
+        arr = _c.grid_array(grids, merge)
         tokens = 0
         for g in grids:
             tokens += g[0] * g[1] * g[2]
