@@ -151,11 +151,16 @@ def qk_norm_rope(q=None, k=None, table=None, pairing: str = "halves", norm: Opti
 # ----------------------------------------------------------- 8-bit products --
 
 
+_MOST_K, _MOST_N = 65536, 1 << 20  # the library's, which takes both in 32 bits
+
+
 def _rows_of(x):
     """(type code, rows, K) of rows that the 8-bit operators take."""
     code = _CODES.get(x.dtype, _c.INCVIT_I8)
     if not (x.is_cuda and code != _c.INCVIT_I8 and x.dim() == 2 and (x.stride(1) == 1 or x.shape[1] == 1)):
         raise ValueError("x: device fp32 or bf16 [rows][K], the values of a row one after another")
+    if x.shape[1] > _MOST_K:
+        raise _c.IncvitError(_c.INCVIT_ERR_UNSUPPORTED, f"rows of K = {x.shape[1]}")
     return code, x.shape[0], x.shape[1]
 
 
@@ -201,7 +206,7 @@ class QLinear:
             if t is not None and not (t.device == self.device and t.dtype == dt and t.is_contiguous() and t.numel() == self.N):
                 raise ValueError("bias: [N] of the weights' type (fp32 with int8 weights); scales: fp32 [N]; on the weights' device")
         L = _c.lib()
-        n = L.incvit_qlinear_weights_bytes(self.K, self.N)
+        n = L.incvit_qlinear_weights_bytes(self.K, self.N) if self.K <= _MOST_K and self.N <= _MOST_N else 0
         if n == 0:
             raise _c.IncvitError(_c.INCVIT_ERR_UNSUPPORTED, f"a product of K = {self.K}, N = {self.N}")
         self.weights = _buffer(n, self.device)
