@@ -637,22 +637,24 @@ hipError_t launch_tiled_epi(const GemmArgs& a, int expected, int rows, hipStream
   }
   auto tiles = [&](int bm, int bn) { return (expected + bm - 1) / bm * ((a.Nout + bn - 1) / bn) * a.ksplit; };
   if (tiles(64, 64) <= 256) return launch_tiled_cfg<EPI, 64, 64, 2, 2, 8>(a, rows, s);
-  // outputs whose columns are stored one by one
-  if constexpr (is_q8<EPI>() && !q8_wide<EPI>()) return launch_tiled_cfg<EPI, 128, 128, 2, 1, 4>(a, rows, s);
-  if constexpr (is_q8<EPI>()) {
-    if (tiles(64, 96) <= 256) return launch_tiled_cfg<EPI, 64, 96, 4, 4, 4>(a, rows, s);
+  if constexpr (is_q8<EPI>() && !q8_wide<EPI>()) {  // outputs whose columns are stored one by one
+    return launch_tiled_cfg<EPI, 128, 128, 2, 1, 4>(a, rows, s);
+  } else {
+    if constexpr (is_q8<EPI>()) {
+      if (tiles(64, 96) <= 256) return launch_tiled_cfg<EPI, 64, 96, 4, 4, 4>(a, rows, s);
+    }
+    if (tiles(64, 128) <= 256) return launch_tiled_cfg<EPI, 64, 128, 2, 2, 6>(a, rows, s);
+    // at least `quarters` quarters of the places in all rounds of t tiles
+    auto full = [](int t, int quarters) { return 4 * t >= quarters * 256 * ((t + 255) / 256); };
+    if constexpr (EPI == EPI_QKV || EPI == EPI_FC1 || is_q8<EPI>()) {
+      const int x = tiles(256, 256);
+      if (x >= 256 && full(x, 4)) return launch_tiled_cfg<EPI, 256, 256, 2, 1, 4>(a, rows, s);
+    }
+    const int l = tiles(256, 128);
+    if (l > 128 && (l <= 256 || full(l, 3))) return launch_tiled_cfg<EPI, 256, 128, 4, 1, 6>(a, rows, s);
+    if (tiles(128, 128) <= 256) return launch_tiled_cfg<EPI, 128, 128, 2, 1, 8>(a, rows, s);
+    return launch_tiled_cfg<EPI, 128, 128, 2, 1, 4>(a, rows, s);
   }
-  if (tiles(64, 128) <= 256) return launch_tiled_cfg<EPI, 64, 128, 2, 2, 6>(a, rows, s);
-  // at least `quarters` quarters of the places in all rounds of t tiles
-  auto full = [](int t, int quarters) { return 4 * t >= quarters * 256 * ((t + 255) / 256); };
-  if constexpr (EPI == EPI_QKV || EPI == EPI_FC1 || is_q8<EPI>()) {
-    const int x = tiles(256, 256);
-    if (x >= 256 && full(x, 4)) return launch_tiled_cfg<EPI, 256, 256, 2, 1, 4>(a, rows, s);
-  }
-  const int l = tiles(256, 128);
-  if (l > 128 && (l <= 256 || full(l, 3))) return launch_tiled_cfg<EPI, 256, 128, 4, 1, 6>(a, rows, s);
-  if (tiles(128, 128) <= 256) return launch_tiled_cfg<EPI, 128, 128, 2, 1, 8>(a, rows, s);
-  return launch_tiled_cfg<EPI, 128, 128, 2, 1, 4>(a, rows, s);
 }
 
 }  // namespace incvit

@@ -56,6 +56,7 @@ template <int V> struct Run<float, V> {
   }
   __device__ float get(int i) const { return v[i]; }
   __device__ static void store(float* p, const float* f) {
+    static_assert(V <= 4, "runs of 8 are bf16 values, whose gains alone are fp32");
     if constexpr (V == 4) *(INCVIT_GLOBAL f32x4_t*)p = f32x4_t{f[0], f[1], f[2], f[3]};
     else *(INCVIT_GLOBAL f32x2_t*)p = f32x2_t{f[0], f[1]};
   }
@@ -340,15 +341,19 @@ hipError_t launch_v(const QkArgs& a, hipStream_t s) {
   return launch_h<T, V, GL, C, 1>(a, s);
 }
 
-// lanes of a head: the power of two that covers its chunks
+// lanes of a head: the power of two that covers its chunks, of which kMaxPairs / V at most
 template <class T, int V>
 hipError_t launch_lanes(const QkArgs& a, hipStream_t s) {
   const int chunks = a.head_dim / 2 / V;
   if (chunks <= 4) return launch_v<T, V, 4, 1>(a, s);
   if (chunks <= 8) return launch_v<T, V, 8, 1>(a, s);
-  if (chunks <= 16) return launch_v<T, V, 16, 1>(a, s);
-  if (chunks <= 32) return launch_v<T, V, 32, 1>(a, s);
-  return launch_v<T, V, 64, 1>(a, s);
+  if constexpr (kMaxPairs / V > 16) {
+    if (chunks > 32) {
+      if constexpr (kMaxPairs / V > 32) return launch_v<T, V, 64, 1>(a, s);
+    }
+    if (chunks > 16) return launch_v<T, V, 32, 1>(a, s);
+  }
+  return launch_v<T, V, 16, 1>(a, s);
 }
 
 // whether every chunk of v values that a call touches is aligned to itself
@@ -395,8 +400,10 @@ hipError_t launch_qk_layer(const QkLayerArgs& a, int rows, hipStream_t s) {
   auto lanes = [&](auto t, auto v) {
     const int chunks = a.sh.dh / 2 / decltype(v)::value;
     if (chunks <= 4) return heads(t, v, std::integral_constant<int, 4>{});
-    if (chunks <= 8) return heads(t, v, std::integral_constant<int, 8>{});
-    return heads(t, v, std::integral_constant<int, 16>{});
+    if constexpr (kMaxHeadDim / 2 / decltype(v)::value > 8) {
+      if (chunks > 8) return heads(t, v, std::integral_constant<int, 16>{});
+    }
+    return heads(t, v, std::integral_constant<int, 8>{});
   };
   if (!a.sh.dtype) return lanes(float{}, std::integral_constant<int, 4>{});
   if (a.sh.dh % 16 == 0) return lanes(uint16_t{}, std::integral_constant<int, 8>{});
