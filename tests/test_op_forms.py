@@ -1,5 +1,5 @@
-"""Which kernels the operators' calls launch (CPU: a stand-in for the runtime writes the launches down): every kernel that is
-compiled for the operators is launched by some call."""
+"""Which kernels the operators' calls launch (CPU: a stand-in for the runtime writes the launches down): the sizes of the GPU
+tests take the forms that those tests are about, and every kernel that is compiled for the operators is launched by some call."""
 import os
 import re
 import shutil
@@ -7,10 +7,14 @@ import subprocess
 
 import pytest
 
-from paper_2607_12287_amd import synth
+from tests import test_gpu_options_large as large
+from tests import test_gpu_q8_forms as q8
+from tests import test_gpu_qk_forms as qk
 from tests.launch_log import launches
 
 OBJDUMP = "/opt/rocm/llvm/bin/llvm-objdump"
+EPI = {("bf16", False): 6, ("f32", False): 7, ("bf16", True): 10, ("f32", True): 11}
+ANY = {"bf16": 8, "f32": 9}
 
 
 def dt(name):
@@ -21,14 +25,51 @@ def linear(dtype, rows, K, N, residual=False):
     return "linear", dict(dtype=dt(dtype), rows=rows, K=K, N=N, residual=residual)
 
 
-def shape(dim, heads, mlp, side=96, dtype="bf16", **kw):
-    """A model of (side / 6)^2 tokens to a frame, with every option."""
-    kw = {**dict(rope="halves", qk_norm="layer", mlp_int8=True), **kw}
-    return synth.ModelShape(side, side, 3, 6, dim, 2, heads, mlp, dtype, **kw)
-
-
 def full(m, B, **kw):
     return "full", dict(shape=m.__dict__, B=B, **kw)
+
+
+def only(entries, prefix):
+    return [e[0] for e in entries if e[0].startswith(prefix)]
+
+
+def test_products_take_the_forms_of_their_tests(tmp_path):
+    calls, want = [], []
+    for forms, wide in ((q8.FORMS, True), (q8.FORMS_ANY, False)):
+        for rows, K, N, form in forms:
+            for dtype in ("bf16", "f32"):
+                for residual in (False, True):
+                    kernel, args = form.split()
+                    calls.append(linear(dtype, rows, K, N, residual))
+                    want.append(f"{kernel}_kernel<{EPI[dtype, residual] if wide else ANY[dtype]},{args}>")
+    for call, got, w in zip(calls, launches(calls, tmp_path), want):
+        assert got[-1][0] == w, call
+    # every form of every epilogue is among them
+    reached = {w for w in want if "gemm" in w}
+    tiles = {f.split()[1] for *_, f in q8.FORMS if f.startswith("gemm_tiled")}
+    few = {f.split()[1] for *_, f in q8.FORMS if f.startswith("q_gemm")}
+    assert len(tiles) == 7 and len(few) == 6 and len(reached) == 4 * 13 + 2 * 8
+
+
+def test_head_norms_take_the_instances_of_their_tests(tmp_path):
+    calls = [("qk", dict(dtype=dt(t), rows=rows, hq=hq, hk=hk, d=d, rot=rot)) for t, rows, hq, hk, d, rot, _ in qk.CASES]
+    for case, got in zip(qk.CASES, launches(calls, tmp_path)):
+        assert [e[0] for e in got] == [f"qk_kernel<{case[-1]}>"], case
+    assert len({c[-1] for c in qk.CASES}) == 9 + 6
+
+
+def test_large_encodes_take_the_kernels_of_their_tests(tmp_path):
+    calls = []
+    for _, m, B, *_ in large.CASES:
+        calls += [full(m, B), ("step", dict(shape=m.__dict__, B=B, tau=float("inf"), caps=[m.n_tokens - 3] * B)), full(m, 1)]
+    got = launches(calls, tmp_path)
+    for i, (name, m, B, _, down, heads) in enumerate(large.CASES):
+        whole, step, one = got[3 * i:3 * i + 3]
+        epi = 12 if m.dtype == "bf16" else 13
+        assert set(only(whole, "qk_layer")) == {f"qk_layer_kernel<{heads}>"}, name
+        for entries in (whole, step):
+            assert not down or f"gemm_tiled_kernel<{epi},{down}>" in only(entries, "gemm_tiled"), name
+        assert B == 1 or any(k.startswith(f"q_gemm_kernel<{epi},") for k in only(one, "q_gemm")), name
 
 
 def compiled(tmp_path, source):
@@ -74,14 +115,14 @@ def sweep():
                 yield linear(dtype, 3, K, N, True)
         for B, dim, heads, mlp in [(b, *s) for b in (1, 2, 3, 4, 8, 10, 17, 32, 33)
                                    for s in ((96, 3, 100), (320, 10, 4096), (1024, 16, 300), (1024, 8, 4096), (1152, 16, 450), (2048, 16, 100))]:
-            yield full(shape(dim, heads, mlp, dtype=dtype), B)
+            yield full(large.shape(dim, heads, mlp, dtype=dtype), B)
         for dim, heads in ((128, 8), (192, 8), (192, 4), (448, 8), (384, 4), (256, 2), (576, 8), (128, 1), (64, 8)):
             for B in (1, 33):
-                yield full(shape(dim, heads, 100, dtype=dtype), B)
+                yield full(large.shape(dim, heads, 100, dtype=dtype), B)
         for side, B in ((12, 1), (24, 1), (48, 1), (54, 2), (60, 3), (96, 1), (96, 2)):
             for mlp in (64, 600, 2200, 4304):
-                yield full(shape(1152, 16, mlp, side=side, dtype=dtype), B)
-                yield full(shape(2048, 16, mlp, side=side, dtype=dtype), B)
+                yield full(large.shape(1152, 16, mlp, side=side, dtype=dtype), B)
+                yield full(large.shape(2048, 16, mlp, side=side, dtype=dtype), B)
 
 
 @pytest.mark.skipif(not os.path.exists(OBJDUMP), reason="llvm-objdump not installed")
