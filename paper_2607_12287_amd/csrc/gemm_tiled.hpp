@@ -628,6 +628,11 @@ hipError_t launch_tiled_cfg(const GemmArgs& a, int rows, hipStream_t s) {
 //   and 14.4, 1024 x 1152 -> 1152 7.3 and 7.2, 640 x 1024 -> 2048 6.4 and 6.7; 1024 x 1152 -> 4304 256 x 128 and
 //   128 x 128 14.6, 64 x 128 16.3; 4096 x 1024 -> 4096 256 x 256 22.8, 256 x 128
 //   27.0, 128 x 128 28.1; 8192 x 4096 -> 1024 256 x 128 33, 128 x 128 37.5.
+//   Outputs that end off 16 bytes, stored column by column, take 256-row tiles
+//   in one round only (us, bf16 outputs): 256 x 1152 -> 4305 64 x 96 8.2, 128 x
+//   128 12.7; 1024 x 4304 -> 1153 64 x 96 14.0, 128 x 128 24.5; 400 x 1152 ->
+//   4305 64 x 128 10.9, 128 x 128 13.7; 1024 x 1152 -> 4305 256 x 128 22.0, 128 x
+//   128 25.0, but 8192 x 1024 -> 4097 108.5 and 97.2 (256 x 256 117.8).
 template <int EPI>
 hipError_t launch_tiled_epi(const GemmArgs& a, int expected, int rows, hipStream_t s) {
   if (a.ksplit < 1 || (!is_q8<EPI>() && (!a.sh.dtype || a.sh.dh % 8))) return hipErrorInvalidValue;
@@ -637,24 +642,21 @@ hipError_t launch_tiled_epi(const GemmArgs& a, int expected, int rows, hipStream
   }
   auto tiles = [&](int bm, int bn) { return (expected + bm - 1) / bm * ((a.Nout + bn - 1) / bn) * a.ksplit; };
   if (tiles(64, 64) <= 256) return launch_tiled_cfg<EPI, 64, 64, 2, 2, 8>(a, rows, s);
-  if constexpr (is_q8<EPI>() && !q8_wide<EPI>()) {  // outputs whose columns are stored one by one
-    return launch_tiled_cfg<EPI, 128, 128, 2, 1, 4>(a, rows, s);
-  } else {
-    if constexpr (is_q8<EPI>()) {
-      if (tiles(64, 96) <= 256) return launch_tiled_cfg<EPI, 64, 96, 4, 4, 4>(a, rows, s);
-    }
-    if (tiles(64, 128) <= 256) return launch_tiled_cfg<EPI, 64, 128, 2, 2, 6>(a, rows, s);
-    // at least `quarters` quarters of the places in all rounds of t tiles
-    auto full = [](int t, int quarters) { return 4 * t >= quarters * 256 * ((t + 255) / 256); };
-    if constexpr (EPI == EPI_QKV || EPI == EPI_FC1 || is_q8<EPI>()) {
-      const int x = tiles(256, 256);
-      if (x >= 256 && full(x, 4)) return launch_tiled_cfg<EPI, 256, 256, 2, 1, 4>(a, rows, s);
-    }
-    const int l = tiles(256, 128);
-    if (l > 128 && (l <= 256 || full(l, 3))) return launch_tiled_cfg<EPI, 256, 128, 4, 1, 6>(a, rows, s);
-    if (tiles(128, 128) <= 256) return launch_tiled_cfg<EPI, 128, 128, 2, 1, 8>(a, rows, s);
-    return launch_tiled_cfg<EPI, 128, 128, 2, 1, 4>(a, rows, s);
+  if constexpr (is_q8<EPI>()) {
+    if (tiles(64, 96) <= 256) return launch_tiled_cfg<EPI, 64, 96, 4, 4, 4>(a, rows, s);
   }
+  if (tiles(64, 128) <= 256) return launch_tiled_cfg<EPI, 64, 128, 2, 2, 6>(a, rows, s);
+  // at least `quarters` quarters of the places in all rounds of t tiles
+  auto full = [](int t, int quarters) { return 4 * t >= quarters * 256 * ((t + 255) / 256); };
+  constexpr bool BY_COLUMN = is_q8<EPI>() && !q8_wide<EPI>();
+  if constexpr (EPI == EPI_QKV || EPI == EPI_FC1 || (is_q8<EPI>() && !BY_COLUMN)) {
+    const int x = tiles(256, 256);
+    if (x >= 256 && full(x, 4)) return launch_tiled_cfg<EPI, 256, 256, 2, 1, 4>(a, rows, s);
+  }
+  const int l = tiles(256, 128);
+  if (l > 128 && (l <= 256 || (!BY_COLUMN && full(l, 3)))) return launch_tiled_cfg<EPI, 256, 128, 4, 1, 6>(a, rows, s);
+  if (tiles(128, 128) <= 256) return launch_tiled_cfg<EPI, 128, 128, 2, 1, 8>(a, rows, s);
+  return launch_tiled_cfg<EPI, 128, 128, 2, 1, 4>(a, rows, s);
 }
 
 }  // namespace incvit

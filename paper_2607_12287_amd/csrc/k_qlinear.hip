@@ -560,6 +560,10 @@ hipError_t launch_few(const GemmArgs& a0, int expected, hipStream_t s) {
 // 448 x 4304 -> 1152 10.1 against 11.2, 512 rows 13.3 (the former's workgroups
 // pass two to a CU) against 11.2; 512 x 4096 -> 1024 8.9 against 10.6, 576 rows
 // 11.9 against 10.8; 1024 x 192 -> 768 3.9 against 4.4, 2048 rows 5.6 against 4.8.
+// Outputs that end off 16 bytes cost both forms more and meet at the same place
+// (fp32): 546 x 1000 -> 1013 5.9 against 6.6, 1024 rows 8.6 against 7.9; 128 x 1152
+// -> 4305 6.5 against 6.8, 192 rows 7.9 against 7.7; 448 x 4304 -> 1153 11.5 against
+// 12.2, 512 rows 15.3 against 12.4; but 700 x 1000 -> 1013 6.5 against 6.9.
 //
 // Few rows: as many row tiles to a workgroup (each W fragment read once for all)
 // as still leave three workgroups to four CUs, four only beyond 128 rows: 64 x

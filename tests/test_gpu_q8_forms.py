@@ -31,7 +31,8 @@ FORMS = [
 FORMS_ANY = [
     (20, 100, 65, "q_gemm 1,2"), (17, 2500, 65, "q_gemm 1,4"), (100, 320, 1033, "q_gemm 2,2"), (40, 2200, 4305, "q_gemm 2,4"),
     (500, 449, 1145, "q_gemm 4,2"), (300, 4304, 809, "q_gemm 4,4"), (770, 430, 1145, "gemm_tiled 64,64,2,2,8"),
-    (1030, 333, 1145, "gemm_tiled 128,128,2,1,4"), (4090, 330, 2041, "gemm_tiled 128,128,2,1,4"),
+    (1030, 333, 1145, "gemm_tiled 64,96,4,4,4"), (400, 700, 4305, "gemm_tiled 64,128,2,2,6"), (2500, 330, 2041, "gemm_tiled 256,128,4,1,6"),
+    (2048, 200, 2001, "gemm_tiled 128,128,2,1,8"), (4090, 330, 4089, "gemm_tiled 128,128,2,1,4"), (8190, 70, 1985, "gemm_tiled 128,128,2,1,4"),
 ]
 
 

@@ -48,7 +48,7 @@ def test_products_take_the_forms_of_their_tests(tmp_path):
     reached = {w for w in want if "gemm" in w}
     tiles = {f.split()[1] for *_, f in q8.FORMS if f.startswith("gemm_tiled")}
     few = {f.split()[1] for *_, f in q8.FORMS if f.startswith("q_gemm")}
-    assert len(tiles) == 7 and len(few) == 6 and len(reached) == 4 * 13 + 2 * 8
+    assert len(tiles) == 7 and len(few) == 6 and len(reached) == 4 * 13 + 2 * 12
 
 
 def test_head_norms_take_the_instances_of_their_tests(tmp_path):
@@ -99,7 +99,7 @@ def sweep():
         for residual in (False, True):
             for m in rows:
                 for K in (70, 1152, 2200, 6200):
-                    for N in (65, 64, 808, 1144, 1145, 2040, 4088, 4304):
+                    for N in (65, 64, 808, 1144, 1145, 2001, 2040, 4088, 4304, 4305):
                         yield linear(dtype, m, K, N, residual)
             yield linear(dtype, 4090, 70, 4088, residual)
         for d in range(2, 258, 2):
