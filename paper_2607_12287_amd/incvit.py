@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -240,23 +241,26 @@ def incvit_rope_table(rope: incvit_rope, tokens: int, pos: int, axis_stride: int
     return lib().incvit_rope_table(ctypes.addressof(rope), tokens, pos, axis_stride, token_stride, table, stream)
 
 
+_GRIDS = [struct.Struct(f"{n}i{24 - 4 * n}x") for n in range(7)]  # an incvit_grid of n values, the others zero
+
+
 def grid_array(grids, merge: int):
-    """A ctypes array of incvit_grid (or itself) from (t, h, w[, t0[, y0[, x0]]]); ctypes would cut what is past 32 bits to
-    its low half."""
+    """(n, incvit_grid[n] as bytes) of (t, h, w[, t0[, y0[, x0]]]); what is past 32 bits, which ctypes would cut to its low
+    half, is refused."""
     if not -0x80000000 <= merge <= 0x7fffffff:
         raise ValueError("merge: a 32-bit integer")
     if isinstance(grids, ctypes.Array):
-        return grids
-    for g in grids:
-        if max(g) > 0x7fffffff or min(g) < -0x80000000:
-            raise ValueError("grids: sizes and first positions are 32-bit integers")
-    return (incvit_grid * len(grids))(*[tuple(g) for g in grids])
+        return len(grids), bytes(grids)
+    try:
+        return len(grids), b"".join([_GRIDS[len(g)].pack(*g) for g in grids])
+    except (struct.error, IndexError):
+        raise ValueError("grids: (t, h, w[, t0[, y0[, x0]]]) of 32-bit integers") from None
 
 
 def incvit_rope_table_grids(rope: incvit_rope, grids, merge: int, table: int, stream: int = 0) -> int:
     """grids: a ctypes array of incvit_grid, or a sequence of (t, h, w[, t0[, y0[, x0]]])."""
-    arr = grid_array(grids, merge)
-    return lib().incvit_rope_table_grids(ctypes.addressof(rope), len(arr), arr, merge, table, stream)
+    n, arr = grid_array(grids, merge)
+    return lib().incvit_rope_table_grids(ctypes.addressof(rope), n, arr, merge, table, stream)
 
 
 def incvit_qk_norm_rope(c: incvit_qk, rows: int, q: Optional[incvit_heads], k: Optional[incvit_heads], table: int,

@@ -53,7 +53,7 @@ def rope_table(rope: _c.incvit_rope, positions=None, grids=None, merge: int = 1,
             raise ValueError("positions: device int32 [axes][tokens]")
         tokens, device = positions.shape[1], positions.device
     else:
-        arr = _c.grid_array(grids, merge)
+        n_grids, arr = _c.grid_array(grids, merge)
         tokens = 0
         for g in grids:
             tokens += g[0] * g[1] * g[2]
@@ -69,7 +69,7 @@ def rope_table(rope: _c.incvit_rope, positions=None, grids=None, merge: int = 1,
         _call(_c.lib().incvit_rope_table, device, _c.ctypes.byref(rope), tokens, positions.data_ptr(), *positions.stride(),
               out.data_ptr())
     else:
-        _call(_c.lib().incvit_rope_table_grids, device, _c.ctypes.byref(rope), len(arr), arr, merge, out.data_ptr())
+        _call(_c.lib().incvit_rope_table_grids, device, _c.ctypes.byref(rope), n_grids, arr, merge, out.data_ptr())
     return out
 
 
