@@ -38,3 +38,23 @@ def test_without_a_rotation_the_index_is_not_looked_at():
     index = torch.full((7,), -1, dtype=torch.int32, device="cuda")
     for a, b in zip(incvit.qk_norm_rope(q, k, q_gamma=qg, k_gamma=kg, index=index), incvit.qk_norm_rope(q, k, q_gamma=qg, k_gamma=kg)):
         assert torch.equal(a, b)
+
+
+def test_captured_and_replayed():
+    """New outputs inside a captured call: each replay starts them from zeros, whatever was written to them between."""
+    q, k, qg, kg, _, _ = make(40, 16, 16, 72, "bf16")
+    table = make_table(64, 36)
+    index = torch.arange(40, dtype=torch.int32, device="cuda")
+    run = lambda: incvit.qk_norm_rope(q, k, table, q_gamma=qg, k_gamma=kg, index=index)  # noqa: E731
+    run()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = run()
+    for seed in range(3):
+        index.copy_(torch.randint(-30, 64, (40,), generator=torch.Generator().manual_seed(seed)))
+        for t in out:
+            t.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, run()):
+            assert torch.equal(a, b) and not b[index < 0].any()
