@@ -46,7 +46,11 @@
  *     HIP launch errors return INCVIT_ERR_HIP; incvit_last_error() gives text;
  *   - a handle is not thread-safe; handles are independent of each other;
  *   - the library allocates no device memory: weights, caches, workspace,
- *     inputs and outputs are all passed in.
+ *     inputs and outputs are all passed in;
+ *   - this header and the library belong together: incvit_config, the other
+ *     structures and the counts of the enums (INCVIT_K_COUNT) grow from one
+ *     version to the next and carry no size of their own, so a program is
+ *     rebuilt with the header of the library that it loads.
  */
 #ifndef INCVIT_H_
 #define INCVIT_H_
