@@ -441,7 +441,7 @@ size_t incvit_qlinear_rows_bytes(int64_t rows, int32_t K);
  * variance, eps >= 0; gamma NULL: none; beta NULL: zeros), [K] of `dtype`.
  * qrows: incvit_qlinear_rows_bytes(rows, K) bytes, 256-byte aligned; it serves
  * any number of products with the same K.  rows >= 0 (none: nothing is
- * enqueued), rows < 2^31.  Errors and asynchrony as above. */
+ * enqueued), rows < 2^31 - 64.  Errors and asynchrony as above. */
 incvit_status incvit_qlinear_quantize_rows(int32_t dtype, int64_t rows, int32_t K, const void* x,
                                            int64_t x_stride, const void* gamma, const void* beta,
                                            float eps, void* qrows, void* stream);

@@ -33,3 +33,10 @@ def test_pairs_past_32_bits(pairs):
 def test_the_ends_of_32_bits_are_taken():
     assert incvit.incvit_rope_table_grids(ROPE, [(1, 2, 2, 2 ** 31 - 1, -2 ** 31, 5)], 2 ** 31 - 1, T) == incvit.INCVIT_ERR_SHAPE
     assert incvit.incvit_rope_table_grids(ROPE, [], 1, T) == incvit.INCVIT_OK
+
+
+def test_most_rows_of_the_8_bit_products():
+    most = 2 ** 31 - 65
+    assert incvit.incvit_qlinear_rows_bytes(most, 64) == (most + 15) // 16 * (1024 + 64)
+    assert incvit.incvit_qlinear_rows_bytes(most + 1, 64) == 0
+    assert incvit.incvit_qlinear_quantize_rows(1, most + 1, 64, T, 64, 0, 0, 1e-6, 2 * T) == incvit.INCVIT_ERR_ARG
