@@ -206,9 +206,10 @@ struct ResRun {
     if constexpr (std::is_same<T, float>::value) return __uint_as_float(w[j]);
     else return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
   }
-  // 16-byte stores of bf16 go past the L2 of the XCD that made them (8192 x 1024 ->
-  // 4096 48.6 -> 46 us, 4096 x 768 -> 2304 15.5 -> 14.2, and what reads them next is
-  // no slower); stores of parts of lines must not
+  // 16-byte stores of bf16 go past the L2 of the XCD that made them (in graphs, 8192 x
+  // 1024 -> 4096 with GELU 55 -> 46 us, 4096 x 768 -> 2304 16.1 -> 14.7, 1024 x 4304 ->
+  // 1152 13.7 either way, and what reads them next is no slower); stores of parts of
+  // lines must not
   __device__ __forceinline__ void store(T* p, const float* y) {
     if constexpr (std::is_same<T, float>::value) {
       *reinterpret_cast<float4*>(p) = make_float4(y[0], y[1], y[2], y[3]);

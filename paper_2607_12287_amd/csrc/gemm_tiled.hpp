@@ -46,9 +46,10 @@
 // The same loop multiplies 8-bit integers (EPI_QBF, EPI_QF32; v_mfma_i32_16x16x64_i8,
 // exact int32 sums): a fragment is 16 rows or columns by 64 values, again a
 // kilobyte, and the epilogue applies the rows' and columns' scales.  8192 x 1024
-// -> 4096 with GELU: 43 us, of which the K loop is 23 (14 at the matrix rate) and the
-// rest the epilogue, which one workgroup per CU does not overlap with it: 67 MB of
-// stores (a fill of as much takes 11) and the GELU (4 to 8).
+// -> 4096 with GELU: 46 us in a graph, of which the K loop is 23 (25 at the 2720 TOP/s
+// that 8192 x 8192 -> 8192 reaches) and the rest the epilogue, which one workgroup
+// per CU does not overlap with it: 67 MB of stores (a fill of as much takes 11) and
+// the GELU (41 without it).
 //
 // bf16 models only otherwise (fp32 models use the small-M kernel).  Results do not
 // depend on the tile shape beyond the fp32 order of the MFMA accumulation,
@@ -407,7 +408,8 @@ __global__ __launch_bounds__(512, (2 * tiled_per_cu<EPI, BM, BN, KD, NS>())) voi
     if constexpr (Q8) {
       // Lane (g, n) holds columns 4g..4g+3 of row n of each 16x16 tile.  For bf16
       // two neighbouring blocks are joined first, so that a lane stores 16 bytes
-      // and a row's 4 lanes 64 in a row (8192 x 1024 -> 4096: 57 us without, 52 with).  The
+      // and a row's 4 lanes 64 in a row (8192 x 1024 -> 4096 with GELU: 61 us without, 46
+      // with).  The
       // scales of a lane's rows are loaded once, its columns' operands and its
       // residuals while the run before is worked on; loads run for every lane
       // (clamped) and only the stores are masked, as below.

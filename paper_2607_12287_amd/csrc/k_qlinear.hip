@@ -3,12 +3,13 @@
 // with q = round(x / s), s = max |x| / 127 over a row's K values, and likewise
 // for the columns of W.  Sums of 8-bit products are exact in int32 (K <= 65536).
 //
-// The kernels (us and rates of single launches on an MI355X, bf16):
+// The kernels (us of a launch within a graph on an MI355X, bf16):
 //   * q_rows_kernel: one or four waves per row find its largest magnitude and
 //     write the row's integers in the matrix instruction's operand order (with a
 //     LayerNorm before it, whose statistics are two passes over registers).
-//     Bound by memory: 8192 x 1024 8.2 us (3.1 TB/s), 8192 x 4096 25 (4.0 TB/s),
-//     23 x 1152 3.2 (latency);
+//     8192 x 1024 7.2 us (3.5 TB/s; fp32 9.1 and 4.6, a copy 5.1), behind a LayerNorm
+//     9.8; 8192 x 4096 27 and 39; 1024 x 4304 5.3 and 8.2; 23 x 1152 2.5 and 3.9 (latency).
+//     Counters give each byte read and written once;
 //   * q_tile_kernel: the same for the encoder's rows in operand order;
 //   * q_gemm_kernel, few rows: weights stream past them once.  A workgroup owns
 //     16 columns; its waves take the K chunks in turn, so every wave has loads of
@@ -43,7 +44,7 @@ __device__ __forceinline__ int q_value(float x, float s) {
 // faithful and the second correctly rounded (Markstein's theorem: a faithful
 // quotient, its exact residual and the correctly rounded reciprocal).  With x
 // and the row's largest magnitude bf16 numbers (BF), one step gives the same
-// integer: shown for every pair of their significands and exponents.  Adding
+// integer, which a test shows for every pair of their significands.  Adding
 // 1.5 * 2^23 rounds to an integer, ties to even, in the low bits; |x / s| is
 // below 127.5, so no clamp.
 __device__ __forceinline__ bool q_plain(float s) { return s > 0x1p-90f && s < 0x1p90f; }

@@ -6,10 +6,12 @@
 // rest's sine and cosine are Taylor polynomials in fp32 (|x| <= pi/4: the first
 // dropped terms are 1.8e-9 and 1.2e-10), swapped and signed by q.
 //
-// Bound: the table's bytes (8 per token and pair), and for a single frame the
-// launch: 256 tokens of 36 pairs 3.4 us; a 6.7 MB table of video grids 6.0.  A
-// thread forms two pairs of one token, 16 bytes, and finds the token's
-// place in its grid by products with reciprocals in fp64.
+// Bound: for a few thousand tokens the launch (256 tokens of 36 pairs 3.4 us in
+// a trace); then the tokens' places and the table's bytes (8 per token and
+// pair).  A 6.7 MB table of video grids takes 4.7 us in a graph: 1.0 of it for the
+// places (3.75 without), 0.3 for sines and cosines (4.4 without), while a fill of
+// the bytes takes 2.7.  A thread forms two pairs of one token, 16 bytes, and finds
+// the token's place in its grid by products with reciprocals in fp64.
 #include <cmath>
 
 #include "ops.hpp"
