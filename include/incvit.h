@@ -466,6 +466,128 @@ incvit_status incvit_qlinear(int32_t dtype, int64_t rows, int32_t K, int32_t N, 
                              const void* residual, int64_t res_stride, void* out,
                              int64_t out_stride, void* workspace, void* stream);
 
+/* --------------------------------------- a cache of keys and values, 8 bits -- */
+
+/* Keys and values of `heads` heads in blocks of `block` tokens (16, 32, 64 or
+ * 128), from a pool of `blocks` of them that the caller hands out to sequences.
+ * A token's slot is block number * block + its place in the block.  For keys and
+ * values apart, each block and head has one fp32 scale s, and a value is q * s
+ * with an integer q in [-127, 127].  head_dim: a multiple of 8 in [8, 256], stored
+ * padded to 32, 64, 80, 96, 128, 192 or 256.  1 <= heads <= 1024, blocks >= 1,
+ * blocks * block < 2^31; otherwise INCVIT_ERR_UNSUPPORTED (or a size of 0). */
+typedef struct {
+  int32_t blocks, block, heads, head_dim;
+} incvit_kv;
+
+/* Bytes of a cache, which is 256-byte aligned device memory.  All zeros is a
+ * cache of zeros. */
+size_t incvit_kv_bytes(const incvit_kv* c);
+
+/* Quantise `rows` rows of new keys and values as they are written: head h of row
+ * r starts at element r * k_row + h * k_head of k (strides in elements, in [0,
+ * 2^40]; views of a projection's output will do) and its values lie one after
+ * another; likewise v.  dtype: incvit_dtype of both.  Row r goes to slots[r]
+ * (device int32 [rows]); a row whose slot is outside the pool (padding: negative)
+ * goes nowhere.  Rows of one block have to follow one another; of rows of one
+ * slot the last one stays.  For each block that is written, and head:
+ *   a = max |x| over the new rows' values, s_new = a / 127 rounded to fp32 (NaN
+ *     where a value is not finite), s = max(s_old, s_new), NaN if either is;
+ *   new values: x / s rounded to fp32, then to the nearest integer (ties to
+ *     even), limited to 127;
+ *   kept ones, where s > s_old: q * r rounded to fp32, then to the nearest
+ *     integer, with r = s_old / s rounded to fp32;
+ * and with s zero or NaN all integers are 0.  A block keeps nothing (s_old and
+ * the other slots are 0) if all of its slots are written, or if begin is 1 and
+ * its first slot is: a sequence that goes on into a block used before.
+ * Pointers aligned to 16 bytes, strides too (multiples of 8 elements, fp32: of
+ * 4).  rows >= 0 (none: nothing is enqueued), rows * heads <= 2^24.  Errors:
+ * INCVIT_ERR_ARG or INCVIT_ERR_UNSUPPORTED (text: incvit_last_error(NULL)).
+ * Asynchronous on `stream`; calls on one cache must not run at once. */
+incvit_status incvit_kv_write(const incvit_kv* c, int32_t dtype, int64_t rows, const void* k,
+                              int64_t k_row, int64_t k_head, const void* v, int64_t v_row,
+                              int64_t v_head, const int32_t* slots, int32_t begin, void* cache,
+                              void* stream);
+
+/* Read slots back, q * s in fp32 rounded to dtype: strides, alignments, slots and
+ * errors as above; slots may repeat, heads of k and v must not overlap.  A row
+ * whose slot is outside the pool is left as it was. */
+incvit_status incvit_kv_read(const incvit_kv* c, const void* cache, int32_t dtype, int64_t rows,
+                             const int32_t* slots, void* k, int64_t k_row, int64_t k_head, void* v,
+                             int64_t v_row, int64_t v_head, void* stream);
+
+/* -------------------------------------------------------------- attention -- */
+
+/* Softmax attention of query heads over grouped keys and values.  Query head h
+ * sees key head h / (q_heads / kv_heads).  The queries of a sequence with `len`
+ * keys are its last q_len tokens: query i is at position p = len - q_len + i, and
+ * sees key j, 0 <= j < len, where
+ *   causal = 0 or j <= p, and
+ *   window = 0, or |p - j| < window, or j < sinks (first tokens that stay
+ *   visible; they count only with a window).
+ * out = sum_j softmax_j(scale * q . k_j) v_j over the keys it sees, zeros where it
+ * sees none; keys and values that it does not see have no effect on it, whatever
+ * they hold.  Scores, softmax and sums are fp32; with bf16 the weights are rounded
+ * to bf16 for their product with the values; one rounding to dtype at the end.
+ * head_dim: as incvit_kv's, of keys and values alike; q_heads a multiple of
+ * kv_heads, both in [1, 1024]; window and sinks in [0, 2^30]; fill 0 or 1; scale >
+ * 0, finite. */
+typedef struct {
+  int32_t dtype; /* incvit_dtype of queries and output (and of given keys and values) */
+  int32_t q_heads, kv_heads, head_dim;
+  int32_t causal; /* 0 or 1 */
+  int32_t window, sinks;
+  int32_t fill; /* rows behind the last sequence: 0 left as they were, 1 zeros */
+  float scale;
+} incvit_attention;
+
+/* Rows of heads: head h of row r starts at element r * row + h * head of p, its
+ * values lie one after another; strides in [0, 2^40] elements.  p and strides are
+ * 16-byte aligned.  Heads of an output must not overlap. */
+typedef struct {
+  const void* p;
+  int64_t row, head;
+} incvit_rows;
+
+/* Bytes of the workspace of an attention call (0 if out of range, or if the call
+ * needs none): partial results of sequences whose keys are split over workgroups.
+ * cached: 1 for incvit_kv_attend, 0 for incvit_attend; the other arguments as
+ * given to them. */
+size_t incvit_attention_workspace_bytes(const incvit_attention* a, int32_t cached, int32_t n,
+                                        int64_t rows, int32_t ragged, int64_t max_len);
+
+/* Attention over a cache.  n sequences; those of `rows` query rows:
+ *   q_start: device int32 [n + 1], ascending from 0: sequence i has query rows
+ *     [q_start[i], q_start[i + 1]); rows from q_start[n] on follow a->fill.
+ *     NULL: rows / n for each (rows a multiple of n);
+ *   lens: device int32 [n], keys of each sequence, its queries' among them (a
+ *     query whose position is negative sees what the mask lets it);
+ *   table: device int32, block e of sequence i at table[i * table_stride + e], e <
+ *     width; keys past width * block, and those of a block number outside the pool,
+ *     are not seen.
+ * max_len: about the most keys of a sequence, for the split over workgroups; the
+ * result does not depend on it beyond the order of sums (0: width * block).
+ * c->heads and c->head_dim are a's.  workspace: incvit_attention_workspace_bytes
+ * bytes (with ragged = (q_start != NULL) and the max_len of the call, not 0),
+ * 256-byte aligned, the call's own until it has run on `stream`; NULL if 0.
+ * n >= 0, rows >= 0 (none: nothing is enqueued), rows * (q_heads / kv_heads) <
+ * 2^30.  Errors: INCVIT_ERR_ARG, INCVIT_ERR_SHAPE or INCVIT_ERR_UNSUPPORTED
+ * (text: incvit_last_error(NULL)).  Asynchronous on `stream`. */
+incvit_status incvit_kv_attend(const incvit_attention* a, const incvit_kv* c, const void* cache,
+                               int32_t n, int64_t rows, const int32_t* q_start,
+                               const int32_t* table, int64_t table_stride, int32_t width,
+                               const int32_t* lens, int64_t max_len, const incvit_rows* q,
+                               const incvit_rows* out, void* workspace, void* stream);
+
+/* Attention over given keys and values of a's dtype, packed one sequence after
+ * another: k_start device int32 [n + 1], ascending from 0, sequence i has key rows
+ * [k_start[i], k_start[i + 1]) of key_rows; NULL: key_rows / n for each (a multiple
+ * of n).  max_len 0: key_rows / n.  key_rows in [0, 2^30]; the rest as above. */
+incvit_status incvit_attend(const incvit_attention* a, int32_t n, int64_t rows,
+                            const int32_t* q_start, int64_t key_rows, const int32_t* k_start,
+                            int64_t max_len, const incvit_rows* q, const incvit_rows* k,
+                            const incvit_rows* v, const incvit_rows* out, void* workspace,
+                            void* stream);
+
 /* ------------------------------------------------------------ HIP graphs -- */
 
 typedef struct incvit_graph incvit_graph;

@@ -1,0 +1,349 @@
+// The cache of keys and values in 8 bits and the attention operators: layouts,
+// arguments, launchers, and what both attention kernels share.
+#pragma once
+
+#include <atomic>
+
+#include "ops.hpp"
+
+namespace incvit {
+
+// ------------------------------------------------------------------ cache --
+
+// Head dims are stored padded to one of these.
+__host__ __device__ constexpr int kv_dims(int d) {
+  return d <= 32 ? 32 : d <= 64 ? 64 : d <= 80 ? 80 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256;
+}
+
+// Scales [blocks][heads] (key, value), then the integers [blocks][heads]: a block
+// of a head is its keys (block * ds bytes), then its values.  Both lie in groups
+// of 16 tokens (16 * ds bytes), in the operand order of the attention's matrix
+// instructions, so that one load per lane is one operand:
+//   keys:   [dims / 16][token][16 dims];
+//   values: chunks of 64 dims (the last of the 16 P that are left, P = 1, 2 or 4);
+//           a chunk is [token / 4][16 P dims][token % 4].
+struct KvLayout {
+  int block, heads, ds, lb;  // lb: log2 of a block's groups
+  size_t head_bytes;         // of one block and head: keys and values
+  size_t data, total;
+  __host__ __device__ KvLayout(int blocks, int block_, int heads_, int d) : block(block_), heads(heads_), ds(kv_dims(d)) {
+    lb = block == 16 ? 0 : block == 32 ? 1 : block == 64 ? 2 : 3;
+    head_bytes = (size_t)2 * block * ds;
+    data = q_align((size_t)blocks * heads * 8);
+    total = data + q_align((size_t)blocks * heads * head_bytes);
+  }
+};
+
+struct KvSide {
+  const void* p;
+  long row, head;
+};
+
+struct KvWriteArgs {
+  KvSide x[2];  // keys, values
+  const int* slots;
+  char* cache;
+  size_t data;
+  long rows;
+  int blocks, block, heads, d, begin, dtype;
+};
+
+struct KvReadArgs {
+  KvSide x[2];  // written
+  const int* slots;
+  const char* cache;
+  size_t data;
+  long rows;
+  int blocks, block, heads, d, dtype;
+};
+
+hipError_t launch_kv_write(const KvWriteArgs& a, hipStream_t s);
+hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t s);
+
+// -------------------------------------------------------------- attention --
+
+constexpr int kKeyTile = 32;   // keys that a wave takes at once
+constexpr int kKeyWaves = 4;   // waves of a workgroup
+
+struct AttendArgs {
+  const int* q_start;  // null: q_len rows for each sequence
+  const int* k_start;  // plain: null: k_len keys for each
+  const int* lens;     // cached
+  const int* table;
+  const char* cache;
+  size_t data;         // of the cache's integers
+  KvSide q, k, v, out;
+  long table_stride;
+  float* parts;        // workspace
+  long rows, key_rows;
+  int n, q_len, k_len, width, blocks, lb;
+  int hq, hk, group, d;
+  int causal, window, sinks;
+  int fill;            // with q_start: rows behind the last sequence as those of one without keys
+  float scale_log2;    // scale * log2(e)
+  int most_rows;       // rows * group of a sequence at most
+  int tiles;           // row tiles of the call
+  int tiles_each;      // of each sequence (q_start null)
+  int splits, chunk;   // most workgroups that share a row tile's keys; key tiles of one at least
+};
+
+// 16-row tiles of a workgroup over the cache, at most: as many as the registers hold.
+constexpr int most_row_tiles(bool bf16, int ds) { return bf16 ? (ds <= 96 ? 4 : ds <= 192 ? 2 : 1) : ds <= 128 ? 2 : 1; }
+
+struct AttendPlan {
+  int nt;              // 16-row tiles of a workgroup
+  long tiles;          // row tiles
+  int tiles_each, splits, chunk;
+  size_t bytes;        // workspace
+};
+AttendPlan attend_plan(const incvit_attention& a, bool cached, long n, long rows, bool ragged, long max_len);
+
+hipError_t launch_kv_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
+hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
+hipError_t launch_attend_join(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
+
+}  // namespace incvit
+
+#if defined(__HIPCC__)
+namespace incvit {
+
+// Where a row tile is: rows [first, first + rows) of a sequence's q_len * group
+// rows (token by token, the heads of a group together), whose token 0 is row q0
+// of the call; its keys: k0 (plain) and len.
+struct RowTile {
+  int seq, first, q_len, len;
+  long q0, k0;
+};
+
+// The tile number f of the launch.  Ragged: sequence i's tiles count from
+// floor(q_start[i] * group / TR) + i on, which leaves each enough numbers, so a
+// wave finds the sequence by counting the starts up to f, 64 at a time.  Whatever
+// the starts hold, the rows are within the call's.
+template <int TR>
+__device__ __forceinline__ bool row_tile(const AttendArgs& a, int f, RowTile& w) {
+  if (!a.q_start) {
+    w.seq = f / a.tiles_each;
+    w.first = (f - w.seq * a.tiles_each) * TR;
+    w.q_len = a.q_len;
+    w.q0 = (long)w.seq * a.q_len;
+  } else {
+    const int lane = threadIdx.x & 63;
+    const int n = a.n + a.fill;
+    int count = 0;
+    for (int i = 0; i < n; i += 64) {
+      const int j = min(i + lane, n - 1);
+      const long at = min(max((long)gbl(a.q_start)[j], 0L), a.rows);
+      const bool up = i + lane < n && (at * a.group) / TR + j <= f;
+      count += __popcll(__ballot(up));
+    }
+    if (count == 0) return false;
+    w.seq = __builtin_amdgcn_readfirstlane(count - 1);
+    const long q0 = min(max((long)gbl(a.q_start)[w.seq], 0L), a.rows);
+    const long q1 = w.seq < a.n ? min(max((long)gbl(a.q_start)[w.seq + 1], q0), a.rows) : a.rows;
+    w.first = (int)(f - (q0 * a.group) / TR - w.seq) * TR;
+    w.q_len = (int)(q1 - q0);
+    w.q0 = q0;
+  }
+  return w.first >= 0 && w.first < w.q_len * a.group;  // below 0: starts that do not ascend
+}
+
+// Keys of a sequence: at most 2^30, so that no position below overflows.
+constexpr int kMostKeys = 1 << 30;
+__device__ __forceinline__ int cached_len(const AttendArgs& a, int seq) {
+  if (seq >= a.n) return 0;
+  return max(min(gbl(a.lens)[seq], (int)min((long)a.width * (16 << a.lb), (long)kMostKeys)), 0);
+}
+// (and the first one's row, k0)
+__device__ __forceinline__ int plain_len(const AttendArgs& a, RowTile& w) {
+  w.k0 = (long)w.seq * a.k_len;
+  if (w.seq >= a.n) return 0;
+  if (!a.k_start) return a.k_len;
+  const long k0 = min(max((long)gbl(a.k_start)[w.seq], 0L), a.key_rows), k1 = min(max((long)gbl(a.k_start)[w.seq + 1], k0), a.key_rows);
+  w.k0 = k0;
+  return (int)(k1 - k0);
+}
+
+// Key tiles that some row of a row tile sees: n0 from key 0 on (the sinks, where
+// they are apart from the window), then those from `t1` on; nt in all.  p0, p1:
+// the first and the last row's position.
+struct KeyTiles {
+  int n0, t1, nt;
+  int p0, p1;
+  __device__ __forceinline__ int at(int i) const { return i < n0 ? i : i - n0 + t1; }
+};
+__device__ __forceinline__ KeyTiles key_tiles(const AttendArgs& a, const RowTile& w, int tr) {
+  KeyTiles k;
+  const int last = min(w.first + tr, w.q_len * a.group) - 1;
+  k.p0 = w.len - w.q_len + w.first / a.group;
+  k.p1 = w.len - w.q_len + last / a.group;
+  const int top = max(0, a.causal ? min(w.len, k.p1 + 1) : w.len);
+  int lo = 0, hi = top;
+  k.n0 = 0;
+  if (a.window) {
+    lo = max(0, k.p0 - a.window + 1);
+    if (!a.causal) hi = max(0, min(top, k.p1 + a.window));  // both at most 2^30
+  }
+  k.t1 = lo / kKeyTile;
+  int t2 = lo < hi ? (hi + kKeyTile - 1) / kKeyTile : k.t1;
+  if (a.window && a.sinks) {
+    const int s = (min(a.sinks, top) + kKeyTile - 1) / kKeyTile;
+    if (s >= k.t1) {
+      k.t1 = 0;
+      t2 = max(t2, s);
+    } else {
+      k.n0 = s;
+    }
+  }
+  k.nt = k.n0 + t2 - k.t1;
+  return k;
+}
+
+// Workgroups that share nt key tiles, and the share of workgroup s.
+__device__ __forceinline__ int key_shares(const AttendArgs& a, int nt) { return max(1, min(a.splits, (nt + a.chunk - 1) / a.chunk)); }
+
+// A row's partial result: m, the largest score in units of log2; l, the sum of
+// 2^(x - m); O.  m = -inf: no key was seen.  kNoMax: keys were seen, none above -inf.
+constexpr float kNoMax = -3.0e38f;
+
+// max, sum and "any" over the four lane groups (lanes n, n + 16, n + 32, n + 48)
+__device__ __forceinline__ float group4_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const float y = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+__device__ __forceinline__ float group4_sum(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const float y = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
+// fp32 values as sums of bf16 numbers, without a rounding: the leading 8 bits of
+// the significand, the next 8 and the last 8.
+__device__ __forceinline__ uint32_t top_halves(float lo, float hi) {
+  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+}
+__device__ __forceinline__ float without_top(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+
+__device__ __forceinline__ void floats_of(const V8<float>& x, float* y) {
+  y[0] = x.a.x, y[1] = x.a.y, y[2] = x.a.z, y[3] = x.a.w, y[4] = x.b.x, y[5] = x.b.y, y[6] = x.b.z, y[7] = x.b.w;
+}
+__device__ __forceinline__ void floats_of(const V8<uint16_t>& x, float* y) {
+  const uint32_t w[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[2 * i] = __uint_as_float(w[i] << 16);
+    y[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+
+// PARTS = 1: x rounded to bf16; 3: x exactly
+template <int PARTS>
+__device__ __forceinline__ void split8(const float* x, uint4* out) {
+  if constexpr (PARTS == 1) {
+    out[0] = make_uint4(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(x[4], x[5]), f2bf2(x[6], x[7]));
+  } else {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      out[k] = make_uint4(top_halves(r[0], r[1]), top_halves(r[2], r[3]), top_halves(r[4], r[5]), top_halves(r[6], r[7]));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = without_top(r[i]);
+    }
+  }
+}
+
+__device__ __forceinline__ f32x4_t mma16(const uint4& a, const uint4& b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// One step of the online softmax for a lane's 8 scores x (in units of log2, -inf
+// where masked) of one query: p = 2^(x - m), and the factor for what was summed.
+__device__ __forceinline__ float soft_step(const float* x, float& m, float& l, float* p) {
+  float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+  const float m_new = fmaxf(m, group4_max(top));
+  const float sub = m_new == -INFINITY ? 0.0f : m_new;  // nothing yet: every p is 0
+  const float alpha = __builtin_amdgcn_exp2f(m - sub);
+  float sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    p[j] = __builtin_amdgcn_exp2f(x[j] - sub);
+    sum += p[j];
+  }
+  l = fmaf(l, alpha, sum);
+  m = m_new;
+  return alpha;
+}
+
+// `bytes` of dynamic LDS for kernel F on the current device: above 64 KB they are
+// asked for once on each.
+template <auto F>
+hipError_t with_lds(int bytes) {
+  static std::atomic<bool> done[kMaxDevices];
+  if (bytes <= 65536) return hipSuccess;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess || (dev >= 0 && dev < kMaxDevices && done[dev])) return e;
+  e = hipFuncSetAttribute(reinterpret_cast<const void*>(F), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess && dev >= 0 && dev < kMaxDevices) done[dev] = true;
+  return e;
+}
+
+template <class T>
+__device__ __forceinline__ void store_out4(T* dst, const float* v) {
+  if constexpr (sizeof(T) == 2) *(INCVIT_GLOBAL u32x2_t*)dst = u32x2_t{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+  else *(INCVIT_GLOBAL f32x4_t*)dst = f32x4_t{v[0], v[1], v[2], v[3]};
+}
+
+// LDS of the exchange between a workgroup's waves: m, l, then O
+template <int DS, int NT>
+constexpr int exchange_bytes() {
+  return kKeyWaves * NT * 16 * (8 + 4 * (DS + 4));
+}
+
+// Joins the waves' partial results, which they have put into LDS (m, l
+// [wave][row], O [wave][row][DS + 4]), and stores rows below `rows`: the result
+// where the tile's keys are one workgroup's, else the partial result.
+template <class T, int DS, int NT>
+__device__ __forceinline__ void join_waves(const AttendArgs& a, const RowTile& w, const char* lds, int h, int share, int shares, int f) {
+  constexpr int TR = 16 * NT;
+  const float* s_m = reinterpret_cast<const float*>(lds);
+  const float* s_l = s_m + kKeyWaves * TR;
+  const float* s_o = s_l + kKeyWaves * TR;
+  const int rows = min(TR, w.q_len * a.group - w.first);
+  float* part = a.parts + ((size_t)((long)f * a.hk + h) * a.splits + share) * TR * (DS + 2);
+  for (int i = threadIdx.x; i < rows * (DS / 4); i += 64 * kKeyWaves) {
+    const int r = i / (DS / 4), d = (i - r * (DS / 4)) * 4;
+    float m = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < kKeyWaves; ++k) m = fmaxf(m, s_m[k * TR + r]);
+    float l = 0.0f;
+    f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < kKeyWaves; ++k) {
+      const float mk = s_m[k * TR + r];
+      const float e = mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk - m);
+      l += e * s_l[k * TR + r];
+      o += *reinterpret_cast<const f32x4_t*>(s_o + (size_t)(k * TR + r) * (DS + 4) + d) * e;
+    }
+    if (shares > 1) {
+      if (d == 0) *(INCVIT_GLOBAL u32x2_t*)(part + 2 * r) = u32x2_t{__float_as_uint(m), __float_as_uint(l)};
+      *(INCVIT_GLOBAL f32x4_t*)(part + 2 * TR + r * DS + d) = o;
+    } else if (d < a.d) {
+      const int row = w.first + r, tok = row / a.group, head = h * a.group + row - tok * a.group;
+      const float inv = 1.0f / l;
+      float y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = m == -INFINITY ? 0.0f : o[j] * inv;
+      store_out4<T>(static_cast<T*>(const_cast<void*>(a.out.p)) + (w.q0 + tok) * a.out.row + (long)head * a.out.head + d, y);
+    }
+  }
+}
+
+}  // namespace incvit
+#endif

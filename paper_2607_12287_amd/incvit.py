@@ -42,7 +42,9 @@ EXPORTS = ("incvit_canonical_weights_bytes", "incvit_packed_weights_bytes", "inc
            "incvit_graph_launch", "incvit_graph_destroy", "incvit_set_tuning", "incvit_encode_frame",
            "incvit_flow_two_anchor", "incvit_step_noalloc", "incvit_rope_table", "incvit_rope_table_grids",
            "incvit_qk_norm_rope", "incvit_qlinear_weights_bytes", "incvit_qlinear_rows_bytes",
-           "incvit_qlinear_pack_weights", "incvit_qlinear_quantize_rows", "incvit_qlinear_multiply", "incvit_qlinear")
+           "incvit_qlinear_pack_weights", "incvit_qlinear_quantize_rows", "incvit_qlinear_multiply", "incvit_qlinear",
+           "incvit_kv_bytes", "incvit_kv_write", "incvit_kv_read", "incvit_attention_workspace_bytes", "incvit_kv_attend",
+           "incvit_attend")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 
 
@@ -79,6 +81,20 @@ class incvit_heads(ctypes.Structure):
     _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("gamma", ctypes.c_void_p),
                 ("beta", ctypes.c_void_p), ("in_row", ctypes.c_int64), ("in_head", ctypes.c_int64),
                 ("out_row", ctypes.c_int64), ("out_head", ctypes.c_int64), ("heads", ctypes.c_int32)]
+
+
+class incvit_kv(ctypes.Structure):
+    _fields_ = [("blocks", ctypes.c_int32), ("block", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class incvit_attention(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("fill", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class incvit_rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
 class IncvitError(RuntimeError):
@@ -133,6 +149,12 @@ def lib() -> ctypes.CDLL:
             "incvit_qlinear_quantize_rows": (I32, [I32, I64, I32, P, I64, P, P, F32, P, P]),
             "incvit_qlinear_multiply": (I32, [I32, I64, I32, I32, P, P, I32, P, I64, P, I64, P]),
             "incvit_qlinear": (I32, [I32, I64, I32, I32, P, I64, P, I32, P, I64, P, I64, P, P]),
+            "incvit_kv_bytes": (S, [P]),
+            "incvit_kv_write": (I32, [P, I32, I64, P, I64, I64, P, I64, I64, P, I32, P, P]),
+            "incvit_kv_read": (I32, [P, P, I32, I64, P, P, I64, I64, P, I64, I64, P]),
+            "incvit_attention_workspace_bytes": (S, [P, I32, I32, I64, I32, I64]),
+            "incvit_kv_attend": (I32, [P, P, P, I32, I64, P, P, I64, I32, P, I64, P, P, P, P]),
+            "incvit_attend": (I32, [P, I32, I64, P, I64, P, I64, P, P, P, P, P, P]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -312,6 +334,42 @@ def incvit_qlinear(dtype: int, rows: int, K: int, N: int, x: int, x_stride: int,
                                 workspace, stream)
 
 
+def _addr(c):
+    return None if c is None else ctypes.addressof(c)
+
+
+def incvit_kv_bytes(c: incvit_kv) -> int:
+    return lib().incvit_kv_bytes(_addr(c))
+
+
+def incvit_kv_write(c: incvit_kv, dtype: int, rows: int, k: int, k_row: int, k_head: int, v: int, v_row: int, v_head: int,
+                    slots: int, begin: int, cache: int, stream: int = 0) -> int:
+    return lib().incvit_kv_write(_addr(c), dtype, rows, k, k_row, k_head, v, v_row, v_head, slots, begin, cache, stream)
+
+
+def incvit_kv_read(c: incvit_kv, cache: int, dtype: int, rows: int, slots: int, k: int, k_row: int, k_head: int, v: int,
+                   v_row: int, v_head: int, stream: int = 0) -> int:
+    return lib().incvit_kv_read(_addr(c), cache, dtype, rows, slots, k, k_row, k_head, v, v_row, v_head, stream)
+
+
+def incvit_attention_workspace_bytes(a: incvit_attention, cached: int, n: int, rows: int, ragged: int, max_len: int) -> int:
+    return lib().incvit_attention_workspace_bytes(_addr(a), cached, n, rows, ragged, max_len)
+
+
+def incvit_kv_attend(a: incvit_attention, c: incvit_kv, cache: int, n: int, rows: int, q_start: int, table: int, table_stride: int,
+                     width: int, lens: int, max_len: int, q: Optional[incvit_rows], out: Optional[incvit_rows], workspace: int,
+                     stream: int = 0) -> int:
+    return lib().incvit_kv_attend(_addr(a), _addr(c), cache, n, rows, q_start, table, table_stride, width, lens, max_len, _addr(q),
+                                  _addr(out), workspace, stream)
+
+
+def incvit_attend(a: incvit_attention, n: int, rows: int, q_start: int, key_rows: int, k_start: int, max_len: int,
+                  q: Optional[incvit_rows], k: Optional[incvit_rows], v: Optional[incvit_rows], out: Optional[incvit_rows],
+                  workspace: int, stream: int = 0) -> int:
+    return lib().incvit_attend(_addr(a), n, rows, q_start, key_rows, k_start, max_len, _addr(q), _addr(k), _addr(v), _addr(out),
+                               workspace, stream)
+
+
 def incvit_cache_export(h, cache: int, dst: int, stream: int = 0) -> int:
     return lib().incvit_cache_export(h, cache, dst, stream)
 
@@ -375,7 +433,7 @@ def incvit_set_tuning(h, cols: Optional[Sequence[int]] = None, attn_qtiles: int 
 # --- operators on torch tensors ------------------------------------------------
 
 # They live in ops.py, which needs torch to be imported; this module does not.
-_OPS = ("rope_table", "qk_norm_rope", "quantize_rows", "QRows", "QLinear")
+_OPS = ("rope_table", "qk_norm_rope", "quantize_rows", "QRows", "QLinear", "KVCache", "attend")
 
 
 def __getattr__(name: str):

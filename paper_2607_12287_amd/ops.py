@@ -18,6 +18,9 @@ _CODES = {_F32: _c.INCVIT_F32, _BF16: _c.INCVIT_BF16, torch.int8: _c.INCVIT_I8}
 # incvit_heads and incvit_qk as their bytes: 0.1 us each, a ctypes structure 0.4
 _HEADS, _QK = struct.Struct("4P4qi4x"), struct.Struct("5if")
 assert _HEADS.size == _c.ctypes.sizeof(_c.incvit_heads) and _QK.size == _c.ctypes.sizeof(_c.incvit_qk)
+_KV, _ATTENTION, _ROWS = struct.Struct("4i"), struct.Struct("8if"), struct.Struct("P2q")
+assert (_KV.size == _c.ctypes.sizeof(_c.incvit_kv) and _ATTENTION.size == _c.ctypes.sizeof(_c.incvit_attention) and
+        _ROWS.size == _c.ctypes.sizeof(_c.incvit_rows))
 _stream_of = torch._C._cuda_getCurrentRawStream
 _current = torch._C._cuda_getDevice
 
@@ -246,3 +249,189 @@ class QLinear:
             _call(L.incvit_qlinear, dev, code, rows, K, N, x.data_ptr(), x.stride(0), self.weights.data_ptr(), bool(gelu), r, rs,
                   out.data_ptr(), out.stride(0), ws.data_ptr())
         return out
+
+
+# ------------------------------- a cache of keys and values in 8 bits --------
+
+
+def _head_rows(t, who: str):
+    """Checks rows of heads [rows][heads][d], the values of a head one after another; the type code."""
+    code = _CODES.get(t.dtype, _c.INCVIT_I8)
+    if not (t.is_cuda and code != _c.INCVIT_I8 and t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] == 1)):
+        raise ValueError(f"{who}: device fp32 or bf16 [rows][heads][d], the values of a head one after another")
+    return code
+
+
+def _indexes(t, n: int, device, who: str):
+    if not (t.dtype == torch.int32 and t.device == device and t.dim() == 1 and t.shape[0] == n and t.is_contiguous()):
+        raise ValueError(f"{who}: device int32 [{n}]")
+    return t.data_ptr()
+
+
+def _starts(t, device, who: str):
+    """(address, sequences) of starts [n + 1]."""
+    if not (t.dtype == torch.int32 and t.device == device and t.dim() == 1 and t.shape[0] >= 1 and t.is_contiguous()):
+        raise ValueError(f"{who}: device int32 [sequences + 1]")
+    return t.data_ptr(), t.shape[0] - 1
+
+
+def _int32(x, who: str) -> int:
+    if not 0 <= x <= 0x7fffffff:
+        raise ValueError(f"{who}: in [0, 2^31)")
+    return int(x)
+
+
+def _attention(code: int, hq: int, hk: int, d: int, causal, window, sinks, fill, scale) -> bytes:
+    if hk < 1 or hq % hk or hq < 1:
+        raise ValueError("as many query heads as keys' or a multiple")
+    return _ATTENTION.pack(code, hq, hk, d, bool(causal), _int32(window, "window"), _int32(sinks, "sinks"), fill,
+                           d ** -0.5 if scale is None else scale)
+
+
+def _output(q, out):
+    if out is None:
+        return torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if not (out.dtype == q.dtype and out.device == q.device and out.shape == q.shape and (out.stride(2) == 1 or out.shape[2] == 1)):
+        raise ValueError("out: rows of q's shape, type and device, the values of a head one after another")
+    return out
+
+
+def _rows(t) -> bytes:
+    return _ROWS.pack(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _workspace(L, a: bytes, cached: int, n: int, rows: int, ragged: bool, max_len: int, device):
+    """(tensor or None, its address) of an attention call."""
+    nbytes = L.incvit_attention_workspace_bytes(a, cached, n, rows, ragged, max_len)
+    if nbytes == 0:
+        return None, None
+    t = _buffer(nbytes, device)
+    return t, t.data_ptr()
+
+
+class KVCache:
+    """Keys and values of `heads` heads in 8 bits, in `blocks` blocks of `block` (16,
+    32, 64 or 128) tokens with a scale for each block and head; zeros at first.  The
+    caller hands blocks out to sequences: slot = block number * block + place."""
+
+    def __init__(self, blocks: int, heads: int, head_dim: int, block: int = 16, device=None):
+        for x, who in ((blocks, "blocks"), (heads, "heads"), (head_dim, "head_dim"), (block, "block")):
+            _int32(x, who)
+        self.blocks, self.heads, self.head_dim, self.block = blocks, heads, head_dim, block
+        self.config = _KV.pack(blocks, block, heads, head_dim)
+        n = _c.lib().incvit_kv_bytes(self.config)
+        if n == 0:
+            raise _c.IncvitError(_c.INCVIT_ERR_UNSUPPORTED, f"a cache of {blocks} blocks of {block} tokens, {heads} heads of {head_dim}")
+        self.buf = torch.zeros(n, dtype=torch.uint8, device="cuda" if device is None else device)
+        if not self.buf.is_cuda:
+            raise ValueError("device: a GPU")
+        self.device = self.buf.device
+
+    def _sides(self, k, v):
+        code = _head_rows(k, "k")
+        if v.dtype != k.dtype or v.shape != k.shape or v.device != k.device or _head_rows(v, "v") != code:
+            raise ValueError("k and v: of one shape and type on one device")
+        if k.shape[1:] != (self.heads, self.head_dim) or k.device != self.device:
+            raise ValueError("k, v: [rows][heads][head_dim] on the cache's device")
+        return code
+
+    def write(self, k, v, slots, begin: bool = False):
+        """Quantise new keys and values [rows][heads][d] (fp32 or bf16, any 16-byte
+        aligned row and head strides) into `slots` (device int32 [rows], negative:
+        nowhere; the rows of one block one after another).  A block keeps what it
+        holds, rounded anew if its scale grows; with `begin` one whose first slot is
+        written holds nothing else afterwards (a sequence that goes on into a block
+        used before)."""
+        code = self._sides(k, v)
+        rows = k.shape[0]
+        at = _indexes(slots, rows, self.device, "slots")
+        _call(_c.lib().incvit_kv_write, self.device, self.config, code, rows, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
+              v.stride(0), v.stride(1), at, bool(begin), self.buf.data_ptr())
+
+    def read(self, slots, dtype=_BF16, k_out=None, v_out=None):
+        """(keys, values) [rows][heads][d] of `slots`, in `dtype` or in given tensors.  A
+        row whose slot is outside the cache (negative) stays what it was in a given
+        tensor and is zeros in a new one."""
+        if (k_out is None) != (v_out is None):
+            raise ValueError("k_out and v_out: both or neither")
+        if k_out is None:
+            if dtype not in (_BF16, _F32):
+                raise ValueError("dtype: fp32 or bf16")
+            k_out, v_out = torch.zeros(2, slots.shape[0], self.heads, self.head_dim, dtype=dtype, device=self.device).unbind(0)
+        code = self._sides(k_out, v_out)
+        rows = k_out.shape[0]
+        at = _indexes(slots, rows, self.device, "slots")
+        _call(_c.lib().incvit_kv_read, self.device, self.config, self.buf.data_ptr(), code, rows, at, k_out.data_ptr(),
+              k_out.stride(0), k_out.stride(1), v_out.data_ptr(), v_out.stride(0), v_out.stride(1))
+        return k_out, v_out
+
+    def attend(self, q, table, lens, q_start=None, causal: bool = True, window: int = 0, sinks: int = 0, scale=None, max_len: int = 0,
+               out=None):
+        """Attention of q [rows][q heads][d] over the cached tokens of `table` (device
+        int32 [sequences][blocks of a sequence]), `lens` (device int32 [sequences]) of
+        them.  A sequence's queries are its last tokens: rows q_start[i] to q_start[i +
+        1] (device int32 [sequences + 1]) or rows / sequences for each.  Query at
+        position p sees key j where j <= p (causal) and |p - j| < window (window 0:
+        all) or j < sinks; a row that sees nothing gives zeros.  scale: 1 / sqrt(d)
+        unless given.  max_len: about the longest sequence, if the table is much wider.
+        Rows behind the last sequence stay what they were in a given out, and are zeros
+        in a new one."""
+        code = _head_rows(q, "q")
+        dev = self.device
+        rows, hq, d = q.shape
+        if q.device != dev or d != self.head_dim:
+            raise ValueError("q: [rows][heads][head_dim] on the cache's device")
+        if not (table.dtype == torch.int32 and table.device == dev and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] < 2)):
+            raise ValueError("table: device int32 [sequences][blocks], a sequence's blocks one after another")
+        n, width = table.shape
+        at = _indexes(lens, n, dev, "lens")
+        starts = None
+        if q_start is not None:
+            starts, m = _starts(q_start, dev, "q_start")
+            if m != n:
+                raise ValueError("q_start: device int32 [sequences + 1]")
+        a = _attention(code, hq, self.heads, d, causal, window, sinks, out is None, scale)
+        new, out = out is None, _output(q, out)
+        if rows == 0 or n == 0:
+            return out.zero_() if new else out
+        most = max_len or width * self.block
+        L = _c.lib()
+        ws, wp = _workspace(L, a, 1, n, rows, starts is not None, most, dev)
+        _call(L.incvit_kv_attend, dev, a, self.config, self.buf.data_ptr(), n, rows, starts, table.data_ptr(), table.stride(0), width, at,
+              most, _rows(q), _rows(out), wp)
+        return out
+
+
+# ---------------------------------------------------------------- attention --
+
+
+def attend(q, k, v, q_start=None, k_start=None, causal: bool = True, window: int = 0, sinks: int = 0, scale=None, max_len: int = 0,
+           out=None):
+    """Attention of q [rows][q heads][d] over keys and values [key rows][heads][d]
+    (fp32 or bf16, any 16-byte aligned row and head strides), sequences one after
+    another: q_start and k_start (device int32 [sequences + 1]), or one sequence.
+    Masks, positions and what is returned as KVCache.attend's."""
+    code = _head_rows(q, "q")
+    dev = q.device
+    rows, hq, d = q.shape
+    for t, who in ((k, "k"), (v, "v")):
+        if _head_rows(t, who) != code or t.device != dev or t.shape != k.shape or t.shape[2] != d:
+            raise ValueError("k and v: of one shape, of q's type, head_dim and device")
+    if (q_start is None) != (k_start is None):
+        raise ValueError("q_start and k_start: both or neither")
+    qs = ks = None
+    n = 1
+    if q_start is not None:
+        (qs, n), (ks, m) = _starts(q_start, dev, "q_start"), _starts(k_start, dev, "k_start")
+        if m != n:
+            raise ValueError("q_start and k_start: device int32 [sequences + 1]")
+    a = _attention(code, hq, k.shape[1], d, causal, window, sinks, out is None, scale)
+    new, out = out is None, _output(q, out)
+    if rows == 0 or n == 0:
+        return out.zero_() if new else out
+    keys = k.shape[0]
+    most = max_len or -(-keys // n)
+    L = _c.lib()
+    ws, wp = _workspace(L, a, 0, n, rows, qs is not None, most, dev)
+    _call(L.incvit_attend, dev, a, n, rows, qs, keys, ks, most, _rows(q), _rows(k), _rows(v), _rows(out), wp)
+    return out
