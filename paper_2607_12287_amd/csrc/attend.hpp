@@ -62,7 +62,7 @@ hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t s);
 
 // -------------------------------------------------------------- attention --
 
-constexpr int kKeyTile = 32;   // keys that a wave takes at once
+constexpr int kKeyTile = 32;   // keys that a wave takes at once where the waves of a workgroup share its keys
 constexpr int kKeyWaves = 4;   // waves of a workgroup
 
 struct AttendArgs {
@@ -82,6 +82,7 @@ struct AttendArgs {
   int fill;            // with q_start: rows behind the last sequence as those of one without keys
   float scale_log2;    // scale * log2(e)
   int most_rows;       // rows * group of a sequence at most
+  int row_log, key_log;  // rows of a row tile and keys of a key tile: powers of two
   int tiles;           // row tiles of the call
   int tiles_each;      // of each sequence (q_start null)
   int splits, chunk;   // most workgroups that share a row tile's keys; key tiles of one at least
@@ -90,8 +91,14 @@ struct AttendArgs {
 // 16-row tiles of a workgroup over the cache, at most: as many as the registers hold.
 constexpr int most_row_tiles(bool bf16, int ds) { return bf16 ? (ds <= 96 ? 4 : ds <= 192 ? 2 : 1) : ds <= 128 ? 2 : 1; }
 
+// 16-row tiles of a wave of its own rows, at most; keys of a tile there
+constexpr int most_wave_tiles(bool bf16, int ds) { return bf16 || ds <= 128 ? 2 : 1; }
+constexpr int rows_key_log(bool bf16, int ds) { return ds * (bf16 ? 2 : 4) <= 512 ? 6 : 5; }
+
 struct AttendPlan {
-  int nt;              // 16-row tiles of a workgroup
+  int by_rows;         // the waves have rows of their own (else keys)
+  int nt;              // 16-row tiles of a workgroup, or of a wave of its own rows
+  int row_log, key_log;
   long tiles;          // row tiles
   int tiles_each, splits, chunk;
   size_t bytes;        // workspace
@@ -100,7 +107,8 @@ AttendPlan attend_plan(const incvit_attention& a, bool cached, long n, long rows
 
 hipError_t launch_kv_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
-hipError_t launch_attend_join(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
+hipError_t launch_attend_rows(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
+hipError_t launch_attend_join(const AttendArgs& a, int dtype, hipStream_t s);
 
 }  // namespace incvit
 
@@ -116,14 +124,14 @@ struct RowTile {
 };
 
 // The tile number f of the launch.  Ragged: sequence i's tiles count from
-// floor(q_start[i] * group / TR) + i on, which leaves each enough numbers, so a
+// floor(q_start[i] * group / rows of a tile) + i on, which leaves each enough numbers, so a
 // wave finds the sequence by counting the starts up to f, 64 at a time.  Whatever
 // the starts hold, the rows are within the call's.
-template <int TR>
 __device__ __forceinline__ bool row_tile(const AttendArgs& a, int f, RowTile& w) {
+  const int log = a.row_log;
   if (!a.q_start) {
     w.seq = f / a.tiles_each;
-    w.first = (f - w.seq * a.tiles_each) * TR;
+    w.first = (f - w.seq * a.tiles_each) << log;
     w.q_len = a.q_len;
     w.q0 = (long)w.seq * a.q_len;
   } else {
@@ -133,14 +141,14 @@ __device__ __forceinline__ bool row_tile(const AttendArgs& a, int f, RowTile& w)
     for (int i = 0; i < n; i += 64) {
       const int j = min(i + lane, n - 1);
       const long at = min(max((long)gbl(a.q_start)[j], 0L), a.rows);
-      const bool up = i + lane < n && (at * a.group) / TR + j <= f;
+      const bool up = i + lane < n && ((at * a.group) >> log) + j <= f;
       count += __popcll(__ballot(up));
     }
     if (count == 0) return false;
     w.seq = __builtin_amdgcn_readfirstlane(count - 1);
     const long q0 = min(max((long)gbl(a.q_start)[w.seq], 0L), a.rows);
     const long q1 = w.seq < a.n ? min(max((long)gbl(a.q_start)[w.seq + 1], q0), a.rows) : a.rows;
-    w.first = (int)(f - (q0 * a.group) / TR - w.seq) * TR;
+    w.first = (int)(f - ((q0 * a.group) >> log) - w.seq) * (1 << log);
     w.q_len = (int)(q1 - q0);
     w.q0 = q0;
   }
@@ -171,9 +179,10 @@ struct KeyTiles {
   int p0, p1;
   __device__ __forceinline__ int at(int i) const { return i < n0 ? i : i - n0 + t1; }
 };
-__device__ __forceinline__ KeyTiles key_tiles(const AttendArgs& a, const RowTile& w, int tr) {
+__device__ __forceinline__ KeyTiles key_tiles(const AttendArgs& a, const RowTile& w) {
+  const int log = a.key_log, up = (1 << log) - 1;
   KeyTiles k;
-  const int last = min(w.first + tr, w.q_len * a.group) - 1;
+  const int last = min(w.first + (1 << a.row_log), w.q_len * a.group) - 1;
   k.p0 = w.len - w.q_len + w.first / a.group;
   k.p1 = w.len - w.q_len + last / a.group;
   const int top = max(0, a.causal ? min(w.len, k.p1 + 1) : w.len);
@@ -183,10 +192,10 @@ __device__ __forceinline__ KeyTiles key_tiles(const AttendArgs& a, const RowTile
     lo = max(0, k.p0 - a.window + 1);
     if (!a.causal) hi = max(0, min(top, k.p1 + a.window));  // both at most 2^30
   }
-  k.t1 = lo / kKeyTile;
-  int t2 = lo < hi ? (hi + kKeyTile - 1) / kKeyTile : k.t1;
+  k.t1 = lo >> log;
+  int t2 = lo < hi ? (hi + up) >> log : k.t1;
   if (a.window && a.sinks) {
-    const int s = (min(a.sinks, top) + kKeyTile - 1) / kKeyTile;
+    const int s = (min(a.sinks, top) + up) >> log;
     if (s >= k.t1) {
       k.t1 = 0;
       t2 = max(t2, s);
@@ -200,6 +209,31 @@ __device__ __forceinline__ KeyTiles key_tiles(const AttendArgs& a, const RowTile
 
 // Workgroups that share nt key tiles, and the share of workgroup s.
 __device__ __forceinline__ int key_shares(const AttendArgs& a, int nt) { return max(1, min(a.splits, (nt + a.chunk - 1) / a.chunk)); }
+
+// The keys that a row at position `pos` sees: `n` from lo on, and those below
+// `sinks`.  Two comparisons without a branch (a chain of && over a lane's keys
+// came out as branches, slower, and in one kernel with scores that the mask had
+// taken put back).
+struct Sight {
+  int lo, sinks;
+  uint32_t n;
+  __device__ __forceinline__ bool sees(int key) const { return ((uint32_t)(key - lo) < n) | (key < sinks); }
+};
+__device__ __forceinline__ Sight sight(const AttendArgs& a, int len, int pos) {
+  const int top = a.causal ? min(len, pos + 1) : len;
+  const int hi = a.window && !a.causal ? min(top, pos + a.window) : top;
+  Sight s;
+  s.lo = a.window ? max(0, pos - a.window + 1) : 0;
+  s.sinks = a.window ? min(a.sinks, top) : 0;
+  s.n = (uint32_t)max(0, hi - s.lo);
+  return s;
+}
+
+// Whether rows at positions p0 to p1 see all of the keys j0 to j1.
+__device__ __forceinline__ bool all_seen(const AttendArgs& a, int len, int p0, int p1, int j0, int j1) {
+  const bool window = !a.window | ((p1 - j0 < a.window) & ((a.causal != 0) | (j1 - p0 < a.window))) | (j1 < a.sinks);
+  return (j1 < len) & (!a.causal | (j1 <= p0)) & window;
+}
 
 // A row's partial result: m, the largest score in units of log2; l, the sum of
 // 2^(x - m); O.  m = -inf: no key was seen.  kNoMax: keys were seen, none above -inf.

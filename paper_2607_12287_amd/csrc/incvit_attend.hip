@@ -102,6 +102,8 @@ AttendArgs attend_args(const incvit_attention& a, const AttendPlan& p, int32_t n
   r.fill = q_start ? a.fill : 0;
   r.scale_log2 = a.scale * 1.44269504088896340736f;
   r.most_rows = (int)((q_start ? rows : rows / n) * r.group);
+  r.row_log = p.row_log;
+  r.key_log = p.key_log;
   r.tiles = (int)p.tiles;
   r.tiles_each = p.tiles_each;
   r.splits = p.splits;
@@ -115,20 +117,32 @@ AttendArgs attend_args(const incvit_attention& a, const AttendPlan& p, int32_t n
 // leave the chip idle, the keys of each are shared by several workgroups.
 AttendPlan incvit::attend_plan(const incvit_attention& a, bool cached, long n, long rows, bool ragged, long max_len) {
   AttendPlan p = {};
+  const bool bf16 = a.dtype == INCVIT_BF16;
   const long group = a.q_heads / a.kv_heads, each = (rows + n - 1) / n * group;
   const int ds = kv_dims(a.head_dim);
-  const int most = cached ? most_row_tiles(a.dtype == INCVIT_BF16, ds) : 1;
-  p.nt = std::min(most, each <= 16 ? 1 : each <= 32 ? 2 : 4);
-  const long tr = 16 * p.nt;
+  p.key_log = 5;
+  if (cached) {
+    p.nt = std::min(most_row_tiles(bf16, ds), each <= 16 ? 1 : each <= 32 ? 2 : 4);
+    p.row_log = p.nt == 1 ? 4 : p.nt == 2 ? 5 : 6;
+  } else if (each > 32) {
+    p.by_rows = 1;
+    p.nt = std::min(most_wave_tiles(bf16, ds), each <= 64 || rows * group / 128 * a.kv_heads < 256 ? 1 : 2);
+    p.row_log = 5 + p.nt;
+    p.key_log = rows_key_log(bf16, ds);
+  } else {
+    p.nt = 1;
+    p.row_log = 4;
+  }
+  const long tr = 1L << p.row_log, kt = 1L << p.key_log;
   p.tiles_each = (int)((rows / n * group + tr - 1) / tr);
   p.tiles = ragged ? rows * group / tr + n + a.fill : n * p.tiles_each;
   // key tiles of a row tile at most
   long span = max_len;
-  if (a.window) span = std::min(span, (long)a.window * (a.causal ? 1 : 2) + tr / group + 1 + a.sinks + 3 * kKeyTile);
-  const long tiles = std::max(1L, (span + kKeyTile - 1) / kKeyTile);
+  if (a.window) span = std::min(span, (long)a.window * (a.causal ? 1 : 2) + tr / group + 1 + a.sinks + 3 * kt);
+  const long tiles = std::max(1L, (span + kt - 1) / kt);
   const long wgs = std::max(1L, p.tiles * a.kv_heads);
-  const long want = std::max(1L, 1024 / wgs);
-  p.chunk = (int)std::max(4L * kKeyWaves, (tiles + want - 1) / want);
+  const long want = std::max(1L, (p.by_rows ? 512 : 1024) / wgs);
+  p.chunk = (int)std::max(p.by_rows ? 8L : 4L * kKeyWaves, (tiles + want - 1) / want);
   p.splits = (int)std::min(256L, (tiles + p.chunk - 1) / p.chunk);
   if (p.splits > 1) p.bytes = (size_t)wgs * p.splits * tr * (ds + 2) * 4;
   return p;
@@ -230,7 +244,7 @@ incvit_status incvit_kv_attend(const incvit_attention* a, const incvit_kv* c, co
   r.lb = lay.lb;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if ((st = launched(launch_kv_attend(r, p, a->dtype, s), "kv_attend")) != INCVIT_OK) return st;
-  return launched(launch_attend_join(r, p, a->dtype, s), "kv_attend");
+  return launched(launch_attend_join(r, a->dtype, s), "kv_attend");
 }
 
 incvit_status incvit_attend(const incvit_attention* a, int32_t n, int64_t rows, const int32_t* q_start, int64_t key_rows,
@@ -261,8 +275,8 @@ incvit_status incvit_attend(const incvit_attention* a, int32_t n, int64_t rows, 
   r.key_rows = (long)key_rows;
   r.k_len = k_start ? 0 : (int)(key_rows / n);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if ((st = launched(launch_attend(r, p, a->dtype, s), "attend")) != INCVIT_OK) return st;
-  return launched(launch_attend_join(r, p, a->dtype, s), "attend");
+  if ((st = launched(p.by_rows ? launch_attend_rows(r, p, a->dtype, s) : launch_attend(r, p, a->dtype, s), "attend")) != INCVIT_OK) return st;
+  return launched(launch_attend_join(r, a->dtype, s), "attend");
 }
 
 }  // extern "C"

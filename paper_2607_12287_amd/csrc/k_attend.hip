@@ -4,88 +4,11 @@
 // other operands: a wave has 32 keys at once, S^T = K Q^T with the keys' rows as
 // loaded, O^T = V^T P^T with values that go through LDS rows, from which bf16 is
 // read transposed.  fp32 multiplies in fp32.
-//
-// A value that no row of a tile may see must not reach a product, where 0 * NaN is
-// NaN: rows past the sequence are zeros in LDS; and in a tile that is partly masked
-// infinities and NaN are, while add_special() adds them for the rows that see them.
-#include "attend.hpp"
+#include "attend_plain.hpp"
 
 namespace incvit {
 
 namespace {
-
-typedef short i16x4_t __attribute__((ext_vector_type(4)));
-
-// Bytes of a row of values in LDS: 16 more than its dims, so that 16 rows' pieces
-// of the same dims spread over the banks.
-template <class T, int DS>
-constexpr int row_bytes() {
-  return DS * (int)sizeof(T) + 16;
-}
-
-template <class T>
-__device__ __forceinline__ bool special(const V8<T>& x) {
-  bool any = false;
-  if constexpr (sizeof(T) == 2) {
-    const uint32_t w[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) any |= (w[i] & 0x7f800000u) == 0x7f800000u || (w[i] & 0x7f80u) == 0x7f80u;
-  } else {
-    float y[8];
-    floats_of(x, y);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) any |= (__float_as_uint(y[i]) & 0x7f800000u) == 0x7f800000u;
-  }
-  return any;
-}
-// infinities and NaN as zeros
-__device__ __forceinline__ void drop_special(V8<uint16_t>& x) {
-  uint32_t w[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0xffffu;
-    if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
-  }
-  x.v = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void drop_special(V8<float>& x) {
-  float y[8];
-  floats_of(x, y);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = (__float_as_uint(y[i]) & 0x7f800000u) == 0x7f800000u ? 0.0f : y[i];
-  x.a = make_float4(y[0], y[1], y[2], y[3]);
-  x.b = make_float4(y[4], y[5], y[6], y[7]);
-}
-
-// The transposed operand of 32 keys: lane (g, n) has dim `dim0` + n of keys 4 g ..
-// + 3 and 16 + 4 g .. + 3, which is the order of its P.
-template <class T, int RB>
-__device__ __forceinline__ V8<T> value_op(const char* v, int dim0, int lane) {
-  const int g = lane >> 4, n = lane & 15;
-  V8<T> x;
-  if constexpr (sizeof(T) == 2) {
-    // 16 lanes give the places of 4 rows of 16 dims, 4 dims each, and get a dim of the 4 rows
-    typedef __attribute__((address_space(3))) i16x4_t* Lds;
-    char* at = const_cast<char*>(v) + (4 * g + (n >> 2)) * RB + (dim0 + 4 * (n & 3)) * 2;
-    const u32x2_t a = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at));
-    const u32x2_t b = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 16 * RB)));
-    x.v = make_uint4(a[0], a[1], b[0], b[1]);
-  } else {
-    const char* at = v + 4 * g * RB + (dim0 + n) * 4;
-    float y[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = *reinterpret_cast<const float*>(at + (16 * (j >> 2) + (j & 3)) * RB);
-    x.a = make_float4(y[0], y[1], y[2], y[3]);
-    x.b = make_float4(y[4], y[5], y[6], y[7]);
-  }
-  return x;
-}
-
-__device__ __forceinline__ void p_op(V8<uint16_t>& out, const float* p) { split8<1>(p, &out.v); }
-__device__ __forceinline__ void p_op(V8<float>& out, const float* p) {
-  out.a = make_float4(p[0], p[1], p[2], p[3]);
-  out.b = make_float4(p[4], p[5], p[6], p[7]);
-}
 
 template <class T, int DS, int NT>
 __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
@@ -98,18 +21,18 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
   const int h = blockIdx.x % a.hk, rest = blockIdx.x / a.hk;
   const int share = rest / a.tiles, f = a.tiles - 1 - (rest - share * a.tiles);
   RowTile w;
-  if (!row_tile<TR>(a, f, w)) return;
+  if (!row_tile(a, f, w)) return;
   w.len = plain_len(a, w);
-  const KeyTiles kt = key_tiles(a, w, TR);
+  const KeyTiles kt = key_tiles(a, w);
   const int shares = key_shares(a, kt.nt);
   if (share >= shares) return;
   const int i1 = (int)((long)(share + 1) * kt.nt / shares);
-  int i = (int)((long)share * kt.nt / shares) + wave;
+  const int first = (int)((long)share * kt.nt / shares) + wave;
+  int i = first;
 
   const T* keys = static_cast<const T*>(a.k.p) + w.k0 * a.k.row + (long)h * a.k.head;
   const T* values = static_cast<const T*>(a.v.p) + w.k0 * a.v.row + (long)h * a.v.head;
   char* vbuf = lds + wave * kKeyTile * RB;
-  float* codes = reinterpret_cast<float*>(lds + kKeyWaves * kKeyTile * RB) + wave * kKeyTile * 16;  // [key][row]
 
   V8<T> kraw[2][NC], vraw[NV];
   auto load_keys = [&](int tile) {
@@ -133,21 +56,20 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
       if (!in) vraw[k].zero();
     }
   };
-  auto put_values = [&](bool clean) {
+  auto put_values = [&]() {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int e = k * 64 + lane, r = e / PER, d = (e - r * PER) * 8;
-      if (clean) drop_special(vraw[k]);
       if (r < kKeyTile) *reinterpret_cast<V8<T>*>(vbuf + r * RB + d * sizeof(T)) = vraw[k];
     }
   };
 
   V8<T> q[NT][NC];
-  int pos[NT];
+  Sight eye[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int row = min(w.first + 16 * t + n, w.q_len * a.group - 1), tok = row / a.group;
-    pos[t] = w.len - w.q_len + tok;
+    eye[t] = sight(a, w.len, w.len - w.q_len + tok);
     const T* src = static_cast<const T*>(a.q.p) + (w.q0 + tok) * a.q.row + (long)(h * a.group + row - tok * a.group) * a.q.head;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -169,20 +91,22 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
     for (int p = 0; p < NP; ++p) o[t][p] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
+  bool odd = false;
   auto work = [&](int tile, int next) {
     const int j0 = tile * kKeyTile, j1 = j0 + kKeyTile - 1;
-    const bool whole = j1 < w.len && (!a.causal || j1 <= kt.p0) &&
-                       (!a.window || (kt.p1 - j0 < a.window && (a.causal || j1 - kt.p0 < a.window)) || j1 < a.sinks);
-    bool odd = false;
+    const bool whole = all_seen(a, w.len, kt.p0, kt.p1, j0, j1);
     auto stage = [&]() {
       if (!whole) {
         bool any = false;
-  #pragma unroll
+#pragma unroll
         for (int k = 0; k < NV; ++k) any |= special(vraw[k]);
-        odd = __any(any);
+        if (__any(any)) {
+          odd = true;
+#pragma unroll
+          for (int k = 0; k < NV; ++k) drop_special(vraw[k]);
+        }
       }
-      if (odd) put_values(true);
-      else put_values(false);
+      put_values();
     };
     if constexpr (AHEAD) {
       stage();
@@ -212,13 +136,9 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
       if (!whole) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int key = j0 + 16 * (j >> 2) + 4 * g + (j & 3), gap = pos[t] - key;
-          const bool v = key < w.len && (!a.causal || gap >= 0) &&
-                         (!a.window || (gap < a.window && -gap < a.window) || key < a.sinks);
-          if (!v) {
-            y[j] = -INFINITY;
-            see &= ~(1u << j);
-          }
+          const bool v = eye[t].sees(j0 + 16 * (j >> 2) + 4 * g + (j & 3));
+          see &= v ? ~0u : ~(1u << j);
+          y[j] = v ? y[j] : -INFINITY;
         }
       }
       seen[t] |= see != 0;
@@ -230,28 +150,6 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
       if (!whole) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = see >> j & 1 ? p[j] : 0.0f;  // also where the row's scores are NaN
-      }
-      if (odd) {
-        // the tile's infinities and NaN, for the rows that see them
-#pragma unroll
-        for (int j = 0; j < 8; ++j) codes[(16 * (j >> 2) + 4 * g + (j & 3)) * 16 + n] = see >> j & 1 ? p[j] : -1.0f;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 1
-        for (int key = j0; key <= min(j1, w.len - 1); ++key) {
-          const float pk = codes[(key - j0) * 16 + n];
-          const T* src = values + (long)key * a.v.row;
-#pragma unroll
-          for (int k = 0; k < NP; ++k) {
-            __builtin_amdgcn_sched_barrier(0);  // a rare path: no registers for all loads at once
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int d = 16 * k + 4 * g + r;
-              const float v = d < a.d ? Elem<T>::f(gbl(src)[d]) : 0.0f;
-              if (!__builtin_isfinite(v) && pk >= 0.0f) o[t][k][r] += pk * v;
-            }
-          }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
       p_op(pop[t], p);
     }
@@ -270,6 +168,14 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
     load_keys(kt.at(i));
     if constexpr (AHEAD) load_values(kt.at(i));
     for (; i < i1; i += kKeyWaves) work(kt.at(i), kt.at(min(i + kKeyWaves, i1 - 1)));
+  }
+  if (odd) {
+#pragma unroll 1
+    for (int e = first; e < i1; e += kKeyWaves) {
+      const int j0 = kt.at(e) * kKeyTile, j1 = j0 + kKeyTile - 1;
+      if (!all_seen(a, w.len, kt.p0, kt.p1, j0, j1))
+        add_special<T, NP, NT>(o, eye, reinterpret_cast<const char*>(values), a.v.row * (long)sizeof(T), a.d, j0, min(j1, w.len - 1), lane);
+    }
   }
 
   __syncthreads();  // the exchange takes the values' place
@@ -294,7 +200,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
 
 template <class T, int DS, int NT>
 hipError_t launch_one(const AttendArgs& a, hipStream_t s) {
-  constexpr int bytes = std::max(exchange_bytes<DS, NT>(), kKeyWaves * kKeyTile * (row_bytes<T, DS>() + 64));
+  constexpr int bytes = std::max(exchange_bytes<DS, NT>(), kKeyWaves * kKeyTile * row_bytes<T, DS>());
   static_assert(bytes <= 160 * 1024, "LDS");
   const hipError_t e = with_lds<attend_kernel<T, DS, NT>>(bytes);
   if (e != hipSuccess) return e;

@@ -9,14 +9,14 @@ namespace incvit {
 namespace {
 
 // cached: whether key tiles are those of the cache (lens) or of given keys
-template <class T, int DS, int NT, bool CACHED>
+template <class T, int DS, bool CACHED>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-  constexpr int TR = 16 * NT;
+  const int TR = 1 << a.row_log;
   const int h = blockIdx.x % a.hk, f = blockIdx.x / a.hk;
   RowTile w;
-  if (!row_tile<TR>(a, f, w)) return;
+  if (!row_tile(a, f, w)) return;
   w.len = CACHED ? cached_len(a, w.seq) : plain_len(a, w);
-  const int shares = key_shares(a, key_tiles(a, w, TR).nt);
+  const int shares = key_shares(a, key_tiles(a, w).nt);
   if (shares < 2) return;
   const int rows = min(TR, w.q_len * a.group - w.first);
   const float* part = a.parts + (size_t)((long)f * a.hk + h) * a.splits * TR * (DS + 2);
@@ -44,38 +44,31 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   store_out4<T>(static_cast<T*>(const_cast<void*>(a.out.p)) + (w.q0 + tok) * a.out.row + (long)head * a.out.head + d, y);
 }
 
-template <class T, int DS, int NT>
-hipError_t launch_one(const AttendArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((long)a.tiles * a.hk), (std::min(16 * NT, a.most_rows) * (DS / 4) + 255) / 256);
-  return a.lens ? launch_k(attend_join_kernel<T, DS, NT, true>, grid, dim3(256), 0, s, a)
-                : launch_k(attend_join_kernel<T, DS, NT, false>, grid, dim3(256), 0, s, a);
-}
-
 template <class T, int DS>
-hipError_t launch_ds(const AttendArgs& a, int nt, hipStream_t s) {
-  if (nt == 1) return launch_one<T, DS, 1>(a, s);
-  if (nt == 2) return launch_one<T, DS, 2>(a, s);
-  return launch_one<T, DS, 4>(a, s);
+hipError_t launch_ds(const AttendArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((long)a.tiles * a.hk), (std::min(1 << a.row_log, a.most_rows) * (DS / 4) + 255) / 256);
+  return a.lens ? launch_k(attend_join_kernel<T, DS, true>, grid, dim3(256), 0, s, a)
+                : launch_k(attend_join_kernel<T, DS, false>, grid, dim3(256), 0, s, a);
 }
 
 template <class T>
-hipError_t launch_t(const AttendArgs& a, int nt, hipStream_t s) {
+hipError_t launch_t(const AttendArgs& a, hipStream_t s) {
   switch (kv_dims(a.d)) {
-    case 32: return launch_ds<T, 32>(a, nt, s);
-    case 64: return launch_ds<T, 64>(a, nt, s);
-    case 80: return launch_ds<T, 80>(a, nt, s);
-    case 96: return launch_ds<T, 96>(a, nt, s);
-    case 128: return launch_ds<T, 128>(a, nt, s);
-    case 192: return launch_ds<T, 192>(a, nt, s);
-    default: return launch_ds<T, 256>(a, nt, s);
+    case 32: return launch_ds<T, 32>(a, s);
+    case 64: return launch_ds<T, 64>(a, s);
+    case 80: return launch_ds<T, 80>(a, s);
+    case 96: return launch_ds<T, 96>(a, s);
+    case 128: return launch_ds<T, 128>(a, s);
+    case 192: return launch_ds<T, 192>(a, s);
+    default: return launch_ds<T, 256>(a, s);
   }
 }
 
 }  // namespace
 
-hipError_t launch_attend_join(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s) {
+hipError_t launch_attend_join(const AttendArgs& a, int dtype, hipStream_t s) {
   if (a.splits < 2) return hipSuccess;
-  return dtype == INCVIT_BF16 ? launch_t<uint16_t>(a, p.nt, s) : launch_t<float>(a, p.nt, s);
+  return dtype == INCVIT_BF16 ? launch_t<uint16_t>(a, s) : launch_t<float>(a, s);
 }
 
 }  // namespace incvit

@@ -61,9 +61,9 @@ __global__ __launch_bounds__(64 * kKeyWaves) void kv_attend_kernel(AttendArgs a)
   const int h = blockIdx.x % a.hk, rest = blockIdx.x / a.hk;
   const int share = rest / a.tiles, f = a.tiles - 1 - (rest - share * a.tiles);
   RowTile w;
-  if (!row_tile<TR>(a, f, w)) return;
+  if (!row_tile(a, f, w)) return;
   w.len = cached_len(a, w.seq);
-  const KeyTiles kt = key_tiles(a, w, TR);
+  const KeyTiles kt = key_tiles(a, w);
   const int shares = key_shares(a, kt.nt);
   if (share >= shares) return;
   const int i1 = (int)((long)(share + 1) * kt.nt / shares);
@@ -106,11 +106,11 @@ __global__ __launch_bounds__(64 * kKeyWaves) void kv_attend_kernel(AttendArgs a)
 
   // queries: lane (g, n) has dims 64 c + 16 g .. + 15 of row n
   uint4 q[NT][2 * NC][PARTS];
-  int pos[NT];
+  Sight eye[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int row = min(w.first + 16 * t + n, w.q_len * a.group - 1), tok = row / a.group;
-    pos[t] = w.len - w.q_len + tok;
+    eye[t] = sight(a, w.len, w.len - w.q_len + tok);
     const T* src = static_cast<const T*>(a.q.p) + (w.q0 + tok) * a.q.row + (long)(h * a.group + row - tok * a.group) * a.q.head;
 #pragma unroll
     for (int c = 0; c < 2 * NC; ++c) {
@@ -157,8 +157,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void kv_attend_kernel(AttendArgs a)
           for (int k = 0; k < PARTS; ++k) s[t][u] = mma16(kop, q[t][c][k], s[t][u]);
       }
     const int j0 = tile * kKeyTile, j1 = j0 + kKeyTile - 1;
-    const bool whole = x.ok == 3 && j1 < w.len && (!a.causal || j1 <= kt.p0) &&
-                       (!a.window || (kt.p1 - j0 < a.window && (a.causal || j1 - kt.p0 < a.window)) || j1 < a.sinks);
+    const bool whole = (x.ok == 3) & all_seen(a, w.len, kt.p0, kt.p1, j0, j1);
     const float c0 = x.ks[0] * a.scale_log2, c1 = x.ks[1] * a.scale_log2;
     uint4 pop[NT][PARTS];
 #pragma unroll
@@ -170,13 +169,9 @@ __global__ __launch_bounds__(64 * kKeyWaves) void kv_attend_kernel(AttendArgs a)
       if (!whole) {  // the same for the wave
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int key = j0 + 16 * (j >> 2) + 4 * g + (j & 3), gap = pos[t] - key;
-          const bool v = (x.ok >> (j >> 2) & 1) && key < w.len && (!a.causal || gap >= 0) &&
-                         (!a.window || (gap < a.window && -gap < a.window) || key < a.sinks);
-          if (!v) {
-            y[j] = -INFINITY;
-            see &= ~(1u << j);
-          }
+          const bool v = eye[t].sees(j0 + 16 * (j >> 2) + 4 * g + (j & 3)) & ((x.ok >> (j >> 2) & 1) != 0);
+          see &= v ? ~0u : ~(1u << j);
+          y[j] = v ? y[j] : -INFINITY;
         }
       }
       seen[t] |= see != 0;
