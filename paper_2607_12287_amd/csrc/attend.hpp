@@ -46,6 +46,7 @@ struct KvWriteArgs {
   size_t data;
   long rows;
   int blocks, block, heads, d, begin, dtype;
+  int each;  // rows of a wave
 };
 
 struct KvReadArgs {
@@ -55,6 +56,7 @@ struct KvReadArgs {
   size_t data;
   long rows;
   int blocks, block, heads, d, dtype;
+  uint32_t per_inv;  // 2^32 / (d / 8), rounded up
 };
 
 hipError_t launch_kv_write(const KvWriteArgs& a, hipStream_t s);
