@@ -66,6 +66,8 @@ hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t s);
 
 constexpr int kKeyTile = 32;   // keys that a wave takes at once where the waves of a workgroup share its keys
 constexpr int kKeyWaves = 4;   // waves of a workgroup
+constexpr int kMostShares = 256;  // of a row tile's keys
+constexpr int kEvenTiles = 64;    // sequences whose shares are made even
 
 struct AttendArgs {
   const int* q_start;  // null: q_len rows for each sequence
@@ -83,11 +85,15 @@ struct AttendArgs {
   int causal, window, sinks;
   int fill;            // with q_start: rows behind the last sequence as those of one without keys
   float scale_log2;    // scale * log2(e)
+  long shares;         // workgroups of a head
   int most_rows;       // rows * group of a sequence at most
   int row_log, key_log;  // rows of a row tile and keys of a key tile: powers of two
   int tiles;           // row tiles of the call
   int tiles_each;      // of each sequence (q_start null)
-  int splits, chunk;   // most workgroups that share a row tile's keys; key tiles of one at least
+  // workgroups that share a row tile's keys: at most `splits` for each, of at least
+  // `chunk` key tiles; or (even > 0) as many as give `even` to a head in all, each of
+  // about as many key tiles, at least `chunk`
+  int splits, chunk, even;
 };
 
 // 16-row tiles of a workgroup over the cache, at most: as many as the registers hold.
@@ -102,7 +108,8 @@ struct AttendPlan {
   int nt;              // 16-row tiles of a workgroup, or of a wave of its own rows
   int row_log, key_log;
   long tiles;          // row tiles
-  int tiles_each, splits, chunk;
+  int tiles_each, splits, chunk, even;
+  long shares;         // of a head at most
   size_t bytes;        // workspace
 };
 AttendPlan attend_plan(const incvit_attention& a, bool cached, long n, long rows, bool ragged, long max_len);
@@ -181,18 +188,17 @@ struct KeyTiles {
   int p0, p1;
   __device__ __forceinline__ int at(int i) const { return i < n0 ? i : i - n0 + t1; }
 };
-__device__ __forceinline__ KeyTiles key_tiles(const AttendArgs& a, const RowTile& w) {
+__device__ __forceinline__ KeyTiles key_tiles(const AttendArgs& a, int len, int p0, int p1) {
   const int log = a.key_log, up = (1 << log) - 1;
   KeyTiles k;
-  const int last = min(w.first + (1 << a.row_log), w.q_len * a.group) - 1;
-  k.p0 = w.len - w.q_len + w.first / a.group;
-  k.p1 = w.len - w.q_len + last / a.group;
-  const int top = max(0, a.causal ? min(w.len, k.p1 + 1) : w.len);
+  k.p0 = p0;
+  k.p1 = p1;
+  const int top = max(0, a.causal ? min(len, p1 + 1) : len);
   int lo = 0, hi = top;
   k.n0 = 0;
   if (a.window) {
-    lo = max(0, k.p0 - a.window + 1);
-    if (!a.causal) hi = max(0, min(top, k.p1 + a.window));  // both at most 2^30
+    lo = max(0, p0 - a.window + 1);
+    if (!a.causal) hi = max(0, min(top, p1 + a.window));  // both at most 2^30
   }
   k.t1 = lo >> log;
   int t2 = lo < hi ? (hi + up) >> log : k.t1;
@@ -208,9 +214,84 @@ __device__ __forceinline__ KeyTiles key_tiles(const AttendArgs& a, const RowTile
   k.nt = k.n0 + t2 - k.t1;
   return k;
 }
+__device__ __forceinline__ KeyTiles key_tiles(const AttendArgs& a, const RowTile& w) {
+  const int last = min(w.first + (1 << a.row_log), w.q_len * a.group) - 1, at = w.len - w.q_len;
+  return key_tiles(a, w.len, at + w.first / a.group, at + last / a.group);
+}
 
-// Workgroups that share nt key tiles, and the share of workgroup s.
-__device__ __forceinline__ int key_shares(const AttendArgs& a, int nt) { return max(1, min(a.splits, (nt + a.chunk - 1) / a.chunk)); }
+// A workgroup's share of a row tile's keys: tiles [share * per, + per) of nt, the
+// n-th part; its partial result is number `slot` (of the call's, for a head).
+struct Share {
+  int f, share, n, per;
+  long slot;
+};
+
+__device__ __forceinline__ int seq_len(const AttendArgs& a, RowTile& w) { return a.lens ? cached_len(a, w.seq) : plain_len(a, w); }
+
+// Sums over the lanes up to each.
+__device__ __forceinline__ int lanes_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // within rows of 16: from 1, 2, 4, 8 lanes before
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row 0's sum to row 1, row 2's to row 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // the first two rows' sum to the others
+  return x;
+}
+
+// Even shares, for up to 64 sequences of one row tile each: every wave has their key
+// tiles in its lanes, which gives the size of a share, and from the shares before
+// each sequence its own.  want: share number (of a head), or with TILE the sequence
+// whose shares are asked for.
+template <bool TILE>
+__device__ __forceinline__ bool even_share(const AttendArgs& a, int want, Share& s) {
+  const int lane = threadIdx.x & 63;
+  const bool in = lane < a.tiles;
+  RowTile w;
+  w.seq = min(lane, a.tiles - 1);
+  const int len = seq_len(a, w), nt = in ? key_tiles(a, len, len - a.q_len, len - 1).nt : 0;
+  const int total = __builtin_amdgcn_readlane(lanes_scan(nt), 63), chunk = max(a.chunk, (total + a.even - 1) / a.even);
+  const int n = in ? max(1, min(kMostShares, (nt + chunk - 1) / chunk)) : 0, upto = lanes_scan(n);
+  const uint64_t there = __ballot(TILE ? lane == want : in & (upto > want));
+  if (!there) return false;
+  s.f = __builtin_ctzll(there);
+  s.n = __builtin_amdgcn_readlane(n, s.f);
+  s.per = (__builtin_amdgcn_readlane(nt, s.f) + s.n - 1) / s.n;
+  const int first = __builtin_amdgcn_readlane(upto, s.f) - s.n;
+  s.share = TILE ? 0 : want - first;
+  s.slot = first + s.share;
+  return true;
+}
+
+// The share of workgroup number b (of a head), its row tile and key tiles; false for
+// one that has none.
+__device__ __forceinline__ bool my_share(const AttendArgs& a, int b, RowTile& w, KeyTiles& k, Share& s) {
+  if (a.even) {
+    if (!even_share<false>(a, b, s) || !row_tile(a, s.f, w)) return false;
+    w.len = seq_len(a, w);
+    k = key_tiles(a, w);
+    return true;
+  }
+  // of the row tiles the last, which see the most keys, start first
+  s.share = b / a.tiles;
+  s.f = a.tiles - 1 - (b - s.share * a.tiles);
+  if (!row_tile(a, s.f, w)) return false;
+  w.len = seq_len(a, w);
+  k = key_tiles(a, w);
+  s.n = max(1, min(a.splits, (k.nt + a.chunk - 1) / a.chunk));
+  s.per = (k.nt + s.n - 1) / s.n;
+  s.slot = (long)s.f * a.splits + s.share;
+  return s.share < s.n;
+}
+// The shares of row tile f, to join them.
+__device__ __forceinline__ bool shares_of(const AttendArgs& a, int f, RowTile& w, Share& s) {
+  if (!row_tile(a, f, w)) return false;
+  if (a.even) return even_share<true>(a, f, s);
+  w.len = seq_len(a, w);
+  s.n = max(1, min(a.splits, (key_tiles(a, w).nt + a.chunk - 1) / a.chunk));
+  s.slot = (long)f * a.splits;
+  return true;
+}
 
 // The keys that a row at position `pos` sees: `n` from lo on, and those below
 // `sinks`.  Two comparisons without a branch (a chain of && over a lane's keys
@@ -298,13 +379,18 @@ __device__ __forceinline__ f32x4_t mma16(const uint4& a, const uint4& b, f32x4_t
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
+// The running maximum follows the scores only where they leave it by more than
+// this (in units of log2): weights stay below 2^8, and sums are rescaled rarely.
+constexpr float kSlack = 8.0f;
+
 // One step of the online softmax for a lane's 8 scores x (in units of log2, -inf
 // where masked) of one query: p = 2^(x - m), and the factor for what was summed.
 __device__ __forceinline__ float soft_step(const float* x, float& m, float& l, float* p) {
   float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-  const float m_new = fmaxf(m, group4_max(top));
+  top = group4_max(top);
+  const float m_new = top > m + kSlack ? top : m;
   const float sub = m_new == -INFINITY ? 0.0f : m_new;  // nothing yet: every p is 0
-  const float alpha = __builtin_amdgcn_exp2f(m - sub);
+  const float alpha = m_new == m ? 1.0f : __builtin_amdgcn_exp2f(m - sub);
   float sum = 0.0f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -346,13 +432,13 @@ constexpr int exchange_bytes() {
 // [wave][row], O [wave][row][DS + 4]), and stores rows below `rows`: the result
 // where the tile's keys are one workgroup's, else the partial result.
 template <class T, int DS, int NT>
-__device__ __forceinline__ void join_waves(const AttendArgs& a, const RowTile& w, const char* lds, int h, int share, int shares, int f) {
+__device__ __forceinline__ void join_waves(const AttendArgs& a, const RowTile& w, const Share& sh, const char* lds, int h) {
   constexpr int TR = 16 * NT;
   const float* s_m = reinterpret_cast<const float*>(lds);
   const float* s_l = s_m + kKeyWaves * TR;
   const float* s_o = s_l + kKeyWaves * TR;
   const int rows = min(TR, w.q_len * a.group - w.first);
-  float* part = a.parts + ((size_t)((long)f * a.hk + h) * a.splits + share) * TR * (DS + 2);
+  float* part = a.parts + (size_t)(sh.slot * a.hk + h) * TR * (DS + 2);
   for (int i = threadIdx.x; i < rows * (DS / 4); i += 64 * kKeyWaves) {
     const int r = i / (DS / 4), d = (i - r * (DS / 4)) * 4;
     float m = -INFINITY;
@@ -367,7 +453,7 @@ __device__ __forceinline__ void join_waves(const AttendArgs& a, const RowTile& w
       l += e * s_l[k * TR + r];
       o += *reinterpret_cast<const f32x4_t*>(s_o + (size_t)(k * TR + r) * (DS + 4) + d) * e;
     }
-    if (shares > 1) {
+    if (sh.n > 1) {
       if (d == 0) *(INCVIT_GLOBAL u32x2_t*)(part + 2 * r) = u32x2_t{__float_as_uint(m), __float_as_uint(l)};
       *(INCVIT_GLOBAL f32x4_t*)(part + 2 * TR + r * DS + d) = o;
     } else if (d < a.d) {

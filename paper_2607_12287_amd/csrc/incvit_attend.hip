@@ -9,6 +9,9 @@ using namespace incvit;
 
 namespace {
 
+// Workgroups of a call that shares keys, where waves have keys and where they have
+// rows, and the key tiles of one at least.
+constexpr long kWant = 1536, kWantRows = 512, kLeast = 16, kLeastRows = 8;
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 
 bool is_dtype(int32_t t) { return t == INCVIT_F32 || t == INCVIT_BF16; }
@@ -76,7 +79,7 @@ incvit_status check_attention(const incvit_attention* a, int32_t n, int64_t rows
 }
 
 incvit_status check_plan(const incvit_attention& a, const AttendPlan& p, const void* workspace) {
-  if (p.tiles * a.kv_heads * p.splits >= (1 << 24)) return op_fail(INCVIT_ERR_UNSUPPORTED, "too many rows and sequences for one launch");
+  if (p.shares * a.kv_heads >= (1 << 24)) return op_fail(INCVIT_ERR_UNSUPPORTED, "too many rows and sequences for one launch");
   if (p.bytes && (!workspace || (uintptr_t)workspace % 256))
     return op_fail(INCVIT_ERR_ARG, "the workspace must be non-null and 256-byte aligned");
   return INCVIT_OK;
@@ -108,6 +111,8 @@ AttendArgs attend_args(const incvit_attention& a, const AttendPlan& p, int32_t n
   r.tiles_each = p.tiles_each;
   r.splits = p.splits;
   r.chunk = p.chunk;
+  r.even = p.even;
+  r.shares = p.shares;
   return r;
 }
 
@@ -141,10 +146,20 @@ AttendPlan incvit::attend_plan(const incvit_attention& a, bool cached, long n, l
   if (a.window) span = std::min(span, (long)a.window * (a.causal ? 1 : 2) + tr / group + 1 + a.sinks + 3 * kt);
   const long tiles = std::max(1L, (span + kt - 1) / kt);
   const long wgs = std::max(1L, p.tiles * a.kv_heads);
-  const long want = std::max(1L, (p.by_rows ? 512 : 1024) / wgs);
-  p.chunk = (int)std::max(p.by_rows ? 8L : 4L * kKeyWaves, (tiles + want - 1) / want);
-  p.splits = (int)std::min(256L, (tiles + p.chunk - 1) / p.chunk);
-  if (p.splits > 1) p.bytes = (size_t)wgs * p.splits * tr * (ds + 2) * 4;
+  p.splits = 1;
+  p.shares = p.tiles;
+  p.chunk = (int)(p.by_rows ? kLeastRows : kLeast);
+  if (tiles <= p.chunk) return p;
+  if (!p.by_rows && !ragged && n > 1 && n <= kEvenTiles && p.tiles_each == 1) {
+    p.even = (int)std::max(1L, kWant / a.kv_heads);
+    p.shares = p.even + p.tiles;
+  } else if (wgs < 256) {
+    const long want = (p.by_rows ? kWantRows : kWant) / wgs;
+    p.chunk = (int)std::max((long)p.chunk, (tiles + want - 1) / want);
+    p.splits = (int)std::min((long)kMostShares, (tiles + p.chunk - 1) / p.chunk);
+    p.shares = p.tiles * p.splits;
+  }
+  if (p.splits > 1 || p.even) p.bytes = (size_t)p.shares * a.kv_heads * tr * (ds + 2) * 4;
   return p;
 }
 

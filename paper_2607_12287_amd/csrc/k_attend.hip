@@ -18,16 +18,13 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
   extern __shared__ __align__(16) char lds[];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = blockIdx.x % a.hk, rest = blockIdx.x / a.hk;
-  const int share = rest / a.tiles, f = a.tiles - 1 - (rest - share * a.tiles);
+  const int h = blockIdx.x % a.hk;
   RowTile w;
-  if (!row_tile(a, f, w)) return;
-  w.len = plain_len(a, w);
-  const KeyTiles kt = key_tiles(a, w);
-  const int shares = key_shares(a, kt.nt);
-  if (share >= shares) return;
-  const int i1 = (int)((long)(share + 1) * kt.nt / shares);
-  const int first = (int)((long)share * kt.nt / shares) + wave;
+  KeyTiles kt;
+  Share sh;
+  if (!my_share(a, blockIdx.x / a.hk, w, kt, sh)) return;
+  const int i1 = min(kt.nt, (sh.share + 1) * sh.per);
+  const int first = sh.share * sh.per + wave;
   int i = first;
 
   const T* keys = static_cast<const T*>(a.k.p) + w.k0 * a.k.row + (long)h * a.k.head;
@@ -195,7 +192,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
     for (int k = 0; k < NP; ++k) *reinterpret_cast<f32x4_t*>(s_o + (size_t)r * (DS + 4) + 16 * k + 4 * g) = o[t][k];
   }
   __syncthreads();
-  join_waves<T, DS, NT>(a, w, lds, h, share, shares, f);
+  join_waves<T, DS, NT>(a, w, sh, lds, h);
 }
 
 template <class T, int DS, int NT>
@@ -204,7 +201,7 @@ hipError_t launch_one(const AttendArgs& a, hipStream_t s) {
   static_assert(bytes <= 160 * 1024, "LDS");
   const hipError_t e = with_lds<attend_kernel<T, DS, NT>>(bytes);
   if (e != hipSuccess) return e;
-  return launch_k(attend_kernel<T, DS, NT>, dim3((unsigned)((long)a.tiles * a.hk * a.splits)), dim3(64 * kKeyWaves), (size_t)bytes, s, a);
+  return launch_k(attend_kernel<T, DS, NT>, dim3((unsigned)(a.shares * a.hk)), dim3(64 * kKeyWaves), (size_t)bytes, s, a);
 }
 
 template <class T>

@@ -1,54 +1,66 @@
-// Partial results of a row tile's shares of keys joined into rows of the output:
-//   m = max m_s,  l = sum 2^(m_s - m) l_s,  out = sum 2^(m_s - m) O_s / l
-// in the order of the shares.  A thread has 4 dims of a row.  Row tiles whose keys
-// were one workgroup's are there already.
+// Partial results of a row's shares of keys joined into the output:
+//   m = max m_s,  l = sum 2^(m_s - m) l_s,  out = sum 2^(m_s - m) O_s / l.
+// A workgroup has a row: its threads take the shares' weights together, then 4 dims
+// each of every (1024 / DS)-th share, and add those through LDS, in a fixed order.
+// Row tiles whose keys were one workgroup's are there already.
 #include "attend.hpp"
 
 namespace incvit {
 
 namespace {
 
-// cached: whether key tiles are those of the cache (lens) or of given keys
-template <class T, int DS, bool CACHED>
+template <class T, int DS>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-  const int TR = 1 << a.row_log;
-  const int h = blockIdx.x % a.hk, f = blockIdx.x / a.hk;
+  constexpr int Q = DS / 4, PARTS = 256 / Q;  // threads of a part, and parts (192 dims: 5 of 48, the rest idle)
+  __shared__ float s_e[kMostShares], s_m[4], s_l[4];
+  __shared__ f32x4_t s_o[PARTS][Q];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int h = blockIdx.x % a.hk, f = blockIdx.x / a.hk, r = blockIdx.y;
   RowTile w;
-  if (!row_tile(a, f, w)) return;
-  w.len = CACHED ? cached_len(a, w.seq) : plain_len(a, w);
-  const int shares = key_shares(a, key_tiles(a, w).nt);
-  if (shares < 2) return;
-  const int rows = min(TR, w.q_len * a.group - w.first);
-  const float* part = a.parts + (size_t)((long)f * a.hk + h) * a.splits * TR * (DS + 2);
-  const int i = blockIdx.y * 256 + threadIdx.x;
-  const int r = i / (DS / 4), d = (i - r * (DS / 4)) * 4;
-  if (r >= rows || d >= a.d) return;
-  float m = -INFINITY;
-  for (int s = 0; s < shares; ++s) m = fmaxf(m, gbl(part)[(size_t)s * TR * (DS + 2) + 2 * r]);
-  float l = 0.0f;
-  f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int s = 0; s < shares; ++s) {
-    const float* p = part + (size_t)s * TR * (DS + 2);
-    const u32x2_t ml = *(const INCVIT_GLOBAL u32x2_t*)(p + 2 * r);
-    const f32x4_t v = *(const INCVIT_GLOBAL f32x4_t*)(p + 2 * TR + r * DS + d);
-    const float ms = __uint_as_float(ml[0]), e = ms == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ms - m);
-    l += e * __uint_as_float(ml[1]);
-    o += v * e;
+  Share sh;
+  if (!shares_of(a, f, w, sh) || sh.n < 2 || w.first + r >= w.q_len * a.group) return;
+  const int shares = sh.n;
+  const size_t step = (size_t)(DS + 2) << a.row_log;
+  const float* part = a.parts + (size_t)(sh.slot * a.hk + h) * step;
+  float m = -INFINITY, l = 0.0f;
+  if (tid < shares) {
+    const u32x2_t ml = *(const INCVIT_GLOBAL u32x2_t*)(part + tid * a.hk * step + 2 * r);
+    m = __uint_as_float(ml[0]);
+    l = __uint_as_float(ml[1]);
   }
+  const float top = wave_max(m);
+  if (lane == 0) s_m[wave] = top;
+  __syncthreads();
+  const float mm = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+  const float e = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mm);
+  s_e[tid] = e;
+  const float sum = wave_sum(e * l);
+  if (lane == 0) s_l[wave] = sum;
+  __syncthreads();
+  const int p = tid / Q, d = (tid - p * Q) * 4;
+  f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (p < PARTS) {
+    const float* at = part + ((size_t)2 << a.row_log) + (size_t)r * DS + d;
+#pragma unroll 8
+    for (int s = p; s < shares; s += PARTS) o += *(const INCVIT_GLOBAL f32x4_t*)(at + s * a.hk * step) * s_e[s];
+    s_o[p][d / 4] = o;
+  }
+  __syncthreads();
+  if (p != 0 || d >= a.d) return;
+#pragma unroll
+  for (int k = 1; k < PARTS; ++k) o += s_o[k][d / 4];
+  const float inv = 1.0f / (s_l[0] + s_l[1] + s_l[2] + s_l[3]);
   const int row = w.first + r, tok = row / a.group, head = h * a.group + row - tok * a.group;
-  const float inv = 1.0f / l;
   float y[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) y[j] = m == -INFINITY ? 0.0f : o[j] * inv;
+  for (int j = 0; j < 4; ++j) y[j] = mm == -INFINITY ? 0.0f : o[j] * inv;
   store_out4<T>(static_cast<T*>(const_cast<void*>(a.out.p)) + (w.q0 + tok) * a.out.row + (long)head * a.out.head + d, y);
 }
 
 template <class T, int DS>
 hipError_t launch_ds(const AttendArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((long)a.tiles * a.hk), (std::min(1 << a.row_log, a.most_rows) * (DS / 4) + 255) / 256);
-  return a.lens ? launch_k(attend_join_kernel<T, DS, true>, grid, dim3(256), 0, s, a)
-                : launch_k(attend_join_kernel<T, DS, false>, grid, dim3(256), 0, s, a);
+  const dim3 grid((unsigned)((long)a.tiles * a.hk), std::min(1 << a.row_log, a.most_rows));
+  return launch_k(attend_join_kernel<T, DS>, grid, dim3(256), 0, s, a);
 }
 
 template <class T>
@@ -67,7 +79,7 @@ hipError_t launch_t(const AttendArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_attend_join(const AttendArgs& a, int dtype, hipStream_t s) {
-  if (a.splits < 2) return hipSuccess;
+  if (a.splits < 2 && !a.even) return hipSuccess;
   return dtype == INCVIT_BF16 ? launch_t<uint16_t>(a, s) : launch_t<float>(a, s);
 }
 

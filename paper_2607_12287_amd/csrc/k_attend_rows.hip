@@ -13,10 +13,6 @@ namespace incvit {
 
 namespace {
 
-// The running maximum follows the scores only where they leave it by more than
-// this (in units of log2): weights stay below 2^8, and sums are rescaled rarely.
-constexpr float kSlack = 8.0f;
-
 template <class T, int DS, int NT>
 __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs a) {
   constexpr int NP = DS / 16, NC = DS / 32 + (DS % 32 != 0), RB = row_bytes<T, DS>(), EB = sizeof(T);
@@ -27,15 +23,12 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
   __shared__ int s_special[2][kKeyWaves];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int h = blockIdx.x % a.hk, rest = blockIdx.x / a.hk;
-  const int share = rest / a.tiles, f = a.tiles - 1 - (rest - share * a.tiles);
+  const int h = blockIdx.x % a.hk;
   RowTile w;
-  if (!row_tile(a, f, w)) return;
-  w.len = plain_len(a, w);
-  const KeyTiles kt = key_tiles(a, w);
-  const int shares = key_shares(a, kt.nt);
-  if (share >= shares) return;
-  const int i0 = (int)((long)share * kt.nt / shares), i1 = (int)((long)(share + 1) * kt.nt / shares);
+  KeyTiles kt;
+  Share sh;
+  if (!my_share(a, blockIdx.x / a.hk, w, kt, sh)) return;
+  const int i0 = sh.share * sh.per, i1 = min(kt.nt, i0 + sh.per);
 
   const int all = w.q_len * a.group, first = w.first + wave * 16 * NT;
   const int p0 = w.len - w.q_len + min(first, all - 1) / a.group, p1 = w.len - w.q_len + (min(first + 16 * NT, all) - 1) / a.group;
@@ -215,7 +208,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
   }
 
   // a lane has dims 16 k + 4 g .. + 3 of its rows
-  if (shares == 1) __syncthreads();  // the rows take the tiles' place
+  if (sh.n == 1) __syncthreads();  // the rows take the tiles' place
   char* rows = lds + wave * 16 * RB;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -223,10 +216,10 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
     const bool any = group4_max(seen[t] ? 1.0f : 0.0f) > 0.0f;
     const int row0 = first + 16 * t;
     if (row0 >= all) break;
-    if (shares > 1) {
+    if (sh.n > 1) {
       const int r = row0 - w.first + n;
       if (row0 + n < all) {
-        float* part = a.parts + (((size_t)((long)f * a.hk + h) * a.splits + share) << a.row_log) * (DS + 2);
+        float* part = a.parts + ((size_t)(sh.slot * a.hk + h) << a.row_log) * (DS + 2);
         if (g == 0)
           *(INCVIT_GLOBAL u32x2_t*)(part + 2 * r) =
               u32x2_t{__float_as_uint(m[t] == -INFINITY && any ? kNoMax : m[t]), __float_as_uint(sum)};
@@ -270,7 +263,7 @@ hipError_t launch_one(const AttendArgs& a, hipStream_t s) {
   static_assert(bytes <= 156 * 1024, "LDS");
   const hipError_t e = with_lds<attend_rows_kernel<T, DS, NT>>(bytes);
   if (e != hipSuccess) return e;
-  return launch_k(attend_rows_kernel<T, DS, NT>, dim3((unsigned)((long)a.tiles * a.hk * a.splits)), dim3(64 * kKeyWaves), (size_t)bytes, s, a);
+  return launch_k(attend_rows_kernel<T, DS, NT>, dim3((unsigned)(a.shares * a.hk)), dim3(64 * kKeyWaves), (size_t)bytes, s, a);
 }
 
 template <class T, int DS>

@@ -50,24 +50,24 @@ struct RawTile {
   int ok;  // bit u: group u lies in a block of the pool
 };
 
+// Three workgroups to a CU where the registers allow it without spills.
 template <class T, int DS, int NT>
-__global__ __launch_bounds__(64 * kKeyWaves) void kv_attend_kernel(AttendArgs a) {
+constexpr int kPerCu = NT == 1 && DS <= (sizeof(T) == 2 ? 128 : 80) ? 3 : 1;
+
+template <class T, int DS, int NT>
+__global__ __launch_bounds__(64 * kKeyWaves, (kPerCu<T, DS, NT>)) void kv_attend_kernel(AttendArgs a) {
   constexpr int NP = DS / 16, NC = (NP + 3) / 4, TAIL = NP % 4, TR = 16 * NT, PARTS = sizeof(T) == 4 ? 3 : 1;
   extern __shared__ __align__(16) char lds[];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // heads first: a head's workgroups share an XCD's L2 where heads are a multiple
-  // of 8; of the tiles the last, which see the most keys, start first
-  const int h = blockIdx.x % a.hk, rest = blockIdx.x / a.hk;
-  const int share = rest / a.tiles, f = a.tiles - 1 - (rest - share * a.tiles);
+  // heads first: a head's workgroups share an XCD's L2 where heads are a multiple of 8
+  const int h = blockIdx.x % a.hk;
   RowTile w;
-  if (!row_tile(a, f, w)) return;
-  w.len = cached_len(a, w.seq);
-  const KeyTiles kt = key_tiles(a, w);
-  const int shares = key_shares(a, kt.nt);
-  if (share >= shares) return;
-  const int i1 = (int)((long)(share + 1) * kt.nt / shares);
-  int i = (int)((long)share * kt.nt / shares) + wave;
+  KeyTiles kt;
+  Share sh;
+  if (!my_share(a, blockIdx.x / a.hk, w, kt, sh)) return;
+  const int i1 = min(kt.nt, (sh.share + 1) * sh.per);
+  int i = sh.share * sh.per + wave;
 
   const int* table = a.table + (long)w.seq * a.table_stride;
   const int mask = (1 << a.lb) - 1;
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void kv_attend_kernel(AttendArgs a)
     }
   }
   __syncthreads();
-  join_waves<T, DS, NT>(a, w, lds, h, share, shares, f);
+  join_waves<T, DS, NT>(a, w, sh, lds, h);
 }
 
 template <class T, int DS, int NT>
@@ -253,7 +253,7 @@ hipError_t launch_one(const AttendArgs& a, hipStream_t s) {
   static_assert(bytes <= 160 * 1024, "LDS");
   const hipError_t e = with_lds<kv_attend_kernel<T, DS, NT>>(bytes);
   if (e != hipSuccess) return e;
-  return launch_k(kv_attend_kernel<T, DS, NT>, dim3((unsigned)((long)a.tiles * a.hk * a.splits)), dim3(64 * kKeyWaves), (size_t)bytes, s, a);
+  return launch_k(kv_attend_kernel<T, DS, NT>, dim3((unsigned)(a.shares * a.hk)), dim3(64 * kKeyWaves), (size_t)bytes, s, a);
 }
 
 template <class T, int DS>
