@@ -510,10 +510,10 @@ incvit_status incvit_kv_write(const incvit_kv* c, int32_t dtype, int64_t rows, c
 
 /* Read slots back, q * s in fp32 rounded to dtype: strides, alignments, slots and
  * errors as above; slots may repeat, heads of k and v must not overlap.  A row
- * whose slot is outside the pool is left as it was. */
+ * whose slot is outside the pool is left as it was (fill 0) or becomes zeros (1). */
 incvit_status incvit_kv_read(const incvit_kv* c, const void* cache, int32_t dtype, int64_t rows,
-                             const int32_t* slots, void* k, int64_t k_row, int64_t k_head, void* v,
-                             int64_t v_row, int64_t v_head, void* stream);
+                             const int32_t* slots, int32_t fill, void* k, int64_t k_row,
+                             int64_t k_head, void* v, int64_t v_row, int64_t v_head, void* stream);
 
 /* -------------------------------------------------------------- attention -- */
 

@@ -18,14 +18,14 @@ DRIVE = os.path.join(HERE, "incvit_drive")
 SOURCES = ["incvit_api.hip", "k_embed.hip", "k_select.hip", "k_gemm.hip", "k_gemm_qkv.hip",
            "k_gemm_fc1.hip", "k_gemm_part.hip", "k_gemm_res.hip", "k_gemm_att.hip", "k_gemm_down.hip", "k_gemm_tiled.hip", "k_rows.hip", "k_attn.hip", "k_misc.hip", "k_flow.hip",
            "incvit_ops.hip", "k_rope.hip", "k_qk.hip", "k_qlinear.hip", "incvit_attend.hip", "k_kv.hip", "k_kv_attend.hip",
-           "k_attend.hip", "k_attend_rows.hip", "k_attend_join.hip"]
+           "k_kv_attend_rows.hip", "k_attend.hip", "k_attend_rows.hip", "k_attend_join.hip"]
 # the fixed-order fp32 embedding and cosine must not be contracted beyond the
 # explicit fma intrinsics
 NO_CONTRACT = {"k_embed.hip"}
 # matrix products write to vector registers, where the softmax needs them, also in
 # kernels of one wave to a SIMD: through accumulation registers the attention
 # kernels took a half more of both
-VECTOR_ACC = {"k_attend.hip", "k_attend_rows.hip", "k_kv_attend.hip"}
+VECTOR_ACC = {"k_attend.hip", "k_attend_rows.hip", "k_kv_attend.hip", "k_kv_attend_rows.hip"}
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

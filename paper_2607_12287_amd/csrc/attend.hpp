@@ -55,7 +55,7 @@ struct KvReadArgs {
   const char* cache;
   size_t data;
   long rows;
-  int blocks, block, heads, d, dtype;
+  int blocks, block, heads, d, dtype, fill;
   uint32_t per_inv;  // 2^32 / (d / 8), rounded up
 };
 
@@ -97,10 +97,11 @@ struct AttendArgs {
 };
 
 // 16-row tiles of a workgroup over the cache, at most: as many as the registers hold.
-constexpr int most_row_tiles(bool bf16, int ds) { return bf16 ? (ds <= 96 ? 4 : ds <= 192 ? 2 : 1) : ds <= 128 ? 2 : 1; }
+constexpr int most_row_tiles(bool bf16, int ds) { return ds <= (bf16 ? 192 : 128) ? 2 : 1; }
 
 // 16-row tiles of a wave of its own rows, at most; keys of a tile there
-constexpr int most_wave_tiles(bool bf16, int ds) { return bf16 || ds <= 128 ? 2 : 1; }
+constexpr int most_wave_tiles(bool bf16, int ds) { return bf16 ? 2 : 1; }
+constexpr int most_cached_wave_tiles(int ds) { return ds <= 128 ? 2 : 1; }
 constexpr int rows_key_log(bool bf16, int ds) { return ds * (bf16 ? 2 : 4) <= 512 ? 6 : 5; }
 
 struct AttendPlan {
@@ -116,6 +117,7 @@ AttendPlan attend_plan(const incvit_attention& a, bool cached, long n, long rows
 
 hipError_t launch_kv_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
+hipError_t launch_kv_attend_rows(const AttendArgs& a, const AttendPlan& p, hipStream_t s);
 hipError_t launch_attend_rows(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
 hipError_t launch_attend_join(const AttendArgs& a, int dtype, hipStream_t s);
 
@@ -321,6 +323,26 @@ __device__ __forceinline__ bool all_seen(const AttendArgs& a, int len, int p0, i
 // A row's partial result: m, the largest score in units of log2; l, the sum of
 // 2^(x - m); O.  m = -inf: no key was seen.  kNoMax: keys were seen, none above -inf.
 constexpr float kNoMax = -3.0e38f;
+
+// Blocks and scales of groups of 16 tokens, one in each lane: read by vector loads
+// for many tiles at once.  (One by one they became scalar loads, each of which a
+// wave waits for alone.)  blk: -1 where the group lies in no block of the pool.
+struct GroupInfo {
+  int blk;
+  float ks, vs;
+  __device__ __forceinline__ void load(const AttendArgs& a, const int* table, int h, int group) {
+    const int e = min(group >> a.lb, a.width - 1);
+    const int b = gbl(table)[e];
+    const bool in = (group >> a.lb < a.width) & (b >= 0) & (b < a.blocks);
+    blk = in ? b : -1;
+    const u32x2_t s = *(const INCVIT_GLOBAL u32x2_t*)(a.cache + ((size_t)(in ? b : 0) * a.hk + h) * 8);
+    ks = __uint_as_float(s[0]);
+    vs = __uint_as_float(s[1]);
+  }
+};
+__device__ __forceinline__ float lane_float(float x, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
+}
 
 // max, sum and "any" over the four lane groups (lanes n, n + 16, n + 32, n + 48)
 __device__ __forceinline__ float group4_max(float x) {

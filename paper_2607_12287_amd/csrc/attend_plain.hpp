@@ -13,11 +13,16 @@ namespace incvit {
 
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 
-// Bytes of a row of values in LDS: 16 more than its dims, so that 16 rows' pieces
-// of the same dims spread over the banks.
+// Bytes of a row in LDS, which spread over the banks what lanes read at once: of keys
+// 16 bytes of 8 rows each (an odd number of 16 bytes more than 128); of values, which
+// bf16 reads transposed, 32 bytes of 4 rows (an odd number of 32 more).
 template <class T, int DS>
 constexpr int row_bytes() {
   return DS * (int)sizeof(T) + 16;
+}
+template <class T, int DS>
+constexpr int value_bytes() {
+  return sizeof(T) == 4 ? row_bytes<T, DS>() : 2 * DS + (2 * DS % 64 == 0 ? 32 : 0);
 }
 
 template <class T>

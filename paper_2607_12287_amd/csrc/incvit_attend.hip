@@ -126,17 +126,14 @@ AttendPlan incvit::attend_plan(const incvit_attention& a, bool cached, long n, l
   const long group = a.q_heads / a.kv_heads, each = (rows + n - 1) / n * group;
   const int ds = kv_dims(a.head_dim);
   p.key_log = 5;
-  if (cached) {
-    p.nt = std::min(most_row_tiles(bf16, ds), each <= 16 ? 1 : each <= 32 ? 2 : 4);
-    p.row_log = p.nt == 1 ? 4 : p.nt == 2 ? 5 : 6;
-  } else if (each > 32) {
+  if (each > (cached ? 64 : 32) && (bf16 || !cached)) {
     p.by_rows = 1;
-    p.nt = std::min(most_wave_tiles(bf16, ds), each <= 64 || rows * group / 128 * a.kv_heads < 256 ? 1 : 2);
+    p.nt = std::min(cached ? most_cached_wave_tiles(ds) : most_wave_tiles(bf16, ds), each <= 64 ? 1 : 2);
     p.row_log = 5 + p.nt;
-    p.key_log = rows_key_log(bf16, ds);
+    p.key_log = cached ? 6 : rows_key_log(bf16, ds);
   } else {
-    p.nt = 1;
-    p.row_log = 4;
+    p.nt = cached ? std::min(most_row_tiles(bf16, ds), each <= 16 ? 1 : 2) : 1;
+    p.row_log = 3 + p.nt;
   }
   const long tr = 1L << p.row_log, kt = 1L << p.key_log;
   p.tiles_each = (int)((rows / n * group + tr - 1) / tr);
@@ -149,7 +146,7 @@ AttendPlan incvit::attend_plan(const incvit_attention& a, bool cached, long n, l
   p.splits = 1;
   p.shares = p.tiles;
   p.chunk = (int)(p.by_rows ? kLeastRows : kLeast);
-  if (tiles <= p.chunk) return p;
+  if (tiles <= 2 * p.chunk) return p;  // a second launch takes as long as the keys that it saves
   if (!p.by_rows && !ragged && n > 1 && n <= kEvenTiles && p.tiles_each == 1) {
     p.even = (int)std::max(1L, kWant / a.kv_heads);
     p.shares = p.even + p.tiles;
@@ -193,12 +190,14 @@ incvit_status incvit_kv_write(const incvit_kv* c, int32_t dtype, int64_t rows, c
   return launched(launch_kv_write(a, static_cast<hipStream_t>(stream)), "kv_write");
 }
 
-incvit_status incvit_kv_read(const incvit_kv* c, const void* cache, int32_t dtype, int64_t rows, const int32_t* slots, void* k,
-                             int64_t k_row, int64_t k_head, void* v, int64_t v_row, int64_t v_head, void* stream) {
+incvit_status incvit_kv_read(const incvit_kv* c, const void* cache, int32_t dtype, int64_t rows, const int32_t* slots,
+                             int32_t fill, void* k, int64_t k_row, int64_t k_head, void* v, int64_t v_row, int64_t v_head,
+                             void* stream) {
   incvit_status st = check_kv(c, dtype, rows, cache, slots);
   if (st != INCVIT_OK || rows == 0) return st;
   if ((st = check_rows(dtype, k, k_row, k_head, "k")) != INCVIT_OK) return st;
   if ((st = check_rows(dtype, v, v_row, v_head, "v")) != INCVIT_OK) return st;
+  if (fill != 0 && fill != 1) return op_fail(INCVIT_ERR_ARG, "fill must be 0 or 1");
   if (!apart(rows, k_row, c->heads, k_head, c->head_dim) || !apart(rows, v_row, c->heads, v_head, c->head_dim))
     return op_fail(INCVIT_ERR_SHAPE, "heads of the output overlap");
   KvReadArgs a = {};
@@ -213,6 +212,7 @@ incvit_status incvit_kv_read(const incvit_kv* c, const void* cache, int32_t dtyp
   a.heads = c->heads;
   a.d = c->head_dim;
   a.dtype = dtype;
+  a.fill = fill;
   return launched(launch_kv_read(a, static_cast<hipStream_t>(stream)), "kv_read");
 }
 
@@ -258,7 +258,7 @@ incvit_status incvit_kv_attend(const incvit_attention* a, const incvit_kv* c, co
   r.blocks = c->blocks;
   r.lb = lay.lb;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if ((st = launched(launch_kv_attend(r, p, a->dtype, s), "kv_attend")) != INCVIT_OK) return st;
+  if ((st = launched(p.by_rows ? launch_kv_attend_rows(r, p, s) : launch_kv_attend(r, p, a->dtype, s), "kv_attend")) != INCVIT_OK) return st;
   return launched(launch_attend_join(r, a->dtype, s), "kv_attend");
 }
 

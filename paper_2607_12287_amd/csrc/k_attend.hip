@@ -12,7 +12,7 @@ namespace {
 
 template <class T, int DS, int NT>
 __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
-  constexpr int NP = DS / 16, NC = DS / 32 + (DS % 32 != 0), TR = 16 * NT, RB = row_bytes<T, DS>();
+  constexpr int NP = DS / 16, NC = DS / 32 + (DS % 32 != 0), TR = 16 * NT, RB = value_bytes<T, DS>();
   constexpr int PER = DS / 8, NV = (kKeyTile * PER + 63) / 64;  // 8-dim pieces of a row of values, of a lane
   constexpr bool AHEAD = DS * sizeof(T) <= 384;  // whether registers hold the next tile's values as well
   extern __shared__ __align__(16) char lds[];
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
 
 template <class T, int DS, int NT>
 hipError_t launch_one(const AttendArgs& a, hipStream_t s) {
-  constexpr int bytes = std::max(exchange_bytes<DS, NT>(), kKeyWaves * kKeyTile * row_bytes<T, DS>());
+  constexpr int bytes = std::max(exchange_bytes<DS, NT>(), kKeyWaves * kKeyTile * value_bytes<T, DS>());
   static_assert(bytes <= 160 * 1024, "LDS");
   const hipError_t e = with_lds<attend_kernel<T, DS, NT>>(bytes);
   if (e != hipSuccess) return e;

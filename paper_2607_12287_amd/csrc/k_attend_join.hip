@@ -2,7 +2,8 @@
 //   m = max m_s,  l = sum 2^(m_s - m) l_s,  out = sum 2^(m_s - m) O_s / l.
 // A workgroup has a row: its threads take the shares' weights together, then 4 dims
 // each of every (1024 / DS)-th share, and add those through LDS, in a fixed order.
-// Row tiles whose keys were one workgroup's are there already.
+// Row tiles whose keys were one workgroup's are there already.  Where row tiles are
+// large, and their shares few, a thread has 4 dims of a row and all of its shares.
 #include "attend.hpp"
 
 namespace incvit {
@@ -58,8 +59,45 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 }
 
 template <class T, int DS>
+__global__ __launch_bounds__(256) void attend_join_rows_kernel(AttendArgs a) {
+  constexpr int Q = DS / 4, ROWS = 256 / Q;  // rows of a workgroup
+  const int h = blockIdx.x % a.hk, f = blockIdx.x / a.hk;
+  const int at = threadIdx.x / Q, r = blockIdx.y * ROWS + at, d = (threadIdx.x - at * Q) * 4;
+  RowTile w;
+  Share sh;
+  if (!shares_of(a, f, w, sh) || sh.n < 2) return;
+  if (at >= ROWS || d >= a.d || r >= min(1 << a.row_log, w.q_len * a.group - w.first)) return;
+  const size_t step = ((size_t)(DS + 2) << a.row_log) * a.hk;
+  const float* part = a.parts + ((size_t)(sh.slot * a.hk + h) << a.row_log) * (DS + 2);
+  const float* row = part + ((size_t)2 << a.row_log) + (size_t)r * DS + d;
+  float m = -INFINITY, l = 0.0f;
+#pragma unroll 4
+  for (int s = 0; s < sh.n; ++s) m = fmaxf(m, gbl(part)[s * step + 2 * r]);
+  f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int s = 0; s < sh.n; ++s) {
+    const u32x2_t ml = *(const INCVIT_GLOBAL u32x2_t*)(part + s * step + 2 * r);
+    const f32x4_t x = *(const INCVIT_GLOBAL f32x4_t*)(row + s * step);
+    const float ms = __uint_as_float(ml[0]), e = ms == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ms - m);
+    l += e * __uint_as_float(ml[1]);
+    o += x * e;
+  }
+  const float inv = 1.0f / l;
+  const int n = w.first + r, tok = n / a.group, head = h * a.group + n - tok * a.group;
+  float y[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) y[j] = m == -INFINITY ? 0.0f : o[j] * inv;
+  store_out4<T>(static_cast<T*>(const_cast<void*>(a.out.p)) + (w.q0 + tok) * a.out.row + (long)head * a.out.head + d, y);
+}
+
+template <class T, int DS>
 hipError_t launch_ds(const AttendArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((long)a.tiles * a.hk), std::min(1 << a.row_log, a.most_rows));
+  const int rows = std::min(1 << a.row_log, a.most_rows);
+  if (a.row_log > 5) {
+    constexpr int each = 256 / (DS / 4);
+    return launch_k(attend_join_rows_kernel<T, DS>, dim3((unsigned)((long)a.tiles * a.hk), (rows + each - 1) / each), dim3(256), 0, s, a);
+  }
+  const dim3 grid((unsigned)((long)a.tiles * a.hk), rows);
   return launch_k(attend_join_kernel<T, DS>, grid, dim3(256), 0, s, a);
 }
 

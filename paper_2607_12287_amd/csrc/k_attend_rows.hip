@@ -15,7 +15,7 @@ namespace {
 
 template <class T, int DS, int NT>
 __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs a) {
-  constexpr int NP = DS / 16, NC = DS / 32 + (DS % 32 != 0), RB = row_bytes<T, DS>(), EB = sizeof(T);
+  constexpr int NP = DS / 16, NC = DS / 32 + (DS % 32 != 0), RB = row_bytes<T, DS>(), VB = value_bytes<T, DS>(), EB = sizeof(T);
   constexpr int KL = rows_key_log(EB == 2, DS), KT = 1 << KL, KU = KT / 16, KS = KT / 32;
   constexpr int PER = DS / 8, NV = (KT * PER + 255) / 256;  // 8-dim pieces of a row, of a thread
   constexpr uint32_t kNowhere = 0xc0000000u;                // past every buffer's end
@@ -55,11 +55,11 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
 #pragma unroll
     for (int k = 0; k < NV; ++k) vraw[k].bload(vr, v_off[k], 0);
   };
-  auto put = [&](char* buf, const V8<T>* x) {
+  auto put = [&](char* buf, const V8<T>* x, int rb) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int e = k * 256 + tid, r = e / PER, d = (e - r * PER) * 8;
-      if (KT * PER % 256 == 0 || r < KT) *reinterpret_cast<V8<T>*>(buf + r * RB + d * EB) = x[k];
+      if (KT * PER % 256 == 0 || r < KT) *reinterpret_cast<V8<T>*>(buf + r * rb + d * EB) = x[k];
     }
   };
 
@@ -97,6 +97,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
     if (none) return;
     const bool whole = all_seen(a, w.len, p0, p1, j0, j1);
     f32x4_t s[NT][KU];
+    __builtin_amdgcn_s_setprio(1);  // products before the other waves' softmax
 #pragma unroll
     for (int u = 0; u < KU; ++u) {
 #pragma unroll
@@ -109,6 +110,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
         for (int t = 0; t < NT; ++t) mma(s[t][u], x, q[t][c]);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     V8<T> pop[NT][KS];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -155,7 +157,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
     for (int k = 0; k < NP; ++k)
 #pragma unroll
       for (int b = 0; b < KS; ++b) {
-        const V8<T> vop = value_op<T, RB>(vbuf + 32 * b * RB, 16 * k, lane);
+        const V8<T> vop = value_op<T, VB>(vbuf + 32 * b * VB, 16 * k, lane);
 #pragma unroll
         for (int t = 0; t < NT; ++t) mma(o[t][k], vop, pop[t][b]);
       }
@@ -164,11 +166,11 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
   bool odd = false;
   if (i0 < i1) load_tile(kt.at(i0));
   for (int i = i0; i < i1; ++i) {
-    char* kbuf = lds + (i & 1) * 2 * KT * RB;
+    char* kbuf = lds + (i & 1) * KT * (RB + VB);
     char* vbuf = kbuf + KT * RB;
     const int tile = kt.at(i), j0 = tile * KT, j1 = j0 + KT - 1;
-    put(kbuf, kraw);
-    put(vbuf, vraw);
+    put(kbuf, kraw, RB);
+    put(vbuf, vraw, VB);
     // whether every row of the workgroup sees all of the tile
     const bool whole = all_seen(a, w.len, kt.p0, kt.p1, j0, j1);
     if (!whole) {
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
         odd = true;
 #pragma unroll 1
         for (int e = tid; e < KT * PER; e += 256) {
-          V8<T>* at = reinterpret_cast<V8<T>*>(vbuf + e / PER * RB + e % PER * 8 * EB);
+          V8<T>* at = reinterpret_cast<V8<T>*>(vbuf + e / PER * VB + e % PER * 8 * EB);
           V8<T> x = *at;
           drop_special(x);
           *at = x;
@@ -259,7 +261,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
 
 template <class T, int DS, int NT>
 hipError_t launch_one(const AttendArgs& a, hipStream_t s) {
-  constexpr int bytes = (4 << rows_key_log(sizeof(T) == 2, DS)) * row_bytes<T, DS>();
+  constexpr int bytes = (2 << rows_key_log(sizeof(T) == 2, DS)) * (row_bytes<T, DS>() + value_bytes<T, DS>());
   static_assert(bytes <= 156 * 1024, "LDS");
   const hipError_t e = with_lds<attend_rows_kernel<T, DS, NT>>(bytes);
   if (e != hipSuccess) return e;

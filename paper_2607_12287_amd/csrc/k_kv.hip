@@ -308,8 +308,9 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvReadArgs a) {
   const long r = (long)blockIdx.x * 4 + wave;
   if (r >= a.rows) return;
   const int slot = __builtin_amdgcn_readfirstlane(gbl(a.slots)[r]);
-  if (slot < 0 || slot >= (long)a.blocks * a.block) return;
-  const int blk = slot / a.block, tok = slot - blk * a.block, n = tok & 15;
+  const bool there = slot >= 0 && slot < (long)a.blocks * a.block;
+  if (!there && !a.fill) return;
+  const int blk = there ? slot / a.block : 0, tok = there ? slot - blk * a.block : 0, n = tok & 15;
   const KvLayout lay(a.blocks, a.block, a.heads, a.d);
   const char* base = a.cache + a.data + (size_t)blk * a.heads * lay.head_bytes + (size_t)(tok >> 4) * (16 * lay.ds);
   const float* scales = reinterpret_cast<const float*>(a.cache) + (long)blk * a.heads * 2;
@@ -329,8 +330,8 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvReadArgs a) {
     float y[8], z[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      y[i] = (float)(int8_t)(k[i >> 2] >> (8 * (i & 3))) * ks;
-      z[i] = (float)(int8_t)((i < 4 ? v0[i & 3] : v1[i & 3]) >> (8 * (n & 3))) * vs;
+      y[i] = there ? (float)(int8_t)(k[i >> 2] >> (8 * (i & 3))) * ks : 0.0f;
+      z[i] = there ? (float)(int8_t)((i < 4 ? v0[i & 3] : v1[i & 3]) >> (8 * (n & 3))) * vs : 0.0f;
     }
     T* kd = ko + (long)h * a.x[0].head + d;
     T* vd = vo + (long)h * a.x[1].head + d;

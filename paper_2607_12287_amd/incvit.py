@@ -151,7 +151,7 @@ def lib() -> ctypes.CDLL:
             "incvit_qlinear": (I32, [I32, I64, I32, I32, P, I64, P, I32, P, I64, P, I64, P, P]),
             "incvit_kv_bytes": (S, [P]),
             "incvit_kv_write": (I32, [P, I32, I64, P, I64, I64, P, I64, I64, P, I32, P, P]),
-            "incvit_kv_read": (I32, [P, P, I32, I64, P, P, I64, I64, P, I64, I64, P]),
+            "incvit_kv_read": (I32, [P, P, I32, I64, P, I32, P, I64, I64, P, I64, I64, P]),
             "incvit_attention_workspace_bytes": (S, [P, I32, I32, I64, I32, I64]),
             "incvit_kv_attend": (I32, [P, P, P, I32, I64, P, P, I64, I32, P, I64, P, P, P, P]),
             "incvit_attend": (I32, [P, I32, I64, P, I64, P, I64, P, P, P, P, P, P]),
@@ -347,9 +347,9 @@ def incvit_kv_write(c: incvit_kv, dtype: int, rows: int, k: int, k_row: int, k_h
     return lib().incvit_kv_write(_addr(c), dtype, rows, k, k_row, k_head, v, v_row, v_head, slots, begin, cache, stream)
 
 
-def incvit_kv_read(c: incvit_kv, cache: int, dtype: int, rows: int, slots: int, k: int, k_row: int, k_head: int, v: int,
-                   v_row: int, v_head: int, stream: int = 0) -> int:
-    return lib().incvit_kv_read(_addr(c), cache, dtype, rows, slots, k, k_row, k_head, v, v_row, v_head, stream)
+def incvit_kv_read(c: incvit_kv, cache: int, dtype: int, rows: int, slots: int, fill: int, k: int, k_row: int, k_head: int,
+                   v: int, v_row: int, v_head: int, stream: int = 0) -> int:
+    return lib().incvit_kv_read(_addr(c), cache, dtype, rows, slots, fill, k, k_row, k_head, v, v_row, v_head, stream)
 
 
 def incvit_attention_workspace_bytes(a: incvit_attention, cached: int, n: int, rows: int, ragged: int, max_len: int) -> int:

@@ -354,14 +354,16 @@ class KVCache:
         tensor and is zeros in a new one."""
         if (k_out is None) != (v_out is None):
             raise ValueError("k_out and v_out: both or neither")
-        if k_out is None:
-            if dtype not in (_BF16, _F32):
+        new = k_out is None
+        if new:
+            if dtype is not _BF16 and dtype is not _F32:
                 raise ValueError("dtype: fp32 or bf16")
-            k_out, v_out = torch.zeros(2, slots.shape[0], self.heads, self.head_dim, dtype=dtype, device=self.device).unbind(0)
+            shape = (slots.shape[0], self.heads, self.head_dim)
+            k_out, v_out = torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device)
         code = self._sides(k_out, v_out)
         rows = k_out.shape[0]
         at = _indexes(slots, rows, self.device, "slots")
-        _call(_c.lib().incvit_kv_read, self.device, self.config, self.buf.data_ptr(), code, rows, at, k_out.data_ptr(),
+        _call(_c.lib().incvit_kv_read, self.device, self.config, self.buf.data_ptr(), code, rows, at, new, k_out.data_ptr(),
               k_out.stride(0), k_out.stride(1), v_out.data_ptr(), v_out.stride(0), v_out.stride(1))
         return k_out, v_out
 

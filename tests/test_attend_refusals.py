@@ -27,7 +27,7 @@ def test_caches_out_of_range(kw):
     c = kv(**kw)
     assert incvit.incvit_kv_bytes(c) == 0
     assert incvit.incvit_kv_write(c, 1, 1, A, 256, 64, B, 256, 64, C, 0, D) == UNSUPPORTED
-    assert incvit.incvit_kv_read(c, D, 1, 1, C, A, 256, 64, B, 256, 64) == UNSUPPORTED
+    assert incvit.incvit_kv_read(c, D, 1, 1, C, 0, A, 256, 64, B, 256, 64) == UNSUPPORTED
     assert "cache" in incvit.incvit_last_error()
 
 
@@ -54,20 +54,21 @@ def test_rows_of_the_cache(kw, status):
     write = list(d.values())
     assert incvit.incvit_kv_write(kv(), *write) == status
     begin, cache = d.pop("begin"), d.pop("cache")
-    assert incvit.incvit_kv_read(kv(), cache, d["dtype"], d["rows"], d["slots"], *[d[x] for x in ("k", "k_row", "k_head", "v", "v_row", "v_head")]) == status
+    assert incvit.incvit_kv_read(kv(), cache, d["dtype"], d["rows"], d["slots"], 0, *[d[x] for x in ("k", "k_row", "k_head", "v", "v_row", "v_head")]) == status
     assert incvit.incvit_last_error() != ""
 
 
 def test_cache_calls():
     w, r = incvit.incvit_kv_write, incvit.incvit_kv_read
     assert w(kv(), *{**OK_ROWS, "begin": 2}.values()) == ARG and w(kv(), *{**OK_ROWS, "begin": -1}.values()) == ARG
-    assert w(None, *OK_ROWS.values()) == ARG and r(None, D, 1, 5, C, A, 256, 64, B, 256, 64) == ARG
+    assert w(None, *OK_ROWS.values()) == ARG and r(None, D, 1, 5, C, 0, A, 256, 64, B, 256, 64) == ARG
+    assert r(kv(), D, 1, 5, C, 2, A, 256, 64, B, 256, 64) == ARG and r(kv(), D, 1, 5, C, -1, A, 256, 64, B, 256, 64) == ARG
     # heads of the output that overlap
     for k_row, k_head in ((0, 64), (256, 0), (256, 56), (248, 64), (64, 64)):
-        assert r(kv(), D, 1, 5, C, A, k_row, k_head, B, 256, 64) == SHAPE
-        assert r(kv(), D, 1, 5, C, A, 256, 64, B, k_row, k_head) == SHAPE
+        assert r(kv(), D, 1, 5, C, 0, A, k_row, k_head, B, 256, 64) == SHAPE
+        assert r(kv(), D, 1, 5, C, 0, A, 256, 64, B, k_row, k_head) == SHAPE
     # nothing to do: nothing is looked at or enqueued
-    assert w(kv(), 1, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0) == OK and r(kv(), 0, 1, 0, 0, 0, 0, 0, 0, 0, 0) == OK
+    assert w(kv(), 1, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0) == OK and r(kv(), 0, 1, 0, 0, 0, 0, 0, 0, 0, 0, 0) == OK
 
 
 def attention(**kw):
@@ -138,7 +139,7 @@ def test_what_the_plain_attention_refuses():
 def test_workspaces():
     f = incvit.incvit_attention_workspace_bytes
     a = attention()
-    assert f(a, 1, 1, 1, 0, 100) == 0 and f(a, 1, 4096, 4096, 0, 10 ** 6) == 0  # one workgroup's keys; rows enough
+    assert f(a, 1, 1, 1, 0, 1024) == 0 and f(a, 1, 4096, 4096, 0, 10 ** 6) == 0  # one workgroup's keys; rows enough
     assert f(a, 1, 1, 1, 0, 10 ** 5) > f(a, 1, 1, 1, 0, 10 ** 4) > 0
     assert f(a, 0, 1, 1, 0, 10 ** 5) > 0
     assert f(attention(window=512), 1, 1, 1, 0, 10 ** 9) == f(attention(window=512), 1, 1, 1, 0, 10 ** 5)

@@ -252,6 +252,24 @@ def test_large_scores(kind, dtype):
     run(kind, [2000], [1], 2, 1, 64, dtype, scale=1e-6)
 
 
+@pytest.mark.parametrize("nq", [1, 5, 100])
+@types
+def test_scales_far_from_one(dtype, nq):
+    """Blocks of keys and values of very different sizes, zeros among them: each weight keeps its place in the sum."""
+    n, d = 200, 64
+    k, v = randn(n, 1, d, dtype=dtype, seed=1), randn(n, 1, d, dtype=dtype, seed=2)
+    sizes = torch.tensor([1.0, 1e-30, 1e30, 0.0, 1e-38, 3e-3], device="cuda")[torch.arange(n, device="cuda") // 16 % 6, None, None]
+    k2 = (k.float() * sizes.clamp(max=3.0)).to(k.dtype)
+    for x in (Cached([n], 1, d, dtype, k=k, v=(v.float() * sizes).to(v.dtype)), Cached([n], 1, d, dtype, k=k2, v=v)):
+        q = randn(nq, 2, d, dtype=dtype, seed=3)
+        compare(x.attend(q, causal=False), x, q, [nq], causal=False)
+    # values without the huge ones: the others are not lost behind them
+    sizes = sizes.clamp(max=1.0)
+    x = Cached([n], 1, d, dtype, k=k, v=(v.float() * sizes).to(v.dtype))
+    q = randn(nq, 2, d, dtype=dtype, seed=3)
+    compare(x.attend(q, window=9), x, q, [nq], window=9)
+
+
 @both
 @types
 def test_strides(kind, dtype):
