@@ -541,8 +541,9 @@ typedef struct {
 } incvit_attention;
 
 /* Rows of heads: head h of row r starts at element r * row + h * head of p, its
- * values lie one after another; strides in [0, 2^40] elements.  p and strides are
- * 16-byte aligned.  Heads of an output must not overlap. */
+ * values lie one after another; strides in [0, 2^40] elements (rows of given keys
+ * and values: 2^23).  p and strides are 16-byte aligned.  Heads of an output must not
+ * overlap; it may be the queries, with their strides, and shares nothing else. */
 typedef struct {
   const void* p;
   int64_t row, head;

@@ -99,10 +99,13 @@ struct AttendArgs {
 // 16-row tiles of a workgroup over the cache, at most: as many as the registers hold.
 constexpr int most_row_tiles(bool bf16, int ds) { return ds <= (bf16 ? 192 : 128) ? 2 : 1; }
 
-// 16-row tiles of a wave of its own rows, at most; keys of a tile there
+// 16-row tiles of a wave of its own rows, at most (fp32 with two takes all registers
+// of a SIMD for one wave: a prompt of 2048 and heads of 128 295 us against 226); keys
+// of a tile there: 64, or 32 in fp32 where two workgroups then fit a CU's LDS (8192
+// keys, window 500, heads of 64: 181 us with 64, 160 with 32; heads of 128: 182, 227)
 constexpr int most_wave_tiles(bool bf16, int ds) { return bf16 ? 2 : 1; }
-constexpr int most_cached_wave_tiles(int ds) { return ds <= 128 ? 2 : 1; }
-constexpr int rows_key_log(bool bf16, int ds) { return ds * (bf16 ? 2 : 4) <= 512 ? 6 : 5; }
+constexpr int cached_wave_tiles(int ds) { return ds <= 128 ? 2 : 1; }
+constexpr int rows_key_log(bool bf16, int ds) { return bf16 || ds == 128 ? 6 : 5; }
 
 struct AttendPlan {
   int by_rows;         // the waves have rows of their own (else keys)
@@ -117,7 +120,7 @@ AttendPlan attend_plan(const incvit_attention& a, bool cached, long n, long rows
 
 hipError_t launch_kv_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
-hipError_t launch_kv_attend_rows(const AttendArgs& a, const AttendPlan& p, hipStream_t s);
+hipError_t launch_kv_attend_rows(const AttendArgs& a, hipStream_t s);
 hipError_t launch_attend_rows(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
 hipError_t launch_attend_join(const AttendArgs& a, int dtype, hipStream_t s);
 
@@ -424,12 +427,12 @@ __device__ __forceinline__ float soft_step(const float* x, float& m, float& l, f
   return alpha;
 }
 
-// `bytes` of dynamic LDS for kernel F on the current device: above 64 KB they are
-// asked for once on each.
+// `bytes` of dynamic LDS for kernel F on the current device: where they may be more
+// than 64 KB with what the kernel has itself, they are asked for once on each.
 template <auto F>
 hipError_t with_lds(int bytes) {
   static std::atomic<bool> done[kMaxDevices];
-  if (bytes <= 65536) return hipSuccess;
+  if (bytes <= 60 * 1024) return hipSuccess;
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess || (dev >= 0 && dev < kMaxDevices && done[dev])) return e;
@@ -444,6 +447,9 @@ __device__ __forceinline__ void store_out4(T* dst, const float* v) {
   else *(INCVIT_GLOBAL f32x4_t*)dst = f32x4_t{v[0], v[1], v[2], v[3]};
 }
 
+// The lane, counted anew: nothing that holds it has to live through a loop.
+__device__ __forceinline__ int lane_now() { return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)); }
+
 // LDS of the exchange between a workgroup's waves: m, l, then O
 template <int DS, int NT>
 constexpr int exchange_bytes() {
@@ -454,14 +460,14 @@ constexpr int exchange_bytes() {
 // [wave][row], O [wave][row][DS + 4]), and stores rows below `rows`: the result
 // where the tile's keys are one workgroup's, else the partial result.
 template <class T, int DS, int NT>
-__device__ __forceinline__ void join_waves(const AttendArgs& a, const RowTile& w, const Share& sh, const char* lds, int h) {
+__device__ __forceinline__ void join_waves(const AttendArgs& a, const RowTile& w, const Share& sh, const char* lds, int h, int tid) {
   constexpr int TR = 16 * NT;
   const float* s_m = reinterpret_cast<const float*>(lds);
   const float* s_l = s_m + kKeyWaves * TR;
   const float* s_o = s_l + kKeyWaves * TR;
   const int rows = min(TR, w.q_len * a.group - w.first);
   float* part = a.parts + (size_t)(sh.slot * a.hk + h) * TR * (DS + 2);
-  for (int i = threadIdx.x; i < rows * (DS / 4); i += 64 * kKeyWaves) {
+  for (int i = tid; i < rows * (DS / 4); i += 64 * kKeyWaves) {
     const int r = i / (DS / 4), d = (i - r * (DS / 4)) * 4;
     float m = -INFINITY;
 #pragma unroll

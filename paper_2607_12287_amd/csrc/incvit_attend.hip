@@ -128,7 +128,7 @@ AttendPlan incvit::attend_plan(const incvit_attention& a, bool cached, long n, l
   p.key_log = 5;
   if (each > (cached ? 64 : 32) && (bf16 || !cached)) {
     p.by_rows = 1;
-    p.nt = std::min(cached ? most_cached_wave_tiles(ds) : most_wave_tiles(bf16, ds), each <= 64 ? 1 : 2);
+    p.nt = cached ? cached_wave_tiles(ds) : std::min(most_wave_tiles(bf16, ds), each <= 64 ? 1 : 2);
     p.row_log = 5 + p.nt;
     p.key_log = cached ? 6 : rows_key_log(bf16, ds);
   } else {
@@ -258,7 +258,7 @@ incvit_status incvit_kv_attend(const incvit_attention* a, const incvit_kv* c, co
   r.blocks = c->blocks;
   r.lb = lay.lb;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if ((st = launched(p.by_rows ? launch_kv_attend_rows(r, p, s) : launch_kv_attend(r, p, a->dtype, s), "kv_attend")) != INCVIT_OK) return st;
+  if ((st = launched(p.by_rows ? launch_kv_attend_rows(r, s) : launch_kv_attend(r, p, a->dtype, s), "kv_attend")) != INCVIT_OK) return st;
   return launched(launch_attend_join(r, a->dtype, s), "kv_attend");
 }
 
@@ -279,6 +279,8 @@ incvit_status incvit_attend(const incvit_attention* a, int32_t n, int64_t rows, 
   if (key_rows > 0) {
     if ((st = check_rows(a->dtype, k->p, k->row, k->head, "k")) != INCVIT_OK) return st;
     if ((st = check_rows(a->dtype, v->p, v->row, v->head, "v")) != INCVIT_OK) return st;
+    // a tile's rows are addressed with 31 bits
+    if (k->row > (1 << 23) || v->row > (1 << 23)) return op_fail(INCVIT_ERR_UNSUPPORTED, "rows of keys and values more than 2^23 elements apart");
   }
   if (!apart(rows, out->row, a->q_heads, out->head, a->head_dim)) return op_fail(INCVIT_ERR_SHAPE, "heads of the output overlap");
   const AttendPlan p = attend_plan(*a, false, n, (long)rows, q_start != nullptr, max_len ? (long)max_len : (long)((key_rows + n - 1) / n));

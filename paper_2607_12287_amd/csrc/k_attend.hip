@@ -192,7 +192,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
     for (int k = 0; k < NP; ++k) *reinterpret_cast<f32x4_t*>(s_o + (size_t)r * (DS + 4) + 16 * k + 4 * g) = o[t][k];
   }
   __syncthreads();
-  join_waves<T, DS, NT>(a, w, sh, lds, h);
+  join_waves<T, DS, NT>(a, w, sh, lds, h, threadIdx.x);
 }
 
 template <class T, int DS, int NT>

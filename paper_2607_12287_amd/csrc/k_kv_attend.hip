@@ -52,7 +52,7 @@ struct RawTile {
 
 // Three workgroups to a CU where the registers allow it without spills.
 template <class T, int DS, int NT>
-constexpr int kPerCu = NT == 1 && DS <= (sizeof(T) == 2 ? 128 : 80) ? 3 : 1;
+constexpr int kPerCu = NT == 1 && DS <= (sizeof(T) == 2 ? 128 : 64) ? 3 : 1;
 
 template <class T, int DS, int NT>
 __global__ __launch_bounds__(64 * kKeyWaves, (kPerCu<T, DS, NT>)) void kv_attend_kernel(AttendArgs a) {
@@ -188,6 +188,7 @@ __global__ __launch_bounds__(64 * kKeyWaves, (kPerCu<T, DS, NT>)) void kv_attend
         for (int k = 0; k < NP; ++k) o[t][k] *= alpha;
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
       const uint4 vop = bf_of_i8x8(x.v[0][k], x.v[1][k]);
@@ -223,6 +224,7 @@ __global__ __launch_bounds__(64 * kKeyWaves, (kPerCu<T, DS, NT>)) void kv_attend
     }
   }
 
+  const int at = lane_now();
   float* s_m = reinterpret_cast<float*>(lds);
   float* s_l = s_m + kKeyWaves * TR;
   float* s_o = s_l + kKeyWaves * TR;
@@ -230,8 +232,8 @@ __global__ __launch_bounds__(64 * kKeyWaves, (kPerCu<T, DS, NT>)) void kv_attend
   for (int t = 0; t < NT; ++t) {
     const float sum = group4_sum(l[t]);
     const bool any = group4_max(seen[t] ? 1.0f : 0.0f) > 0.0f;
-    const int r = wave * TR + 16 * t + n;
-    if (g == 0) {
+    const int r = wave * TR + 16 * t + (at & 15);
+    if (at < 16) {
       s_m[r] = m[t] == -INFINITY && any ? kNoMax : m[t];
       s_l[r] = sum;
     }
@@ -240,11 +242,11 @@ __global__ __launch_bounds__(64 * kKeyWaves, (kPerCu<T, DS, NT>)) void kv_attend
     for (int k = 0; k < NP; ++k) {
       const int c = k >> 2, P = TAIL != 0 && c == NC - 1 ? TAIL : 4;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s_o[(size_t)r * (DS + 4) + 64 * c + P * (4 * g + j) + (k & 3)] = o[t][k][j];
+      for (int j = 0; j < 4; ++j) s_o[(size_t)r * (DS + 4) + 64 * c + P * (4 * (at >> 4) + j) + (k & 3)] = o[t][k][j];
     }
   }
   __syncthreads();
-  join_waves<T, DS, NT>(a, w, sh, lds, h);
+  join_waves<T, DS, NT>(a, w, sh, lds, h, wave * 64 + at);
 }
 
 template <class T, int DS, int NT>

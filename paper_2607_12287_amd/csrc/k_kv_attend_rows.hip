@@ -292,34 +292,26 @@ __global__ __launch_bounds__(64 * kKeyWaves) void kv_attend_rows_kernel(AttendAr
   }
 }
 
-template <int DS, int NT>
+template <int DS>
 hipError_t launch_one(const AttendArgs& a, hipStream_t s) {
-  constexpr int NP = DS / 16, NC = (NP + 3) / 4, bytes = 2 * (8 * NC + 2 * NP) * 1024;
+  constexpr int NT = cached_wave_tiles(DS), NP = DS / 16, NC = (NP + 3) / 4, bytes = 2 * (8 * NC + 2 * NP) * 1024;
   static_assert(bytes <= 156 * 1024 && bytes >= 64 * (DS * 2 + 16), "LDS");
   const hipError_t e = with_lds<kv_attend_rows_kernel<DS, NT>>(bytes);
   if (e != hipSuccess) return e;
   return launch_k(kv_attend_rows_kernel<DS, NT>, dim3((unsigned)(a.shares * a.hk)), dim3(64 * kKeyWaves), (size_t)bytes, s, a);
 }
 
-template <int DS>
-hipError_t launch_ds(const AttendArgs& a, int nt, hipStream_t s) {
-  if constexpr (most_cached_wave_tiles(DS) > 1) {
-    if (nt == 2) return launch_one<DS, 2>(a, s);
-  }
-  return launch_one<DS, 1>(a, s);
-}
-
 }  // namespace
 
-hipError_t launch_kv_attend_rows(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
+hipError_t launch_kv_attend_rows(const AttendArgs& a, hipStream_t s) {
   switch (kv_dims(a.d)) {
-    case 32: return launch_ds<32>(a, p.nt, s);
-    case 64: return launch_ds<64>(a, p.nt, s);
-    case 80: return launch_ds<80>(a, p.nt, s);
-    case 96: return launch_ds<96>(a, p.nt, s);
-    case 128: return launch_ds<128>(a, p.nt, s);
-    case 192: return launch_ds<192>(a, p.nt, s);
-    default: return launch_ds<256>(a, p.nt, s);
+    case 32: return launch_one<32>(a, s);
+    case 64: return launch_one<64>(a, s);
+    case 80: return launch_one<80>(a, s);
+    case 96: return launch_one<96>(a, s);
+    case 128: return launch_one<128>(a, s);
+    case 192: return launch_one<192>(a, s);
+    default: return launch_one<256>(a, s);
   }
 }
 

@@ -285,6 +285,52 @@ def test_strides(kind, dtype):
     assert torch.equal(heads_first[..., 8:].transpose(0, 1), want) and (heads_first[..., :8] == 7).all()
 
 
+@both
+@types
+@pytest.mark.parametrize("new", [[1, 1], [40, 90]])
+def test_the_output_may_be_the_queries(kind, dtype, new):
+    x = KINDS[kind]([3000, 200], 2, 64, dtype)
+    q = randn(sum(new), 4, 64, dtype=dtype)
+    want = x.attend(q, q_start=starts(new))
+    same = x.attend(q, q_start=starts(new), out=q)
+    assert same is q and torch.equal(q, want)
+
+
+@both
+def test_keys_that_all_sequences_share(kind):
+    """The same blocks in every row of the table; rows without a stride."""
+    x = Cached([333], 2, 64)
+    q = randn(4, 4, 64)
+    if kind == "cached":
+        got = x.cache.attend(q, x.table.expand(4, -1), x.lens.expand(4).contiguous())
+        want, bound = kv_ref.attention(q, x.k[0], x.v[0], torch.ones(4, 333, dtype=torch.bool, device="cuda"))
+    else:
+        k = randn(1, 2, 64, seed=1).expand(100, -1, -1)
+        q = randn(300, 4, 64)
+        got = incvit.attend(q, k, k, causal=False)
+        want, bound = kv_ref.attention(q, k, k, torch.ones(300, 100, dtype=torch.bool, device="cuda"))
+    kv_ref.check(got, want, bound)
+
+
+def test_a_cache_past_4_gib():
+    """Blocks whose bytes, and whose scales' numbers, lie past 32 bits."""
+    blocks, hk, d = 400000, 4, 128
+    c = incvit.KVCache(blocks, hk, d)
+    assert c.buf.numel() > 2 ** 32 + 2 ** 30
+    k, v, n = randn(100, hk, d, seed=1), randn(100, hk, d, seed=2), 100
+    table = torch.tensor([[blocks - 1, 3, blocks - 7, 262144, blocks - 2, 262143, 0]], dtype=torch.int32, device="cuda")
+    slots = (table[0].long()[torch.arange(n, device="cuda") // 16] * 16 + torch.arange(n, device="cuda") % 16).int()
+    c.write(k, v, slots, begin=True)
+    small = Cached([n], hk, d, k=k, v=v)
+    got = c.read(slots, dtype=torch.float32)
+    for y, want in zip(got, (small.k[0], small.v[0])):
+        assert torch.equal(y.double(), want.float().double())
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    for nq in (1, 30, 70):
+        q = randn(nq, 8, d)
+        assert torch.equal(c.attend(q, table, lens), small.attend(q))
+
+
 def test_blocks_outside_the_pool_are_not_seen():
     lens, d = [100, 100], 64
     x = Cached(lens, 1, d)
