@@ -138,9 +138,9 @@ struct RowTile {
 };
 
 // The tile number f of the launch.  Ragged: sequence i's tiles count from
-// floor(q_start[i] * group / rows of a tile) + i on, which leaves each enough numbers, so a
-// wave finds the sequence by counting the starts up to f, 64 at a time.  Whatever
-// the starts hold, the rows are within the call's.
+// floor(q_start[i] * group / rows of a tile) + i on, which leaves each enough numbers,
+// and a wave counts the starts up to f by a search over 64 of them at a time.
+// Whatever the starts hold, the rows are within the call's.
 __device__ __forceinline__ bool row_tile(const AttendArgs& a, int f, RowTile& w) {
   const int log = a.row_log;
   if (!a.q_start) {
@@ -150,13 +150,14 @@ __device__ __forceinline__ bool row_tile(const AttendArgs& a, int f, RowTile& w)
     w.q0 = (long)w.seq * a.q_len;
   } else {
     const int lane = threadIdx.x & 63;
-    const int n = a.n + a.fill;
-    int count = 0;
-    for (int i = 0; i < n; i += 64) {
-      const int j = min(i + lane, n - 1);
-      const long at = min(max((long)gbl(a.q_start)[j], 0L), a.rows);
-      const bool up = i + lane < n && ((at * a.group) >> log) + j <= f;
-      count += __popcll(__ballot(up));
+    int count = 0;  // starts up to f: `left` ones from `count` on are open
+    for (int left = a.n + a.fill; left > 0;) {
+      const int step = (left + 63) / 64, j = count + lane * step;
+      const long at = min(max((long)gbl(a.q_start)[min(j, a.n)], 0L), a.rows);
+      const int up = __popcll(__ballot((lane * step < left) & (((at * a.group) >> log) + j <= f)));
+      if (up == 0) break;
+      count += (up - 1) * step + 1;
+      left = min(step - 1, left - (up - 1) * step - 1);
     }
     if (count == 0) return false;
     w.seq = __builtin_amdgcn_readfirstlane(count - 1);
@@ -255,7 +256,7 @@ __device__ __forceinline__ bool even_share(const AttendArgs& a, int want, Share&
   RowTile w;
   w.seq = min(lane, a.tiles - 1);
   const int len = seq_len(a, w), nt = in ? key_tiles(a, len, len - a.q_len, len - 1).nt : 0;
-  const int total = __builtin_amdgcn_readlane(lanes_scan(nt), 63), chunk = max(a.chunk, (total + a.even - 1) / a.even);
+  const int total = __builtin_amdgcn_readlane(lanes_scan(min(nt, 1 << 24)), 63), chunk = max(a.chunk, (total + a.even - 1) / a.even);
   const int n = in ? max(1, min(kMostShares, (nt + chunk - 1) / chunk)) : 0, upto = lanes_scan(n);
   const uint64_t there = __ballot(TILE ? lane == want : in & (upto > want));
   if (!there) return false;

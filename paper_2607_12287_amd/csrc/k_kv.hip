@@ -244,7 +244,7 @@ __device__ __forceinline__ void write_block(const KvWriteArgs& a, int* map, uint
   const int np = lay.ds / 16;
   float* scale = reinterpret_cast<float*>(a.cache) + ((long)blk * a.heads + h) * 2 + side;
   char* dst = a.cache + a.data + ((size_t)blk * a.heads + h) * lay.head_bytes + (side ? (size_t)B * lay.ds : 0) + (size_t)wave * (16 * lay.ds);
-  const float before = *gbl(scale);
+  float before = *gbl(scale);
   Group<NPC> q;
   const bool here = W == 1 || __any(map[16 * wave + (lane & 15)] >= 0);  // new rows in the wave's group
   uint32_t top = 0;  // the largest magnitude as bits, which order like it, NaN on top
@@ -259,7 +259,8 @@ __device__ __forceinline__ void write_block(const KvWriteArgs& a, int* map, uint
   }
   if constexpr (W > 1) {
     if (lane == 0) tops[wave] = top;
-    __syncthreads();  // also: every wave has the old scale
+    asm volatile("" : "+v"(before));  // every wave has the old scale before one writes the new
+    __syncthreads();
 #pragma unroll
     for (int k = 0; k < W; ++k) top = max(top, tops[k]);
   }

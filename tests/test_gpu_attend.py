@@ -22,6 +22,10 @@ def starts(lens):
     return torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32, device="cuda")
 
 
+def starts_of(lens):
+    return torch.tensor([0] + torch.tensor(lens).cumsum(0).tolist(), dtype=torch.int32, device="cuda")
+
+
 class Cached:
     """Sequences in a pool of shuffled blocks, and the values that the cache holds for them in 64 bits."""
 
@@ -157,6 +161,17 @@ def test_many_sequences(kind):
     lens = [1 + (37 * i) % 90 for i in range(200)]
     new = [0 if i % 5 == 3 else 1 + i % min(m, 7) for i, m in enumerate(lens)]
     run(kind, lens, new, 4, 2, 32)
+
+
+@pytest.mark.parametrize("n", [63, 64, 65, 4096, 4097, 6000])
+def test_thousands_of_sequences(n):
+    """Starts that a wave searches in one, two and three steps: each sequence's only key gives its value back."""
+    new = [0 if i % 7 == 3 else 1 + i % 3 for i in range(n)]
+    v = torch.arange(n, device="cuda").float()[:, None, None].expand(n, 1, 32).contiguous()
+    q = torch.zeros(sum(new), 1, 32, device="cuda")
+    got = incvit.attend(q, v, v, q_start=starts_of(new), k_start=starts_of([1] * n), causal=False)
+    want = torch.repeat_interleave(torch.arange(n, device="cuda"), torch.tensor(new, device="cuda")).float()
+    assert torch.equal(got, want[:, None, None].expand_as(got))
 
 
 @both
