@@ -169,6 +169,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
     char* kbuf = lds + (i & 1) * KT * (RB + VB);
     char* vbuf = kbuf + KT * RB;
     const int tile = kt.at(i), j0 = tile * KT, j1 = j0 + KT - 1;
+    __builtin_amdgcn_s_setprio(2);  // what a whole workgroup waits for goes first
     put(kbuf, kraw, RB);
     put(vbuf, vraw, VB);
     // whether every row of the workgroup sees all of the tile
@@ -181,6 +182,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_rows_kernel(AttendArgs 
       if (lane == 0) s_special[i & 1][wave] = any;
     }
     if (i + 1 < i1) load_tile(kt.at(i + 1));
+    __builtin_amdgcn_s_setprio(0);
     __syncthreads();
     if (!whole) {
       bool here = false;

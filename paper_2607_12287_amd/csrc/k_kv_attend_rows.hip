@@ -233,8 +233,10 @@ __global__ __launch_bounds__(64 * kKeyWaves) void kv_attend_rows_kernel(AttendAr
   if (i0 < i1) load_group(i0);
   for (int i = i0; i < i1; ++i) {
     char* kbuf = lds + (i & 1) * (KB + VB);
+    __builtin_amdgcn_s_setprio(2);  // what a whole workgroup waits for goes first
     put_group(kbuf, kbuf + KB, i & 1);
     if (i + 1 < i1) load_group(i + 1);
+    __builtin_amdgcn_s_setprio(0);
     __syncthreads();
     work(kbuf, kbuf + KB, kt.at(i), i & 1);
   }
