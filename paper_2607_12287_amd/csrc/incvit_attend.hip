@@ -10,8 +10,28 @@ using namespace incvit;
 namespace {
 
 // Workgroups of a call that shares keys, where waves have keys and where they have
-// rows, and the key tiles of one at least.
+// rows, and the key tiles of one at least.  16 sequences over 76 k keys, heads of 128
+// (cached): 39, 38, 37, 35 us with 512, 768, 1024, 1536.
 constexpr long kWant = 1536, kWantRows = 512, kLeast = 16, kLeastRows = 8;
+
+// Rows times query heads of a call, up to which waves share keys for longer sequences
+// (a workgroup of waves with rows takes four times the rows, and so leaves the chip
+// idle sooner).  Measured, us, heads of 64 in groups of 4, waves with keys | rows.
+// 8192 keys of one sequence, 4 key heads, 16 rows: 15 | 26 cached, 15 | 19 plain; 32
+// rows: 16 | 27, 18 | 24; 64 rows: 21 | 29, 27 | 26.  16 sequences of 2048 keys, 4, 8,
+// 16, 24 rows: cached 15 | 24, 19 | 25, 26 | 27, 35 | 29; plain 21 | 20, 31 | 21,
+// 28 | 25, 29 | 28.
+constexpr long kFewRows = 1024;
+
+// Rows times query heads, up to which a wave has one tile of 16 rows and not two, so
+// that there are more workgroups: twice as many up to 128 dims, where two fit a CU's
+// LDS.  Only for sequences of enough rows, which do not wait for memory, and whose
+// keys are not shared anyway.  Measured, 16 heads in groups of 4, one tile | two, us: a
+// prompt of 2048 rows and heads of 64 37 | 49, 128 60 | 68, 256 106 | 135 (with a window
+// of 512 64 | 54); 1024 rows of 256 50 | 73; of 4096 rows, 128: 137 | 136, 6000: 288 | 216.
+// 64 sequences of 24 rows and 1024 keys, 128: 74 | 46; 512 rows, 8192 keys: 76 | 59.
+constexpr long kOneTileRows = 16384, kOneTileEach = 256;
+
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 
 bool is_dtype(int32_t t) { return t == INCVIT_F32 || t == INCVIT_BF16; }
@@ -116,19 +136,18 @@ AttendArgs attend_args(const incvit_attention& a, const AttendPlan& p, int32_t n
   return r;
 }
 
-}  // namespace
-
 // Rows of a workgroup by those of a sequence; then, where the row tiles alone
 // leave the chip idle, the keys of each are shared by several workgroups.
-AttendPlan incvit::attend_plan(const incvit_attention& a, bool cached, long n, long rows, bool ragged, long max_len) {
+AttendPlan plan_with(const incvit_attention& a, bool cached, long n, long rows, bool ragged, long max_len, int most) {
   AttendPlan p = {};
   const bool bf16 = a.dtype == INCVIT_BF16;
   const long group = a.q_heads / a.kv_heads, each = (rows + n - 1) / n * group;
   const int ds = kv_dims(a.head_dim);
   p.key_log = 5;
-  if (each > (cached ? 64 : 32) && (bf16 || !cached)) {
+  const long all = rows * a.q_heads;
+  if (each > (cached ? (all <= kFewRows ? 256 : 64) : bf16 ? (all <= kFewRows / 2 ? 128 : 16) : 32) && (bf16 || !cached)) {
     p.by_rows = 1;
-    p.nt = cached ? cached_wave_tiles(ds) : std::min(most_wave_tiles(bf16, ds), each <= 64 ? 1 : 2);
+    p.nt = cached ? cached_wave_tiles(ds) : std::min(most_wave_tiles(bf16, ds), each <= 64 ? 1 : most);
     p.row_log = 5 + p.nt;
     p.key_log = cached ? 6 : rows_key_log(bf16, ds);
   } else {
@@ -158,6 +177,16 @@ AttendPlan incvit::attend_plan(const incvit_attention& a, bool cached, long n, l
   }
   if (p.splits > 1 || p.even) p.bytes = (size_t)p.shares * a.kv_heads * tr * (ds + 2) * 4;
   return p;
+}
+
+}  // namespace
+
+AttendPlan incvit::attend_plan(const incvit_attention& a, bool cached, long n, long rows, bool ragged, long max_len) {
+  const AttendPlan p = plan_with(a, cached, n, rows, ragged, max_len, 2);
+  const bool few = rows * a.q_heads <= (kv_dims(a.head_dim) <= 128 ? 2 : 1) * kOneTileRows;
+  const long each = (rows + n - 1) / n * (a.q_heads / a.kv_heads);
+  if (cached || !p.by_rows || p.splits > 1 || !few || each < kOneTileEach) return p;
+  return plan_with(a, cached, n, rows, ragged, max_len, 1);
 }
 
 extern "C" {

@@ -73,10 +73,11 @@ def gpu_test_calls():
             for block in (16, 32, 64, 128):
                 yield dict(op="write", d=d, hk=2, dtype=dt, rows=2 * block + block // 2 + 3, block=block)
             yield dict(op="read", d=d, hk=2, dtype=dt, rows=80)
+            yield dict(op="plain", d=d, hk=1, hq=4, dtype=1, n=3, rows=8462, keys=8192, ragged=1)
             for op in ("cached", "plain"):
                 for nq in (1, 5, 9, 70):
                     yield dict(op=op, d=d, hk=1, hq=4, dtype=dt, n=2, rows=2 * nq, keys=99)
-                for nq in (1, 30):  # keys shared by workgroups
+                for nq in (1, 30, 150):  # keys shared by workgroups
                     yield dict(op=op, d=d, hk=2, hq=8, dtype=dt, n=2, rows=2 * nq, keys=3000)
 
 
@@ -114,6 +115,9 @@ def test_splits(tmp_path):
     assert kernels(op="cached") == ["kv_attend_kernel"] and kernels(op="plain") == ["attend_kernel"]
     assert kernels(op="cached", keys=1100) == ["kv_attend_kernel", "attend_join_kernel"]
     assert kernels(op="plain", keys=9000, n=30, rows=30) == ["attend_kernel", "attend_join_kernel"]
+    assert kernels(op="cached", keys=500, rows=64) == ["kv_attend_kernel"] and kernels(op="plain", keys=500, rows=32) == ["attend_kernel"]
+    assert kernels(op="cached", keys=500, n=16, rows=320) == ["kv_attend_rows_kernel"]
+    assert kernels(op="plain", keys=500, n=16, rows=80) == ["attend_rows_kernel"]
     assert kernels(op="plain", keys=8192, rows=8192) == ["attend_rows_kernel"]
     assert kernels(op="cached", keys=8192, rows=512) == ["kv_attend_rows_kernel", "attend_join_rows_kernel"]
     assert kernels(op="cached", keys=8192, rows=8192, ragged=1) == ["kv_attend_rows_kernel"]

@@ -106,6 +106,31 @@ def test_head_sizes(kind, dtype, d, nq):
 
 @both
 @types
+@pytest.mark.parametrize("d", [8, 40, 64, 80, 96, 128, 136, 192, 256])
+@pytest.mark.parametrize("nq", [1, 30, 150])
+def test_keys_shared_by_workgroups(kind, dtype, d, nq):
+    run(kind, [3000, 3000], [nq, nq], 8, 2, d, dtype)
+
+
+@pytest.mark.parametrize("d", [8, 32, 40, 64, 72, 80, 96, 120, 128, 136, 192, 200, 256])
+@pytest.mark.parametrize("mask", [dict(causal=False), dict(window=150, sinks=3)])
+def test_thousands_of_rows(d, mask):
+    """So many that a wave has two row tiles."""
+    run("plain", [300, 99, 8192], [70, 200, 8192], 4, 1, d, **mask)
+
+
+@pytest.mark.parametrize("mask", [dict(), dict(causal=False), dict(window=40, sinks=1), dict(causal=False, window=9, sinks=40)])
+def test_thousands_of_rows_key_by_key(mask):
+    n = 250
+    v = torch.zeros(n, 1, 256)
+    v[torch.arange(n), :, torch.arange(n)] = 1.0
+    x = Plain([n], 1, 256, v=v.to(DT["bf16"]).cuda())
+    q = randn(16400, 2, 256, seed=3) / 4
+    compare(x.attend(q, **mask), x, q, [16400], **mask)
+
+
+@both
+@types
 @pytest.mark.parametrize("hq,hk", [(1, 1), (3, 3), (6, 2), (7, 1), (24, 8), (40, 2)])
 def test_groups(kind, dtype, hq, hk):
     run(kind, [150], [3], hq, hk, 64, dtype)
