@@ -527,7 +527,7 @@ incvit_status incvit_kv_read(const incvit_kv* c, const void* cache, int32_t dtyp
  * out = sum_j softmax_j(scale * q . k_j) v_j over the keys it sees, zeros where it
  * sees none; keys and values that it does not see have no effect on it, whatever
  * they hold.  Scores, softmax and sums are fp32; with bf16 the weights are rounded
- * to bf16 for their product with the values; one rounding to dtype at the end.
+ * to bf16, or to the sum of two, for their product with the values; one rounding to dtype at the end.
  * head_dim: as incvit_kv's, of keys and values alike; q_heads a multiple of
  * kv_heads, both in [1, 1024]; window and sinks in [0, 2^30]; fill 0 or 1; scale >
  * 0, finite. */

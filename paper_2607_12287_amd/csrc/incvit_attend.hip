@@ -10,7 +10,7 @@ using namespace incvit;
 namespace {
 
 // Workgroups of a call that shares keys, where waves have keys and where they have
-// rows, and the key tiles of one at least.  16 sequences over 76 k keys, heads of 128
+// rows, and the key tiles of one at least.  32 sequences over 152 k keys, heads of 128
 // (cached): 39, 38, 37, 35 us with 512, 768, 1024, 1536.
 constexpr long kWant = 1536, kWantRows = 512, kLeast = 16, kLeastRows = 8;
 

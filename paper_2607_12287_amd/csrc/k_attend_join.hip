@@ -4,6 +4,10 @@
 // each of every (1024 / DS)-th share, and add those through LDS, in a fixed order.
 // Row tiles whose keys were one workgroup's are there already.  Where row tiles are
 // large, and their shares few, a thread has 4 dims of a row and all of its shares.
+//
+// 5.0 us behind 32 decoding sequences in 416 shares, 8.5 behind 1024 rows in 4 (34 MB of parts:
+// 4.0 TB/s).  All shares in one thread for decoding rows too:
+// one sequence of 131072 keys 113 us instead of 32.
 #include "attend.hpp"
 
 namespace incvit {

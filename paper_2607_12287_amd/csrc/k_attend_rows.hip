@@ -7,6 +7,17 @@
 // S^T, softmax and O^T are those of k_attend.hip, but a row stays with its wave, so
 // nothing is exchanged at the end.  A wave leaves out tiles that none of its rows
 // sees.
+//
+// Bound by the three things that a tile needs in turn, products, LDS operands and
+// softmax, which two workgroups to a CU overlap in part.  A causal prompt of 8192, 16 +
+// 4 heads of 128: 293 us, 939 TFLOP/s (a large library product here: 1300); matrix
+// cores busy 39% of the cycles, vector instructions 53%, LDS reads 39% and their
+// conflicts 10%.  Taken out of a variant of 326 us one at a time: operand reads 267,
+// staging and barriers 254, softmax 293, all three 150.  32 rows of a wave: 16 took
+// 437 us, since every row tile reads all operands, 64 453, with one wave to a SIMD.
+// Workgroups of eight waves whose halves take turns at products and softmax 356 (308
+// without), and operands read a group ahead gained nothing.  fp32, 2048 rows: 184 us,
+// 93 TFLOP/s of 154.
 #include "attend_plain.hpp"
 
 namespace incvit {

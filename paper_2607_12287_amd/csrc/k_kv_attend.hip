@@ -8,7 +8,17 @@
 // accumulates O^T = V^T P^T, for which the lane's P is the operand as it stands.
 // Keys and values come from the cache in operand order, one load per lane and
 // 64 dims, without LDS; integers are exact in bf16.  Scales go on the scores and
-// on P.  fp32: queries and P as sums of three bf16 numbers, which is exact.
+// on P.  fp32: queries and P as sums of three bf16 numbers, which is exact.  bf16: P as
+// two, within 2^-15, since few keys may carry a row (rounded to one, a row of one key was
+// off by two roundings); the loads hide the second product.
+//
+// A few rows are bound by the cache's bytes, so waves have keys and not rows: every
+// byte is loaded once for all heads of a group, 16 NT queries to a load.  32 sequences
+// over 152 k keys, 16 + 4 heads of 128 (156 MB): 35 us with the join, 4.4 TB/s; 256
+// sequences of 1000 keys 46 us, 5.7 TB/s; one of 777 keys 11.3 us, a workgroup's chain
+// of table, scales, keys and values seven times over.  Two tiles of loads ahead in
+// registers let three workgroups share a CU; looking up blocks and scales a lane at a
+// time gained nothing and left registers in memory.
 #include "attend.hpp"
 
 namespace incvit {
@@ -56,7 +66,7 @@ constexpr int kPerCu = NT == 1 && DS <= (sizeof(T) == 2 ? 128 : 64) ? 3 : 1;
 
 template <class T, int DS, int NT>
 __global__ __launch_bounds__(64 * kKeyWaves, (kPerCu<T, DS, NT>)) void kv_attend_kernel(AttendArgs a) {
-  constexpr int NP = DS / 16, NC = (NP + 3) / 4, TAIL = NP % 4, TR = 16 * NT, PARTS = sizeof(T) == 4 ? 3 : 1;
+  constexpr int NP = DS / 16, NC = (NP + 3) / 4, TAIL = NP % 4, TR = 16 * NT, PARTS = sizeof(T) == 4 ? 3 : 1, WP = sizeof(T) == 4 ? 3 : 2;
   extern __shared__ __align__(16) char lds[];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -159,7 +169,7 @@ __global__ __launch_bounds__(64 * kKeyWaves, (kPerCu<T, DS, NT>)) void kv_attend
     const int j0 = tile * kKeyTile, j1 = j0 + kKeyTile - 1;
     const bool whole = (x.ok == 3) & all_seen(a, w.len, kt.p0, kt.p1, j0, j1);
     const float c0 = x.ks[0] * a.scale_log2, c1 = x.ks[1] * a.scale_log2;
-    uint4 pop[NT][PARTS];
+    uint4 pop[NT][WP];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       float y[8], p[8];
@@ -182,7 +192,7 @@ __global__ __launch_bounds__(64 * kKeyWaves, (kPerCu<T, DS, NT>)) void kv_attend
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = see >> j & 1 ? p[j] : 0.0f;  // whatever the scale of a value that is not seen
       }
-      split8<PARTS>(p, pop[t]);
+      split8<WP>(p, pop[t]);
       if (__any(alpha != 1.0f)) {
 #pragma unroll
         for (int k = 0; k < NP; ++k) o[t][k] *= alpha;
@@ -195,7 +205,7 @@ __global__ __launch_bounds__(64 * kKeyWaves, (kPerCu<T, DS, NT>)) void kv_attend
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int r = 0; r < PARTS; ++r) o[t][k] = mma16(vop, pop[t][r], o[t][k]);
+        for (int r = 0; r < WP; ++r) o[t][k] = mma16(vop, pop[t][r], o[t][k]);
     }
   };
 
