@@ -11,7 +11,7 @@
 // Bound by the three things that a tile needs in turn, products, LDS operands and
 // softmax, which two workgroups to a CU overlap in part.  A causal prompt of 8192, 16 +
 // 4 heads of 128: 293 us, 939 TFLOP/s (a large library product here: 1300); matrix
-// cores busy 39% of the cycles, vector instructions 53%, LDS reads 39% and their
+// cores busy 40% of the cycles, vector instructions 55%, LDS reads 41% and their
 // conflicts 10%.  Taken out of a variant of 326 us one at a time: operand reads 267,
 // staging and barriers 254, softmax 293, all three 150.  32 rows of a wave: 16 took
 // 437 us, since every row tile reads all operands, 64 453, with one wave to a SIMD.

@@ -13,9 +13,9 @@
 // of the values (4 tokens together, of which it takes a byte of each dim).
 //
 // Both are bound by memory where rows are many: 8192 rows of 16 heads of 64 in bf16,
-// written 16.1 us, of which 33.5 MB in and 16.8 MB out take 9.9 at a copy's rate (5.1
-// TB/s; 16.8 MB of the counters' reads, the rest is still in the 256 MB cache), read
-// 11.3 us for the same bytes the other way (4.5 TB/s).  Few rows are a chain of
+// written 16.1 us for 33.6 MB in and 16.8 MB out (counters: 33.7 and 16.5; 3.1 TB/s of
+// a copy's 5.1), read 11.3 us for the same the other way (4.5 TB/s; 25.2 MB in, since
+// 8 tokens' keys share a line and workgroups on two XCDs read it).  Few rows are a chain of
 // latencies: slots, rows and what the block keeps, then the waves' exchange (one row
 // of 4 heads of 128: 5.2 us in a graph, read 3.4).  A wave for 2, 4 or 8 rows of a
 // read gained nothing, nor did 8 or 16 waves to a workgroup.

@@ -14,7 +14,8 @@
 //
 // A few rows are bound by the cache's bytes, so waves have keys and not rows: every
 // byte is loaded once for all heads of a group, 16 NT queries to a load.  32 sequences
-// over 152 k keys, 16 + 4 heads of 128 (156 MB): 35 us with the join, 4.4 TB/s; 256
+// over 152 k keys, 16 + 4 heads of 128 (156 MB): 35 us with the join, 4.4 TB/s, each
+// byte once by the counters; 256
 // sequences of 1000 keys 46 us, 5.7 TB/s; one of 777 keys 11.3 us, a workgroup's chain
 // of table, scales, keys and values seven times over.  Two tiles of loads ahead in
 // registers let three workgroups share a CU; looking up blocks and scales a lane at a
