@@ -67,7 +67,7 @@ hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t s);
 constexpr int kKeyTile = 32;   // keys that a wave takes at once where the waves of a workgroup share its keys
 constexpr int kKeyWaves = 4;   // waves of a workgroup
 constexpr int kMostShares = 256;  // of a row tile's keys
-constexpr int kEvenTiles = 64;    // sequences whose shares are made even
+constexpr int kEvenTiles = 64;    // sequences whose shares are made even: the lanes of a wave (a batch of 32, 200 to 16384 keys: 35 us, without 48)
 
 struct AttendArgs {
   const int* q_start;  // null: q_len rows for each sequence
@@ -81,7 +81,7 @@ struct AttendArgs {
   float* parts;        // workspace
   long rows, key_rows;
   int n, q_len, k_len, width, blocks, lb;
-  int hq, hk, group, d;
+  int hk, group, d;
   int causal, window, sinks;
   int fill;            // with q_start: rows behind the last sequence as those of one without keys
   float scale_log2;    // scale * log2(e)
@@ -383,7 +383,7 @@ __device__ __forceinline__ void floats_of(const V8<uint16_t>& x, float* y) {
   }
 }
 
-// PARTS = 1: x rounded to bf16; 3: x exactly
+// PARTS = 1: x rounded to bf16; 2: x within 2^-15; 3: x exactly
 template <int PARTS>
 __device__ __forceinline__ void split8(const float* x, uint4* out) {
   if constexpr (PARTS == 1) {

@@ -115,7 +115,6 @@ AttendArgs attend_args(const incvit_attention& a, const AttendPlan& p, int32_t n
   r.rows = (long)rows;
   r.n = n;
   r.q_len = q_start ? 0 : (int)(rows / n);
-  r.hq = a.q_heads;
   r.hk = a.kv_heads;
   r.group = a.q_heads / a.kv_heads;
   r.d = a.head_dim;

@@ -272,9 +272,6 @@ hipError_t launch_one(const AttendArgs& a, hipStream_t s) {
 template <class T, int DS>
 hipError_t launch_ds(const AttendArgs& a, int nt, hipStream_t s) {
   constexpr int most = most_row_tiles(sizeof(T) == 2, DS);
-  if constexpr (most >= 4) {
-    if (nt == 4) return launch_one<T, DS, 4>(a, s);
-  }
   if constexpr (most >= 2) {
     if (nt == 2) return launch_one<T, DS, 2>(a, s);
   }
