@@ -67,6 +67,7 @@ hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t s);
 constexpr int kKeyTile = 32;   // keys that a wave takes at once where the waves of a workgroup share its keys
 constexpr int kKeyWaves = 4;   // waves of a workgroup
 constexpr int kMostShares = 256;  // of a row tile's keys
+constexpr int kMostKeys = 1 << 30;  // of a sequence that are looked at: no position overflows
 constexpr int kEvenTiles = 64;    // sequences whose shares are made even: the lanes of a wave (a batch of 32, 200 to 16384 keys: 35 us, without 48)
 
 struct AttendArgs {
@@ -170,8 +171,6 @@ __device__ __forceinline__ bool row_tile(const AttendArgs& a, int f, RowTile& w)
   return w.first >= 0 && w.first < w.q_len * a.group;  // below 0: starts that do not ascend
 }
 
-// Keys of a sequence: at most 2^30, so that no position below overflows.
-constexpr int kMostKeys = 1 << 30;
 __device__ __forceinline__ int cached_len(const AttendArgs& a, int seq) {
   if (seq >= a.n) return 0;
   return max(min(gbl(a.lens)[seq], (int)min((long)a.width * (16 << a.lb), (long)kMostKeys)), 0);

@@ -156,8 +156,9 @@ AttendPlan plan_with(const incvit_attention& a, bool cached, long n, long rows, 
   const long tr = 1L << p.row_log, kt = 1L << p.key_log;
   p.tiles_each = (int)((rows / n * group + tr - 1) / tr);
   p.tiles = ragged ? rows * group / tr + n + a.fill : n * p.tiles_each;
-  // key tiles of a row tile at most
-  long span = max_len;
+  // key tiles of a row tile at most: the kernels see no more keys of a sequence, and
+  // counts of their tiles stay within 32 bits
+  long span = std::min(max_len, (long)kMostKeys);
   if (a.window) span = std::min(span, (long)a.window * (a.causal ? 1 : 2) + tr / group + 1 + a.sinks + 3 * kt);
   const long tiles = std::max(1L, (span + kt - 1) / kt);
   const long wgs = std::max(1L, p.tiles * a.kv_heads);

@@ -149,6 +149,30 @@ def test_workspaces():
     assert incvit.lib().incvit_attention_workspace_bytes(None, 1, 1, 1, 0, 5) == 0
 
 
+@pytest.mark.parametrize("most", [2 ** 30, 2 ** 31 + 5, 2 ** 36, 2 ** 39, 2 ** 40])
+def test_hints_past_the_most_keys_plan_as_those(most):
+    """A hint may be any number to 2^40; a sequence has 2^30 keys at most, and the split is made for no more."""
+    f = incvit.incvit_attention_workspace_bytes
+    forms = set()
+    for dtype in (0, 1):
+        for hk in (1, 2, 3, 4, 7, 16, 64, 255, 1000):
+            for cached in (0, 1):
+                for n, rows, ragged in [(1, 1, 0), (1, 40, 0), (1, 4096, 0), (1, 8192, 0), (1, 8192, 1), (180, 180, 0), (180, 180, 1), (60, 60, 0)]:
+                    a = attention(dtype=dtype, q_heads=hk, kv_heads=hk)
+                    got = f(a, cached, n, rows, ragged, most)
+                    assert got == f(a, cached, n, rows, ragged, 2 ** 30), (dtype, hk, cached, n, rows, ragged)
+                    forms.add(got > 0)
+                    # partial results of 128 rows at most: of 1536 shares, or of as many (one for each head) and one for each sequence
+                    assert got <= (max(1536, hk) + 64 * hk) * 128 * (64 + 2) * 4
+    assert forms == {False, True}
+
+
+def test_the_widest_tables_are_planned():
+    """Without a hint the table's width stands for it, up to 2^38 keys: shared, so that a call without a workspace is refused."""
+    for block, width, n, rows_ in ((128, 2 ** 31 - 1, 1, 1), (128, 2 ** 31 - 1, 1, 1000), (16, 2 ** 31 - 1, 3, 3), (128, 2 ** 31 - 1, 31, 62)):
+        assert cached(c=kv(block=block), n=n, rows_=rows_, width=width, workspace=0) == ARG
+
+
 def test_sizes_past_32_bits_are_refused_in_python():
     for kw in (dict(blocks=2 ** 32 + 1), dict(heads=2 ** 32 + 1), dict(head_dim=2 ** 32 + 64), dict(block=2 ** 32 + 16), dict(blocks=-1)):
         with pytest.raises(ValueError):
