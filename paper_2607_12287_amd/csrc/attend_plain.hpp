@@ -89,6 +89,10 @@ __device__ __forceinline__ void p_op(V8<float>& out, const float* p) {
   out.b = make_float4(p[4], p[5], p[6], p[7]);
 }
 
+// Dim i of the 4 that lane group g has of piece k, in a row of d; 0 for dims past the head
+// (heads of 8: groups 2 and 3), whose value is not used.
+__host__ __device__ constexpr int special_dim(int k, int g, int i, int d) { return 16 * k + 4 * g < d ? 16 * k + 4 * g + i : 0; }
+
 // The infinities and NaN of the values of keys j0 to j1, for the rows that see them:
 // a weight is above 0, so each makes its sum what it is itself.
 template <class T, int NP, int NT>
@@ -97,13 +101,13 @@ __device__ __forceinline__ void add_special(f32x4_t (&o)[NT][NP], const Sight (&
   const int g = lane >> 4;
 #pragma unroll 1
   for (int key = j0; key <= j1; ++key) {
-    const T* src = reinterpret_cast<const T*>(values + key * v_row) + 4 * g;
+    const T* src = reinterpret_cast<const T*>(values + key * v_row);
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
       __builtin_amdgcn_sched_barrier(0);  // a rare path: few registers
       float x[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = Elem<T>::f(gbl(src)[16 * k + 4 * g < d ? 16 * k + i : 0]);
+      for (int i = 0; i < 4; ++i) x[i] = Elem<T>::f(gbl(src)[special_dim(k, g, i, d)]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const bool odd = !__builtin_isfinite(x[i]) & (16 * k + 4 * g < d);
