@@ -244,6 +244,20 @@ __device__ __forceinline__ int lanes_scan(int x) {
   return x;
 }
 
+// Even shares: key tiles that one has, of `total` and at least `least`, and how many
+// a sequence of nt key tiles gets.  `even` and one for each sequence are enough for
+// all of them if the total counts what even_count does: kEvenMost at most, so that
+// 64 of them add up within 32 bits.
+constexpr int kEvenMost = 1 << 24;
+__host__ __device__ constexpr int even_chunk(int total, int least, int even) {
+  const int chunk = (total + even - 1) / even;
+  return chunk > least ? chunk : least;
+}
+__host__ __device__ constexpr int even_count(int nt, int chunk) {
+  const int n = ((nt < kEvenMost ? nt : kEvenMost) + chunk - 1) / chunk;
+  return n < 1 ? 1 : n < kMostShares ? n : kMostShares;
+}
+
 // Even shares, for up to 64 sequences of one row tile each: every wave has their key
 // tiles in its lanes, which gives the size of a share, and from the shares before
 // each sequence its own.  want: share number (of a head), or with TILE the sequence
@@ -255,8 +269,8 @@ __device__ __forceinline__ bool even_share(const AttendArgs& a, int want, Share&
   RowTile w;
   w.seq = min(lane, a.tiles - 1);
   const int len = seq_len(a, w), nt = in ? key_tiles(a, len, len - a.q_len, len - 1).nt : 0;
-  const int total = __builtin_amdgcn_readlane(lanes_scan(min(nt, 1 << 24)), 63), chunk = max(a.chunk, (total + a.even - 1) / a.even);
-  const int n = in ? max(1, min(kMostShares, (nt + chunk - 1) / chunk)) : 0, upto = lanes_scan(n);
+  const int total = __builtin_amdgcn_readlane(lanes_scan(min(nt, kEvenMost)), 63), chunk = even_chunk(total, a.chunk, a.even);
+  const int n = in ? even_count(nt, chunk) : 0, upto = lanes_scan(n);
   const uint64_t there = __ballot(TILE ? lane == want : in & (upto > want));
   if (!there) return false;
   s.f = __builtin_ctzll(there);

@@ -29,3 +29,27 @@ def test_looking_for_infinities_stays_in_the_row(tmp_path):
           const int at = special_dim(k, g, i, d);
           if (at < 0 || at >= d || (16 * k + 4 * g < d && at != 16 * k + 4 * g + i)) printf("d %d k %d g %d i %d: %d\\n", d, k, g, i, at);
         }""")
+
+
+def test_even_shares_are_no_more_than_the_launch_has(tmp_path):
+    """As many as `even` and one for each sequence, also for the longest sequences (2^30 keys, 2^25 tiles)."""
+    run_on_host(tmp_path, "attend.hpp", """
+  std::mt19937 r(5);
+  for (int trial = 0; trial < 200000; ++trial) {
+    const int n = 1 + r() % kEvenTiles, even = 1 + r() % 1536, most = r() % 26;
+    int nt[kEvenTiles];
+    long total = 0;
+    for (int i = 0; i < n; ++i) {
+      nt[i] = trial % 7 == 0 ? 1 << most : (int)(r() % (1u << (r() % (most + 1)))) + (r() % 2);
+      total += nt[i] < kEvenMost ? nt[i] : kEvenMost;
+    }
+    if (total != (int)total) printf("total %ld\\n", total);
+    const int chunk = even_chunk((int)total, 16, even);
+    long shares = 0;
+    for (int i = 0; i < n; ++i) {
+      const int c = even_count(nt[i], chunk);
+      shares += c;
+      if (c < 1 || c > kMostShares || (c < kMostShares && nt[i] <= kEvenMost && (long)c * chunk < nt[i])) printf("%d tiles: %d of %d\\n", nt[i], c, chunk);
+    }
+    if (shares > even + n) printf("%d sequences, %d: %ld\\n", n, even, shares);
+  }""")

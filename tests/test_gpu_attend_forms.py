@@ -1,5 +1,5 @@
-"""Attention over given keys and values where a form of the kernels is at its limits: the smallest heads with values that are not
-finite.  The bound is derived in kv_ref.attention."""
+"""Attention at the limits of its kernels: the smallest heads with values that are not finite, the longest sequences.  The bound
+is derived in kv_ref.attention."""
 import math
 
 import pytest
@@ -30,3 +30,21 @@ def test_values_that_are_not_finite_in_the_last_head(d, dtype, rows):
     assert (got[-1, 2:, 0:d - 1:3] == -math.inf).all() and got[-2:, 2:, d - 1].isnan().all()
     keep = [i for i in range(d - 1) if i % 3]
     assert torch.equal(got[..., keep], want[..., keep]) and torch.equal(got[-2, :, :d - 1], want[-2, :, :d - 1])
+
+
+def test_the_longest_sequences():
+    """64 sequences of 2^30 tokens, of which two blocks lie in the pool: the first and the last."""
+    n, hk, d, block = 64, 1, 32, 128
+    cache = incvit.KVCache(4, hk, d, block=block)
+    k, v = randn(2 * block, hk, d, seed=1), randn(2 * block, hk, d, seed=2)
+    slots = torch.arange(2 * block, dtype=torch.int32, device="cuda")
+    cache.write(k, v, slots, begin=True)
+    table = torch.full((1, 2 ** 30 // block), -1, dtype=torch.int32, device="cuda")
+    table[0, 0], table[0, -1] = 0, 1
+    q = randn(n, 2, d, seed=3)
+    got = cache.attend(q, table.expand(n, -1), torch.full((n,), 2 ** 30, dtype=torch.int32, device="cuda"))
+    held = [kv_ref.Held(4, hk, d, block) for _ in range(2)]
+    for h, x in zip(held, (k, v)):
+        h.write(x, slots.tolist(), True)
+    see = torch.ones(n, 2 * block, dtype=torch.bool, device="cuda")
+    kv_ref.check(got, *kv_ref.attention(q, *(h.exact()[:2 * block].cuda() for h in held), see))
