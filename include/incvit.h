@@ -488,8 +488,10 @@ size_t incvit_kv_bytes(const incvit_kv* c);
  * 2^40]; views of a projection's output will do) and its values lie one after
  * another; likewise v.  dtype: incvit_dtype of both.  Row r goes to slots[r]
  * (device int32 [rows]); a row whose slot is outside the pool (padding: negative)
- * goes nowhere.  Rows of one block have to follow one another; of rows of one
- * slot the last one stays.  For each block that is written, and head:
+ * goes nowhere, wherever it stands.  The other rows of one block have to follow one
+ * another: a block whose rows stand in two places, with another block's between
+ * them, holds anything afterwards.  Of rows of one slot the last one stays.  For
+ * each block that is written, and head:
  *   a = max |x| over the new rows' values, s_new = a / 127 rounded to fp32 (NaN
  *     where a value is not finite), s = max(s_old, s_new), NaN if either is;
  *   new values: x / s rounded to fp32, then to the nearest integer (ties to

@@ -1,11 +1,11 @@
 // Keys and values written into a cache in 8 bits, and read back.
 //
 // Write: a wave for each group of 16 tokens of a block, one head, keys or values,
-// takes the rows of the block that follow one another.  They are put at their places
-// (a map in LDS; of rows of one slot the last), loaded into registers together with
-// what the group keeps, and the waves of a block join their largest magnitudes; then
-// new rows are quantised, kept integers rounded anew where the scale has grown, and
-// only what changes is written.  The launch has a block's waves for every row (those
+// takes the rows of the block that follow one another, padding aside.  They are put at
+// their places (a map in LDS; of rows of one slot the last), loaded into registers
+// together with what the group keeps, and the waves of a block join their largest
+// magnitudes; then new rows are quantised, kept integers rounded anew where the scale
+// has grown, and only what changes is written.  The launch has a block's waves for every row (those
 // whose row goes on with a block end at once) or, from kFewItems and kManyItems on,
 // for every 4 and 16 (32) rows, and they take the blocks that begin there in turn.
 //
@@ -222,23 +222,55 @@ __device__ __forceinline__ void block_sync() {
   else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// The run that begins with row base + first; the lanes have the slots of the rows
-// from base on.
+// Slots of the 64 rows from `base` on; -1 past the call's.  (Rows have 24 bits.)
+__device__ __forceinline__ int slots_of(const KvWriteArgs& a, int base, int lane) {
+  const int r = base + lane, rows = (int)a.rows, s = gbl(a.slots)[(uint32_t)min(max(r, 0), rows - 1)];
+  return (uint32_t)r < (uint32_t)rows ? s : -1;
+}
+__device__ __forceinline__ bool in_pool(const KvWriteArgs& a, int slot) { return (uint32_t)slot < (uint32_t)(a.blocks * a.block); }
+
+// Padding is passed over 256 rows at a time, whose slots are on the way together:
+// the slots of the next 64 rows (from base + 64 on) or those before (from base - 64)
+// that are not padding alone, and `base` is where they are; false if none.
+template <int STEP>
+__device__ __forceinline__ bool pass_padding(const KvWriteArgs& a, int& base, int& slot, int lane) {
+  constexpr int N = 4;
+  while (true) {
+    int s[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) s[k] = slots_of(a, base + STEP * (k + 1), lane);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      base += STEP;
+      slot = s[k];
+      if (__ballot(in_pool(a, slot))) return true;
+      if (STEP > 0 ? base >= (int)a.rows : base <= 0) return false;
+    }
+  }
+}
+
+// The block of a slot; -1 for padding.
+template <int W>
+__device__ __forceinline__ int block_of(const KvWriteArgs& a, int slot) {
+  return in_pool(a, slot) ? slot / (16 * W) : -1;
+}
+
+// The run that begins with row base + first, up to the next row of another block
+// (padding does not end it); the lanes have the slots of the rows from base on.
 template <class T, int NPC, int W>
-__device__ __forceinline__ void write_block(const KvWriteArgs& a, int* map, uint32_t* tops, long base, int first, int slot, int blk, int h,
+__device__ __forceinline__ void write_block(const KvWriteArgs& a, int* map, uint32_t* tops, int base, int first, int slot, int blk, int h,
                                             int side, int lane, int wave) {
   constexpr int B = 16 * W;
   if (lane < 16) map[16 * wave + lane] = -1;
   block_sync<W>();
   if (wave == 0) {
     while (true) {
-      const uint64_t in = __ballot(slot >= (long)blk * B && slot < (blk + 1L) * B) >> first;
-      const int run = in == ~0ull ? 64 : __builtin_ctzll(~in);
-      if (lane >= first && lane < first + run) atomicMax(&map[slot - blk * B], (int)(base + lane));
-      if (first + run < 64) break;
-      base += 64;
+      const int mine = block_of<W>(a, slot);
+      const uint64_t other = __ballot(mine >= 0 && mine != blk) & (~0ull << first);
+      const int end = other ? __builtin_ctzll(other) : 64;
+      if (mine == blk && lane >= first && lane < end) atomicMax(&map[slot % B], base + lane);
+      if (other || base + 64 >= (int)a.rows || !pass_padding<64>(a, base, slot, lane)) break;
       first = 0;
-      slot = base + lane < a.rows ? gbl(a.slots)[base + lane] : -1;
     }
   }
   block_sync<W>();
@@ -295,13 +327,25 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kv_write_kernel(KvWrite
   const int lane = threadIdx.x & 63, tw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = W == 1 ? 0 : tw;
   // a row's heads and sides one after another
   const uint32_t item = W == 1 ? blockIdx.x * 4 + tw : blockIdx.x, sides = 2 * a.heads;
-  const long r0 = (long)(item / sides) * a.each;
+  const int r0 = (int)(item / sides) * a.each;
   if (r0 >= a.rows) return;
   const int rest = item % sides, side = rest & 1, h = rest >> 1;
-  // rows that begin a run of their block; the first lane has the row before
-  const long pool = (long)a.blocks * a.block, r = r0 - 1 + lane;
-  const int slot = r >= 0 && r < a.rows ? gbl(a.slots)[r] : -1;
-  const int blk = slot >= 0 && slot < pool ? slot / (16 * W) : -1, prev = __shfl_up(blk, 1);
+  // rows that begin a run of their block: the row before, padding aside, is another's;
+  // the first lane has the row before the item's
+  const int slot = slots_of(a, r0 - 1, lane), blk = block_of<W>(a, slot);
+  int prev = __shfl_up(blk, 1);
+  const uint64_t there = __ballot(blk >= 0);
+  if (__builtin_expect((~there & ((2ull << a.each) - (r0 ? 1 : 2))) != 0, 0)) {  // padding, or the call's last rows
+    const uint64_t below = there & ((1ull << lane) - 1);
+    prev = __shfl(blk, below ? 63 - __builtin_clzll(below) : 0);
+    if (!(there & 1) && (there & ((2ull << a.each) - 1))) {  // rows that have only padding before them here
+      int base = r0 - 1, s = -1;
+      const bool found = base > 0 && pass_padding<-64>(a, base, s, lane);
+      const uint64_t last = __ballot(in_pool(a, s));
+      const int back = found ? __builtin_amdgcn_readlane(block_of<W>(a, s), 63 - __builtin_clzll(last)) : -1;
+      if (!below) prev = back;
+    }
+  }
   uint64_t lead = __ballot(lane > 0 && lane <= a.each && blk >= 0 && blk != prev);
   while (lead) {
     const int i = __builtin_ctzll(lead);

@@ -338,7 +338,7 @@ class KVCache:
     def write(self, k, v, slots, begin: bool = False):
         """Quantise new keys and values [rows][heads][d] (fp32 or bf16, any 16-byte
         aligned row and head strides) into `slots` (device int32 [rows], negative:
-        nowhere; the rows of one block one after another).  A block keeps what it
+        nowhere; the rows of one block one after another, with any of those between).  A block keeps what it
         holds, rounded anew if its scale grows; with `begin` one whose first slot is
         written holds nothing else afterwards (a sequence that goes on into a block
         used before)."""

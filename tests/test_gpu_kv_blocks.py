@@ -1,0 +1,49 @@
+"""Rows written into the cache in 8 bits as workgroups take them: padding between the rows of a block.  Bit for bit, as in
+test_gpu_kv."""
+import random
+
+import pytest
+import torch
+
+from tests.test_gpu_kv import Pair, rows_of
+
+pytestmark = pytest.mark.gpu
+blocks_of = pytest.mark.parametrize("block", [16, 32, 64, 128])
+
+
+def write(p, slots, heads, d, dtype="bf16", seed=0, size=1.0, begin=False):
+    n = len(slots)
+    p.write(rows_of(n, heads, d, dtype, seed, size), rows_of(n, heads, d, dtype, seed + 1, size), slots, begin)
+
+
+@blocks_of
+@pytest.mark.parametrize("heads", [1, 8, 32])  # 512, 4096 and 16384 items: a workgroup's rows are 1 and 4
+def test_frames_whose_other_tokens_are_padding(block, heads):
+    """A call of one size for every frame: a row for each token, and no slot for those that stay."""
+    p = Pair(256 // block, heads, 40, block)
+    write(p, list(range(256)), heads, 40, begin=True)
+    pick = random.Random(block + heads)
+    for i, share in enumerate((0.7, 0.3, 0.05, 0.01, 0.0)):
+        slots = [t if pick.random() < share else pick.choice([-1, -9, 256, 2 ** 31 - 1, -2 ** 31]) for t in range(256)]
+        write(p, slots, heads, 40, seed=10 + i, size=0.5 + 0.4 * i)
+        p.check()
+
+
+@blocks_of
+@pytest.mark.parametrize("heads", [1, 2, 6])  # 1 (4 for the longest), 4 and 16 or 32 rows of a workgroup
+@pytest.mark.parametrize("gap", [62, 63, 64, 65, 511, 512, 513, 577, 1200])
+def test_long_padding_between_the_rows_of_a_block(block, heads, gap):
+    p = Pair(4, heads, 32, block)
+    write(p, list(range(4 * block)), heads, 32, begin=True)
+    # two rows of a block, one and two of the next, with padding before, between and behind; then a block's second half
+    valid = [5, 3, block + 1, 2 * block + 7, 2 * block + 7, 3 * block + 15]
+    slots = [-1] * (gap // 2)
+    for s in valid:
+        slots += [s] + [-1] * gap
+    n = 3600 if heads == 1 else 5000
+    slots += [-1] * max(0, n - len(slots))
+    write(p, slots, heads, 32, seed=3, size=2.0)
+    p.check()
+    write(p, [-1] * n + [block], heads, 32, seed=5, size=3.0)  # behind padding alone
+    write(p, [-1] * n, heads, 32, seed=7, size=3.0)
+    p.check()
