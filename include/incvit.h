@@ -565,7 +565,7 @@ size_t incvit_attention_workspace_bytes(const incvit_attention* a, int32_t cache
  *   lens: device int32 [n], keys of each sequence, its queries' among them (a
  *     query whose position is negative sees what the mask lets it);
  *   table: device int32, block e of sequence i at table[i * table_stride + e], e <
- *     width; keys past width * block, and those of a block number outside the pool,
+ *     width (0: the table may be NULL); keys past width * block, and those of a block number outside the pool,
  *     are not seen.
  * max_len: about the most keys of a sequence, for the split over workgroups; the
  * result does not depend on it beyond the order of sums (0: width * block).

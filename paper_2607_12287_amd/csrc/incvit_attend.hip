@@ -264,7 +264,7 @@ incvit_status incvit_kv_attend(const incvit_attention* a, const incvit_kv* c, co
   if (n == 0 || rows == 0) return INCVIT_OK;
   if (!q || !out) return op_fail(INCVIT_ERR_ARG, "null queries or output");
   if (!cache || (uintptr_t)cache % 256) return op_fail(INCVIT_ERR_ARG, "the cache must be non-null and 256-byte aligned");
-  if (!table || !lens) return op_fail(INCVIT_ERR_ARG, "null table or lens");
+  if ((!table && width > 0) || !lens) return op_fail(INCVIT_ERR_ARG, "null table or lens");
   if (((uintptr_t)table | (uintptr_t)lens | (uintptr_t)q_start) % 4)
     return op_fail(INCVIT_ERR_ARG, "q_start, table and lens must be 4-byte aligned");
   if (width < 0 || table_stride < 0 || table_stride > kMostStride)

@@ -1,5 +1,5 @@
-"""Attention at the limits of its kernels: the smallest heads with values that are not finite, the longest sequences.  The bound
-is derived in kv_ref.attention."""
+"""Attention at the limits of its kernels: the smallest heads with values that are not finite, the longest sequences and
+those without any block.  The bound is derived in kv_ref.attention."""
 import math
 
 import pytest
@@ -48,3 +48,17 @@ def test_the_longest_sequences():
         h.write(x, slots.tolist(), True)
     see = torch.ones(n, 2 * block, dtype=torch.bool, device="cuda")
     kv_ref.check(got, *kv_ref.attention(q, *(h.exact()[:2 * block].cuda() for h in held), see))
+
+
+@types
+@pytest.mark.parametrize("rows", [2, 400])
+def test_tables_without_columns(dtype, rows):
+    """No sequence has a block yet: every row is zeros, as with lengths of 0."""
+    cache = incvit.KVCache(4, 2, 64)
+    q = randn(rows, 4, 64, dtype=dtype)
+    table, lens = torch.zeros(2, 0, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    for kw in (dict(), dict(causal=False), dict(window=5, sinks=2), dict(causal=False, window=5, sinks=2)):
+        assert (cache.attend(q, table, lens, **kw) == 0).all()
+        lens.fill_(99)  # keys past the table's columns are not seen
+        out = cache.attend(q, table, lens, q_start=torch.tensor([0, 1, rows], dtype=torch.int32, device="cuda"), **kw)
+        assert (out == 0).all()
