@@ -47,3 +47,32 @@ def test_long_padding_between_the_rows_of_a_block(block, heads, gap):
     write(p, [-1] * n + [block], heads, 32, seed=5, size=3.0)  # behind padding alone
     write(p, [-1] * n, heads, 32, seed=7, size=3.0)
     p.check()
+
+
+@blocks_of
+@pytest.mark.parametrize("dtype,heads,n", [("bf16", 4, 1500), ("f32", 3, 6000)])  # 12000 and 36000 items: 4 and 16 or 32 rows
+def test_workgroups_that_take_several_blocks(block, dtype, heads, n):
+    """Prompts through shuffled blocks, from the middle of one to the middle of one, then rows here and there: groups of a block
+    with new rows and without, under a scale that stays and one that grows."""
+    need = -(-n // block) + 2
+    order = torch.randperm(need, generator=torch.Generator().manual_seed(n)).tolist()
+    p = Pair(need, heads, 40, block)
+    slots = [order[t // block] * block + t % block for t in range(block // 2 + 3, block // 2 + 3 + n)]
+    write(p, slots, heads, 40, dtype, begin=True)
+    p.check()
+    pick = random.Random(block)
+    for seed, (share, size) in enumerate(((0.9, 0.3), (0.9, 2.0))):
+        write(p, [s for s in slots if pick.random() < share], heads, 40, dtype, 10 + 2 * seed, size)
+        p.check()
+    write(p, [-1 if (s // 16) % 3 else s for s in slots], heads, 40, dtype, 20, 3.0)  # two groups of three without new rows
+    p.check(dtype)
+
+
+@blocks_of
+@pytest.mark.parametrize("heads,n", [(12, 400), (24, 700)])  # 9600 and 33600 items
+def test_a_token_of_each_of_many_sequences(block, heads, n):
+    """Every row begins a block's run: a workgroup takes as many blocks as it has rows."""
+    p = Pair(n, heads, 8, block)
+    for i in range(3):
+        write(p, [b * block + (7 * b + i) % block for b in range(n)], heads, 8, "bf16", 2 * i, 1.0 + i, begin=i == 1)
+    p.check()
