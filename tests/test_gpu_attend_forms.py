@@ -1,5 +1,5 @@
 """Attention at the limits of its kernels: the smallest heads with values that are not finite, the longest sequences and
-those without any block.  The bound is derived in kv_ref.attention."""
+those without any block; and the C entry without starts.  The bound is derived in kv_ref.attention."""
 import math
 
 import pytest
@@ -62,3 +62,31 @@ def test_tables_without_columns(dtype, rows):
         lens.fill_(99)  # keys past the table's columns are not seen
         out = cache.attend(q, table, lens, q_start=torch.tensor([0, 1, rows], dtype=torch.int32, device="cuda"), **kw)
         assert (out == 0).all()
+
+
+@types
+@pytest.mark.parametrize("mask", [dict(), dict(causal=False, window=700, sinks=9)])
+@pytest.mark.parametrize("n,rows", [(2, 1), (3, 5), (64, 1), (64, 2), (3, 150)])
+@pytest.mark.parametrize("given", [True, False])
+def test_equal_query_rows_without_starts(dtype, mask, n, rows, given):
+    """The C entry: each sequence has rows / n query rows, and its keys from k_start or key_rows / n; one row tile of each gets
+    shares of the keys by its length."""
+    hq, hk, d = 8, 2, 64
+    lens = [1 + (997 * i * i + 3100) % 5000 for i in range(n)] if given else [1300] * n
+    q, k, v = randn(n * rows, hq, d, dtype=dtype, seed=3), randn(sum(lens), hk, d, dtype=dtype, seed=1), randn(sum(lens), hk, d, dtype=dtype, seed=2)
+    start = torch.tensor([sum(lens[:i]) for i in range(n + 1)], dtype=torch.int32, device="cuda")
+    a = incvit.incvit_attention(incvit.INCVIT_BF16 if dtype == "bf16" else incvit.INCVIT_F32, hq, hk, d, mask.get("causal", 1),
+                                mask.get("window", 0), mask.get("sinks", 0), 0, d ** -0.5)
+    for hint in (max(lens), 0):
+        out = torch.full_like(q, math.nan)
+        nbytes = incvit.incvit_attention_workspace_bytes(a, 0, n, n * rows, 0, hint or -(-sum(lens) // n))
+        assert nbytes > 0 or not hint or rows > 5 or mask
+        ws = torch.empty(max(nbytes, 1), dtype=torch.uint8, device="cuda")
+        r = [incvit.incvit_rows(t.data_ptr(), t.stride(0), t.stride(1)) for t in (q, k, v, out)]
+        assert incvit.incvit_attend(a, n, n * rows, 0, sum(lens), start.data_ptr() if given else 0, hint, *r, ws.data_ptr(),
+                                    torch.cuda.current_stream().cuda_stream) == incvit.INCVIT_OK
+        for i, m in enumerate(lens):
+            see = kv_ref.visible(rows, m, device="cuda", **mask)
+            at = slice(start[i].item(), start[i].item() + m)
+            mine = slice(i * rows, (i + 1) * rows)
+            kv_ref.check(out[mine], *kv_ref.attention(q[mine], k[at], v[at], see))
