@@ -532,7 +532,7 @@ incvit_status incvit_kv_read(const incvit_kv* c, const void* cache, int32_t dtyp
  * to bf16, or to the sum of two, for their product with the values; one rounding to dtype at the end.
  * head_dim: as incvit_kv's, of keys and values alike; q_heads a multiple of
  * kv_heads, both in [1, 1024]; window and sinks in [0, 2^30]; fill 0 or 1; scale >
- * 0, finite. */
+ * 0, scale * log2(e) finite. */
 typedef struct {
   int32_t dtype; /* incvit_dtype of queries and output (and of given keys and values) */
   int32_t q_heads, kv_heads, head_dim;

@@ -33,6 +33,7 @@ constexpr long kFewRows = 1024;
 constexpr long kOneTileRows = 16384, kOneTileEach = 256;
 
 constexpr int64_t kMostStride = (int64_t)1 << 40;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 bool is_dtype(int32_t t) { return t == INCVIT_F32 || t == INCVIT_BF16; }
 
@@ -83,7 +84,7 @@ incvit_status check_kv(const incvit_kv* c, int32_t dtype, int64_t rows, const vo
 bool attention_ok(const incvit_attention& a) {
   return is_dtype(a.dtype) && dims_ok(a.head_dim) && a.q_heads >= 1 && a.q_heads <= 1024 && a.kv_heads >= 1 &&
          a.q_heads % a.kv_heads == 0 && (a.causal == 0 || a.causal == 1) && (a.fill == 0 || a.fill == 1) && a.window >= 0 && a.window <= (1 << 30) && a.sinks >= 0 &&
-         a.sinks <= (1 << 30) && a.scale > 0.0f && std::isfinite(a.scale);
+         a.sinks <= (1 << 30) && a.scale > 0.0f && std::isfinite(a.scale * kLog2e);
 }
 
 incvit_status check_attention(const incvit_attention* a, int32_t n, int64_t rows) {
@@ -122,7 +123,7 @@ AttendArgs attend_args(const incvit_attention& a, const AttendPlan& p, int32_t n
   r.window = a.window;
   r.sinks = a.sinks;
   r.fill = q_start ? a.fill : 0;
-  r.scale_log2 = a.scale * 1.44269504088896340736f;
+  r.scale_log2 = a.scale * kLog2e;
   r.most_rows = (int)((q_start ? rows : rows / n) * r.group);
   r.row_log = p.row_log;
   r.key_log = p.key_log;

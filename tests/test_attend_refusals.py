@@ -105,6 +105,14 @@ def test_attentions_out_of_range(kw, status):
     assert incvit.incvit_attention_workspace_bytes(a, 1, 2, 6, 0, 10 ** 6) == 0
 
 
+def test_scales_that_are_infinite_in_units_of_log2():
+    """Infinity times a score of 0 would be NaN."""
+    for scale, status in ((3.4e38, ARG), (2.4e38, ARG), (2.35e38, OK)):
+        a = attention(scale=scale)
+        assert cached(a, rows_=0) == status and plain(a, rows_=0) == status
+        assert (incvit.incvit_attention_workspace_bytes(a, 1, 2, 6, 0, 10 ** 6) > 0) == (status == OK)
+
+
 @pytest.mark.parametrize("call", [cached, plain])
 def test_what_both_attentions_refuse(call):
     for kw, status in [(dict(n=-1), ARG), (dict(n=2 ** 24 + 1, rows_=2 ** 24 + 1), ARG), (dict(rows_=-1), ARG), (dict(rows_=2 ** 29), ARG),
