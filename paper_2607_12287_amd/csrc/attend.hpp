@@ -120,7 +120,7 @@ struct AttendPlan {
 AttendPlan attend_plan(const incvit_attention& a, bool cached, long n, long rows, bool ragged, long max_len);
 
 hipError_t launch_kv_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
-hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
+hipError_t launch_attend(const AttendArgs& a, int dtype, hipStream_t s);
 hipError_t launch_kv_attend_rows(const AttendArgs& a, hipStream_t s);
 hipError_t launch_attend_rows(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
 hipError_t launch_attend_join(const AttendArgs& a, int dtype, hipStream_t s);
@@ -375,6 +375,16 @@ __device__ __forceinline__ float group4_sum(float x) {
   const float y = __uint_as_float(p[0]) + __uint_as_float(p[1]);
   const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
+// four 8-bit integers as bf16, which is exact
+__device__ __forceinline__ uint2 bf_of_i8(uint32_t w) {
+  const float a = (float)(int8_t)w, b = (float)(int8_t)(w >> 8), c = (float)(int8_t)(w >> 16), d = (float)(int8_t)(w >> 24);
+  return make_uint2(f2bf2(a, b), f2bf2(c, d));
+}
+__device__ __forceinline__ uint4 bf_of_i8x8(uint32_t w0, uint32_t w1) {
+  const uint2 a = bf_of_i8(w0), b = bf_of_i8(w1);
+  return make_uint4(a.x, a.y, b.x, b.y);
 }
 
 // fp32 values as sums of bf16 numbers, without a rounding: the leading 8 bits of

@@ -322,7 +322,7 @@ incvit_status incvit_attend(const incvit_attention* a, int32_t n, int64_t rows, 
   r.key_rows = (long)key_rows;
   r.k_len = k_start ? 0 : (int)(key_rows / n);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if ((st = launched(p.by_rows ? launch_attend_rows(r, p, a->dtype, s) : launch_attend(r, p, a->dtype, s), "attend")) != INCVIT_OK) return st;
+  if ((st = launched(p.by_rows ? launch_attend_rows(r, p, a->dtype, s) : launch_attend(r, a->dtype, s), "attend")) != INCVIT_OK) return st;
   return launched(launch_attend_join(r, a->dtype, s), "attend");
 }
 

@@ -15,8 +15,9 @@ namespace incvit {
 
 namespace {
 
-template <class T, int DS, int NT>
+template <class T, int DS>
 __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
+  constexpr int NT = 1;  // 16-row tiles of a workgroup (attend_plan)
   constexpr int NP = DS / 16, NC = DS / 32 + (DS % 32 != 0), TR = 16 * NT, RB = value_bytes<T, DS>();
   constexpr int PER = DS / 8, NV = (kKeyTile * PER + 63) / 64;  // 8-dim pieces of a row of values, of a lane
   constexpr bool AHEAD = DS * sizeof(T) <= 384;  // whether registers hold the next tile's values as well
@@ -206,31 +207,31 @@ __global__ __launch_bounds__(64 * kKeyWaves) void attend_kernel(AttendArgs a) {
   join_waves<T, DS, NT>(a, w, sh, lds, h, threadIdx.x);
 }
 
-template <class T, int DS, int NT>
+template <class T, int DS>
 hipError_t launch_one(const AttendArgs& a, hipStream_t s) {
-  constexpr int bytes = std::max(exchange_bytes<DS, NT>(), kKeyWaves * kKeyTile * value_bytes<T, DS>());
+  constexpr int bytes = std::max(exchange_bytes<DS, 1>(), kKeyWaves * kKeyTile * value_bytes<T, DS>());
   static_assert(bytes <= 160 * 1024, "LDS");
-  const hipError_t e = with_lds<attend_kernel<T, DS, NT>>(bytes);
+  const hipError_t e = with_lds<attend_kernel<T, DS>>(bytes);
   if (e != hipSuccess) return e;
-  return launch_k(attend_kernel<T, DS, NT>, dim3((unsigned)(a.shares * a.hk)), dim3(64 * kKeyWaves), (size_t)bytes, s, a);
+  return launch_k(attend_kernel<T, DS>, dim3((unsigned)(a.shares * a.hk)), dim3(64 * kKeyWaves), (size_t)bytes, s, a);
 }
 
 template <class T>
 hipError_t launch_t(const AttendArgs& a, hipStream_t s) {
   switch (kv_dims(a.d)) {
-    case 32: return launch_one<T, 32, 1>(a, s);
-    case 64: return launch_one<T, 64, 1>(a, s);
-    case 80: return launch_one<T, 80, 1>(a, s);
-    case 96: return launch_one<T, 96, 1>(a, s);
-    case 128: return launch_one<T, 128, 1>(a, s);
-    case 192: return launch_one<T, 192, 1>(a, s);
-    default: return launch_one<T, 256, 1>(a, s);
+    case 32: return launch_one<T, 32>(a, s);
+    case 64: return launch_one<T, 64>(a, s);
+    case 80: return launch_one<T, 80>(a, s);
+    case 96: return launch_one<T, 96>(a, s);
+    case 128: return launch_one<T, 128>(a, s);
+    case 192: return launch_one<T, 192>(a, s);
+    default: return launch_one<T, 256>(a, s);
   }
 }
 
 }  // namespace
 
-hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s) {
+hipError_t launch_attend(const AttendArgs& a, int dtype, hipStream_t s) {
   return dtype == INCVIT_BF16 ? launch_t<uint16_t>(a, s) : launch_t<float>(a, s);
 }
 

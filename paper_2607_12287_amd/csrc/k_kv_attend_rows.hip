@@ -19,16 +19,6 @@ namespace incvit {
 
 namespace {
 
-// four 8-bit integers as bf16
-__device__ __forceinline__ uint2 bf_of_i8(uint32_t w) {
-  const float a = (float)(int8_t)w, b = (float)(int8_t)(w >> 8), c = (float)(int8_t)(w >> 16), d = (float)(int8_t)(w >> 24);
-  return make_uint2(f2bf2(a, b), f2bf2(c, d));
-}
-__device__ __forceinline__ uint4 bf_of_i8x8(uint32_t w0, uint32_t w1) {
-  const uint2 a = bf_of_i8(w0), b = bf_of_i8(w1);
-  return make_uint4(a.x, a.y, b.x, b.y);
-}
-
 template <int DS, int NT>
 __global__ __launch_bounds__(64 * kKeyWaves) void kv_attend_rows_kernel(AttendArgs a) {
   constexpr int NP = DS / 16, NC = (NP + 3) / 4, TAIL = NP % 4, KT = 64, KU = 4, KS = 2;
