@@ -490,14 +490,16 @@ size_t incvit_kv_bytes(const incvit_kv* c);
  * (device int32 [rows]); a row whose slot is outside the pool (padding: negative)
  * goes nowhere, wherever it stands.  The other rows of one block have to follow one
  * another: a block whose rows stand in two places, with another block's between
- * them, holds anything afterwards.  Of rows of one slot the last one stays.  For
- * each block that is written, and head:
- *   a = max |x| over the new rows' values, s_new = a / 127 rounded to fp32 (NaN
- *     where a value is not finite), s = max(s_old, s_new), NaN if either is;
+ * them, holds anything afterwards.  Of rows of one slot the last one stays, and the
+ * others count for nothing.  For each block that is written, and head:
+ *   a = max |x| over the values of the new rows that stay, s_new = a / 127 rounded
+ *     to fp32 (NaN where a value is not finite), s = max(s_old, s_new), NaN if
+ *     either is;
  *   new values: x / s rounded to fp32, then to the nearest integer (ties to
  *     even), limited to 127;
  *   kept ones, where s > s_old: q * r rounded to fp32, then to the nearest
- *     integer, with r = s_old / s rounded to fp32;
+ *     integer, with r = s_old / s rounded to fp32, which moves a kept value by up to
+ *     about s / 2 each time that the scale grows;
  * and with s zero or NaN all integers are 0.  A block keeps nothing (s_old and
  * the other slots are 0) if all of its slots are written, or if begin is 1 and
  * its first slot is: a sequence that goes on into a block used before.
@@ -529,7 +531,10 @@ incvit_status incvit_kv_read(const incvit_kv* c, const void* cache, int32_t dtyp
  * out = sum_j softmax_j(scale * q . k_j) v_j over the keys it sees, zeros where it
  * sees none; keys and values that it does not see have no effect on it, whatever
  * they hold.  Scores, softmax and sums are fp32; with bf16 the weights are rounded
- * to bf16, or to the sum of two, for their product with the values; one rounding to dtype at the end.
+ * to bf16, or to the sum of two, for their product with the values; one rounding to
+ * dtype at the end.  The sum over a row's keys is divided last and has weights up to
+ * 2^8: 2^8 times the sum of its values' magnitudes must be finite in fp32, and over a
+ * cache also the products of the queries with the integers.
  * head_dim: as incvit_kv's, of keys and values alike; q_heads a multiple of
  * kv_heads, both in [1, 1024]; window and sinks in [0, 2^30]; fill 0 or 1; scale >
  * 0, scale * log2(e) finite. */

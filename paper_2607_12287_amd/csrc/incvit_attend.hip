@@ -26,9 +26,12 @@ constexpr long kFewRows = 1024;
 // Rows times query heads, up to which a wave has one tile of 16 rows and not two, so
 // that there are more workgroups: twice as many up to 128 dims, where two fit a CU's
 // LDS.  Only for sequences of enough rows, which do not wait for memory, and whose
-// keys are not shared anyway.  Measured, 16 heads in groups of 4, one tile | two, us: a
-// prompt of 2048 rows and heads of 64 37 | 49, 128 60 | 68, 256 106 | 135 (with a window
-// of 512 64 | 54); 1024 rows of 256 50 | 73; of 4096 rows, 128: 137 | 136, 6000: 288 | 216.
+// keys are not shared anyway.  Measured, 16 heads in groups of 4, one tile | two, us, a
+// prompt that sees everything, then with a window of 512:
+//   1024 rows, heads of 64: 18 | 25, 13 | 18; 128: 29 | 35, 19 | 24; 256: 48 | 69, 31 | 45;
+//   2048 rows,          64: 34 | 45, 16 | 18; 128: 57 | 63, 23 | 25; 256: 99 | 129, 60 | 49;
+//   4096 rows,          64: 72 | 91, 24 | 23; 128: 126 | 130, 44 | 32; 256: 358 | 270, 121 | 96.
+// Rows alone decide: where a window turns the order (2048 rows of 256, 4096 of 64), two.
 // 64 sequences of 24 rows and 1024 keys, 128: 74 | 46; 512 rows, 8192 keys: 76 | 59.
 constexpr long kOneTileRows = 16384, kOneTileEach = 256;
 

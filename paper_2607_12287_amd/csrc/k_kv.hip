@@ -13,7 +13,7 @@
 // of the values (4 tokens together, of which it takes a byte of each dim).
 //
 // Both are bound by memory where rows are many: 8192 rows of 16 heads of 64 in bf16,
-// written 16.1 us for 33.6 MB in and 16.8 MB out (counters: 33.7 and 16.5; 3.1 TB/s of
+// written 15.6 us for 33.6 MB in and 16.8 MB out (counters: 33.7 and 16.5; 3.2 TB/s of
 // a copy's 5.1), read 11.3 us for the same the other way (4.5 TB/s; 25.2 MB in, since
 // 8 tokens' keys share a line and workgroups on two XCDs read it).  Few rows are a chain of
 // latencies: slots, rows and what the block keeps, then the waves' exchange (one row
@@ -26,9 +26,12 @@ namespace incvit {
 namespace {
 
 // rows * heads * 2.  A wave that finds nothing to do costs, and so does taking blocks
-// in turn; measured, us, for 1, 4 and 16 rows: 256 sequences' tokens (4096 items)
-// 7.1, 12.8, 39.9; 1024 of 16 heads (32768) 40.3, 35.1, 52.4; 2728 scattered rows
-// (87296) 39.3, 27.8, 29.8; a prompt of 8192 (262144) 68.8, 45.2, 16.4.
+// in turn; measured, us, for 1, 4 and 16 (32) rows: 256 sequences' tokens (4096 items)
+// 6.5, 12.1, 39.6; 1024 of 16 heads (32768) 37.7, 32.3, 50.0; 2728 scattered rows
+// (87392) 22.5, 16.1, 14.1; a prompt of 8192 (262144) 61.2, 40.5, 14.6, in blocks of 32
+// 16.7, of 64 18.5, of 128 186, 66.0, 25.6: of the workgroups there, which look for
+// starts among 32 rows, three of four find none.  fp32, 8 heads of 128: 16.8 in blocks
+// of 16 (84 MB), 27 of 64.
 constexpr int64_t kFewItems = 8192, kManyItems = 32768;
 
 __device__ __forceinline__ float kv_scale(float top) {
